@@ -65,7 +65,7 @@ extern "C" {
 typedef struct mlp2_plan_s* mlp2_plan_t; /* opaque; created by mlp2_plan, freed by mlp2_destroy */
 
 enum mlp2_act { MLP2_ACT_IDENTITY = 0, MLP2_ACT_GELU_TANH = 1, MLP2_ACT_SWIGLU = 2 };
-enum mlp2_dtype { MLP2_DTYPE_BF16 = 0 };
+enum mlp2_dtype { MLP2_DTYPE_BF16 = 0, MLP2_DTYPE_F32 = 1 /* mlp2_norm_* and mlp2_ortho_* only */ };
 /* MLP2_MODE_SENTINEL is the pipelined launch with the Lamport-style
  * synchronisation the paper discusses as an alternative (Sec. V-A): GEMM1
  * tiles store the intermediate at device scope with no fence and no ready
@@ -363,6 +363,82 @@ int mlp2_chain_trace_attach(mlp2_chain_t plan, void* buffer, int records_per_gro
 
 /* Free the chain plan and its workspace (synchronises the device first).  NULL-safe. */
 void mlp2_chain_destroy(mlp2_chain_t plan);
+
+/* ---- Training.  Three operators make a training step of a pre-norm MLP
+ * block: the two-layer MLP with its backward pass, layer norm with its
+ * backward pass, and the orthogonalised update of the weights.  Each has a
+ * plan that owns its workspace; its calls enqueue on `stream` (a hipStream_t;
+ * NULL = the default stream), allocate nothing, synchronise nothing and use no
+ * atomics on results: the same inputs give the same bits.  A plan's calls are
+ * ordered on one stream; it must not run on two at once.  All pointers are
+ * device pointers that the caller owns; an output must not overlap an input or
+ * another output (MLP2_ERR_INVALID_ARG). */
+typedef struct mlp2_train_s* mlp2_train_t;
+typedef struct mlp2_norm_s* mlp2_norm_t;
+typedef struct mlp2_ortho_s* mlp2_ortho_t;
+
+/* Plan the MLP Y = act(X . W1) . W2 for training with up to max_rows rows a
+ * call: 1 <= max_rows <= 1<<20, H and F multiples of 64 in [64, 1<<18], act in
+ * enum mlp2_act, dtype MLP2_DTYPE_BF16.  Layouts as mlp2_plan; there is no
+ * 4 GB limit on the operands.  NULL on failure (mlp2_last_error). */
+mlp2_train_t mlp2_train_plan(int64_t max_rows, int64_t H, int64_t F, int act, int dtype);
+
+/* Forward pass over M rows (0 <= M <= max_rows; 0 does nothing): Y [M, H] and
+ * the pre-activations P that the backward pass needs, bf16 [M, F], for SwiGLU
+ * [2, M, F] (X . Wg, then X . Wu).  Z is computed from the fp32 sums, not from
+ * the rounded P.  For inference alone mlp2_run does the same without P. */
+int mlp2_train_forward(mlp2_train_t plan, int64_t M, const void* X, const void* W1, const void* W2, void* P, void* Y, void* stream);
+
+/* Backward pass: from dY [M, H] and the forward pass's X, W1, W2 and P the
+ * gradients dX [M, H], dW1 (as W1) and dW2 [F, H], all bf16 and overwritten.
+ * A NULL gradient is not computed (at least one must be given).  The
+ * intermediate gradient dP is rounded to bf16.  With M = 0 the weights'
+ * gradients are zeros (and the inputs may be NULL). */
+int mlp2_train_backward(mlp2_train_t plan, int64_t M, const void* dY, const void* X, const void* W1, const void* W2, const void* P,
+                        void* dX, void* dW1, void* dW2, void* stream);
+
+/* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
+void mlp2_train_destroy(mlp2_train_t plan);
+
+/* Plan layer norm over rows of H elements, up to max_rows rows a call:
+ * 1 <= max_rows <= 1<<24, 1 <= H <= 16384.  x_dtype is the type of X and dX,
+ * y_dtype that of Y and dY: both bf16, both F32, or F32 and bf16 (a 32-bit
+ * residual stream).  Weight, bias, statistics and their gradients are F32. */
+mlp2_norm_t mlp2_norm_plan(int64_t max_rows, int64_t H, int x_dtype, int y_dtype);
+
+/* Y = (X - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps), eps >= 0.
+ * ldx and ldy (>= H) are the rows' strides in elements; rows may start at any
+ * element.  weight (NULL: ones) and bias (NULL: zeros) hold H values; mean and
+ * rstd receive M values each for the backward pass, or are NULL. */
+int mlp2_norm_forward(mlp2_norm_t plan, int64_t M, const void* X, int64_t ldx, const float* weight, const float* bias, float eps,
+                      void* Y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Gradients of X, weight and bias from dY and the forward pass's mean and
+ * rstd.  dweight and dbias (H values, overwritten) may be NULL.  With M = 0
+ * both are zeros (and the other pointers may be NULL). */
+int mlp2_norm_backward(mlp2_norm_t plan, int64_t M, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* weight,
+                       const float* mean, const float* rstd, void* dX, int64_t lddx, float* dweight, float* dbias, void* stream);
+
+/* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
+void mlp2_norm_destroy(mlp2_norm_t plan);
+
+/* Plan the orthogonalisation of `count` matrices [rows, cols] at a time (the
+ * two weights of a gated layer, a stack of layers): 1 <= count <= 4096, rows
+ * and cols in [1, 65536], dtype (of the input) bf16 or F32. */
+mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtype);
+
+/* O [count, rows, cols] bf16 from G: each matrix scaled to X = G / (|G|_F +
+ * eps), then `steps` (1 .. 64) times X <- a X + (b A + c A A) X with A = X X^T
+ * (on the shorter side), (a, b, c) = coeffs[3 k .. 3 k + 2] of step k (host
+ * array of 3 * steps floats of magnitude <= 64, read during the call).  The
+ * products are fp16 with fp32 sums; X is held in 22 bits.  Coefficients must
+ * keep X's singular values below 4 (the usual ones stay below 1.3): beyond
+ * that the fp16 intermediates overflow to infinity and the result is NaN.  A
+ * zero matrix gives zeros (with eps > 0); a NaN or infinity in G gives NaN. */
+int mlp2_ortho_run(mlp2_ortho_t plan, const void* G, void* O, int steps, const float* coeffs, float eps, void* stream);
+
+/* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
+void mlp2_ortho_destroy(mlp2_ortho_t plan);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(PKG, "libmlp2.so")
 TRACE_LIB_PATH = os.path.join(PKG, "libmlp2_trace.so")
 
 ACT_IDENTITY, ACT_GELU_TANH, ACT_SWIGLU = 0, 1, 2
-DTYPE_BF16 = 0
+DTYPE_BF16, DTYPE_F32 = 0, 1
 MODE_SEQUENTIAL, MODE_TILE_PIPELINED, MODE_WORKQUEUE, MODE_STAGE1, MODE_STAGE2, MODE_SENTINEL = 0, 1, 2, 3, 4, 5
 MODES = {"sequential": MODE_SEQUENTIAL, "tile_pipelined": MODE_TILE_PIPELINED, "workqueue": MODE_WORKQUEUE,
          "stage1": MODE_STAGE1, "stage2": MODE_STAGE2, "sentinel": MODE_SENTINEL}
@@ -45,6 +45,17 @@ EXPORTS = (
     "mlp2_chain_grid",
     "mlp2_chain_trace_attach",
     "mlp2_run_noalloc",
+    "mlp2_train_plan",
+    "mlp2_train_forward",
+    "mlp2_train_backward",
+    "mlp2_train_destroy",
+    "mlp2_norm_plan",
+    "mlp2_norm_forward",
+    "mlp2_norm_backward",
+    "mlp2_norm_destroy",
+    "mlp2_ortho_plan",
+    "mlp2_ortho_run",
+    "mlp2_ortho_destroy",
 )
 
 
@@ -168,6 +179,24 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.mlp2_run_noalloc.restype = ctypes.c_int
     lib.mlp2_run_noalloc.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_int,
                                      P, P, P, P, P, ctypes.c_int]
+    I64, F32 = ctypes.c_int64, ctypes.c_float
+    for name in ("train", "norm", "ortho"):
+        getattr(lib, f"mlp2_{name}_plan").restype = P
+        getattr(lib, f"mlp2_{name}_destroy").restype = None
+        getattr(lib, f"mlp2_{name}_destroy").argtypes = [P]
+    lib.mlp2_train_plan.argtypes = [I64, I64, I64, ctypes.c_int, ctypes.c_int]
+    lib.mlp2_train_forward.restype = ctypes.c_int
+    lib.mlp2_train_forward.argtypes = [P, I64] + [P] * 6
+    lib.mlp2_train_backward.restype = ctypes.c_int
+    lib.mlp2_train_backward.argtypes = [P, I64] + [P] * 9
+    lib.mlp2_norm_plan.argtypes = [I64, I64, ctypes.c_int, ctypes.c_int]
+    lib.mlp2_norm_forward.restype = ctypes.c_int
+    lib.mlp2_norm_forward.argtypes = [P, I64, P, I64, P, P, F32, P, I64, P, P, P]
+    lib.mlp2_norm_backward.restype = ctypes.c_int
+    lib.mlp2_norm_backward.argtypes = [P, I64, P, I64, P, I64, P, P, P, P, I64, P, P, P]
+    lib.mlp2_ortho_plan.argtypes = [I64, I64, I64, ctypes.c_int]
+    lib.mlp2_ortho_run.restype = ctypes.c_int
+    lib.mlp2_ortho_run.argtypes = [P, P, P, ctypes.c_int, ctypes.POINTER(F32), F32, P]
     _lib = lib
     return lib
 
@@ -385,3 +414,192 @@ class ChainPlan:
         rc = self.lib.mlp2_chain_set_spin_limit(self.handle, int(polls))
         if rc != OK:
             raise Mlp2Error(rc, "mlp2_chain_set_spin_limit")
+
+
+def _stream(stream, device) -> int:
+    import torch
+
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _dtype_code(dtype) -> int:
+    import torch
+
+    codes = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+    if dtype not in codes:
+        raise TypeError(f"{dtype} is not supported: bfloat16 or float32")
+    return codes[dtype]
+
+
+def _check_shape(t, name, shape, dtype, device, rows=False):
+    """``t`` is a ``dtype`` tensor of ``shape`` on ``device``; contiguous, or with ``rows`` a matrix of contiguous rows."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, is {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+    if rows:
+        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name}'s rows must be contiguous and apart from each other")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _row_stride(t) -> int:
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+
+
+class _Owned:
+    """A plan handle, freed with its object."""
+
+    _name = ""
+
+    def _create(self, *args):
+        import torch
+
+        self.lib = load()
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        h = getattr(self.lib, f"mlp2_{self._name}_plan")(*args)
+        if not h:
+            raise Mlp2Error(self.lib.mlp2_last_error(), f"mlp2_{self._name}_plan")
+        self.handle = ctypes.c_void_p(h)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            getattr(self.lib, f"mlp2_{self._name}_destroy")(self.handle)
+            self.handle = None
+
+    def __del__(self):  # pragma: no cover - best effort
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _done(self, rc, call):
+        if rc != OK:
+            raise Mlp2Error(rc, f"mlp2_{self._name}_{call}")
+
+
+class TrainPlan(_Owned):
+    """Training of ``Y = act(X @ W1) @ W2`` with up to ``max_rows`` rows a call, on the current device.
+
+    ``W1`` is ``[H, F]``, for SwiGLU ``[2, H, F]``; ``forward`` also writes the
+    pre-activations ``P`` (``[M, F]`` or ``[2, M, F]``) that ``backward`` takes.
+    A leading 1 in ``W1``, ``P`` and ``dW1`` of an MLP without gate is accepted.
+    """
+
+    _name = "train"
+
+    def __init__(self, max_rows: int, H: int, F: int, act: int):
+        self.max_rows, self.H, self.F, self.act = int(max_rows), int(H), int(F), int(act)
+        self._create(self.max_rows, self.H, self.F, self.act, DTYPE_BF16)
+
+    def _check(self, t, name, *shape):
+        import torch
+
+        lead = 2 if self.act == ACT_SWIGLU else 1
+        if name in ("W1", "P", "dW1") and (lead == 2 or t.dim() == 3):
+            shape = (lead,) + shape
+        _check_shape(t, name, shape, torch.bfloat16, self.device)
+
+    def forward(self, X, W1, W2, P, Y, stream=None) -> None:
+        """Enqueue ``P = X @ W1`` and ``Y = act(P) @ W2`` on ``stream`` (default: torch's current stream)."""
+        M, H, F = int(X.shape[0]), self.H, self.F
+        for t, name, shape in ((X, "X", (M, H)), (W1, "W1", (H, F)), (W2, "W2", (F, H)), (P, "P", (M, F)), (Y, "Y", (M, H))):
+            self._check(t, name, *shape)
+        self._done(self.lib.mlp2_train_forward(self.handle, M, _ptr(X), _ptr(W1), _ptr(W2), _ptr(P), _ptr(Y),
+                                               _stream(stream, self.device)), "forward")
+
+    def backward(self, dY, X, W1, W2, P, dX=None, dW1=None, dW2=None, stream=None) -> None:
+        """Enqueue the gradients that are asked for (None: not computed)."""
+        M, H, F = int(X.shape[0]), self.H, self.F
+        for t, name, shape in ((dY, "dY", (M, H)), (X, "X", (M, H)), (W1, "W1", (H, F)), (W2, "W2", (F, H)), (P, "P", (M, F)),
+                               (dX, "dX", (M, H)), (dW1, "dW1", (H, F)), (dW2, "dW2", (F, H))):
+            if t is not None or not name.startswith(("dX", "dW")):
+                self._check(t, name, *shape)
+        self._done(self.lib.mlp2_train_backward(self.handle, M, _ptr(dY), _ptr(X), _ptr(W1), _ptr(W2), _ptr(P), _ptr(dX),
+                                                _ptr(dW1), _ptr(dW2), _stream(stream, self.device)), "backward")
+
+
+class NormPlan(_Owned):
+    """Layer norm over rows of ``H`` elements, up to ``max_rows`` rows a call, on the current device.
+
+    ``x_dtype`` is the type of ``X`` and ``dX``, ``y_dtype`` (default: the same)
+    that of ``Y`` and ``dY``; everything else is float32.  Matrices may have any
+    row stride.
+    """
+
+    _name = "norm"
+
+    def __init__(self, max_rows: int, H: int, x_dtype=None, y_dtype=None):
+        import torch
+
+        self.max_rows, self.H = int(max_rows), int(H)
+        self.x_dtype = torch.bfloat16 if x_dtype is None else x_dtype
+        self.y_dtype = self.x_dtype if y_dtype is None else y_dtype
+        self._create(self.max_rows, self.H, _dtype_code(self.x_dtype), _dtype_code(self.y_dtype))
+
+    def _vectors(self, **named):
+        import torch
+
+        for name, (t, n) in named.items():
+            if t is not None:
+                _check_shape(t, name, (n,), torch.float32, self.device)
+
+    def forward(self, X, weight, bias, Y, mean=None, rstd=None, eps=1e-5, stream=None) -> None:
+        """Enqueue ``Y = (X - mean) * rstd * weight + bias`` (None: no weight, no bias, statistics not written)."""
+        M = int(X.shape[0])
+        _check_shape(X, "X", (M, self.H), self.x_dtype, self.device, rows=True)
+        _check_shape(Y, "Y", (M, self.H), self.y_dtype, self.device, rows=True)
+        self._vectors(weight=(weight, self.H), bias=(bias, self.H), mean=(mean, M), rstd=(rstd, M))
+        self._done(self.lib.mlp2_norm_forward(self.handle, M, _ptr(X), _row_stride(X), _ptr(weight), _ptr(bias), float(eps),
+                                              _ptr(Y), _row_stride(Y), _ptr(mean), _ptr(rstd),
+                                              _stream(stream, self.device)), "forward")
+
+    def backward(self, dY, X, weight, mean, rstd, dX, dweight=None, dbias=None, stream=None) -> None:
+        """Enqueue the gradients of X, and of weight and bias where asked for."""
+        M = int(X.shape[0])
+        _check_shape(dY, "dY", (M, self.H), self.y_dtype, self.device, rows=True)
+        _check_shape(X, "X", (M, self.H), self.x_dtype, self.device, rows=True)
+        _check_shape(dX, "dX", (M, self.H), self.x_dtype, self.device, rows=True)
+        self._vectors(weight=(weight, self.H), mean=(mean, M), rstd=(rstd, M), dweight=(dweight, self.H), dbias=(dbias, self.H))
+        self._done(self.lib.mlp2_norm_backward(self.handle, M, _ptr(dY), _row_stride(dY), _ptr(X), _row_stride(X), _ptr(weight),
+                                               _ptr(mean), _ptr(rstd), _ptr(dX), _row_stride(dX), _ptr(dweight), _ptr(dbias),
+                                               _stream(stream, self.device)), "backward")
+
+
+#: The quintic of the Muon optimiser: five steps bring singular values of (0.003, 1] to about (0.7, 1.2).
+ORTHO_COEFFS = (3.4445, -4.7750, 2.0315)
+
+
+class OrthoPlan(_Owned):
+    """Newton-Schulz orthogonalisation of ``count`` matrices ``[rows, cols]`` at a time, on the current device."""
+
+    _name = "ortho"
+
+    def __init__(self, count: int, rows: int, cols: int, dtype=None):
+        import torch
+
+        self.shape = (int(count), int(rows), int(cols))
+        self.dtype = torch.float32 if dtype is None else dtype
+        self._create(*self.shape, _dtype_code(self.dtype))
+
+    def run(self, G, O, steps: int = 5, coeffs=ORTHO_COEFFS, eps: float = 1e-7, stream=None) -> None:
+        """Enqueue ``steps`` steps on the matrices G (``[count, rows, cols]``; ``[rows, cols]`` for one) into the bf16 O.
+
+        ``coeffs``: three numbers for every step, or ``steps`` triples."""
+        import torch
+
+        flat = [float(v) for c in coeffs for v in (c if hasattr(c, "__len__") else (c,))]
+        if len(flat) == 3:
+            flat = flat * int(steps)
+        if len(flat) != 3 * int(steps):
+            raise ValueError(f"coeffs must hold 3 or {3 * int(steps)} numbers")
+        for t, name, dtype in ((G, "G", self.dtype), (O, "O", torch.bfloat16)):
+            _check_shape(t, name, self.shape[1:] if self.shape[0] == 1 and t.dim() == 2 else self.shape, dtype, self.device)
+        arr = (ctypes.c_float * len(flat))(*flat)
+        self._done(self.lib.mlp2_ortho_run(self.handle, _ptr(G), _ptr(O), int(steps), arr, float(eps),
+                                           _stream(stream, self.device)), "run")

@@ -1,0 +1,451 @@
+// Layer norm over the rows of a matrix, forward and backward.
+//
+//   y  = (x - mean) rstd w + b,   rstd = (var + eps)^(-1/2)
+//   dx = rstd (g - mean(g) - xhat mean(g xhat)),   g = dy w,  xhat = (x - mean) rstd
+//   dw = sum over rows of dy xhat,   db = sum over rows of dy
+//
+// Both directions are bound by memory traffic.  A row is held in registers by
+// a group of 64 to 1024 threads (up to 16 elements a thread), so each input is
+// read once; the variance is taken around the mean in a second pass over the
+// registers.  The groups of a persistent grid walk the rows with the weights
+// (forward) or the running dw and db of their columns (backward) in registers.
+// The backward pass leaves one partial dw and db per work-group, and a second
+// small kernel adds these in a fixed order: no atomics, the same bits each run.
+#include <new>
+
+#include "mlp2_device.hpp"
+#include "mlp2_host.h"
+
+namespace mlp2 {
+
+constexpr int kNormMaxWidth = 16384;
+constexpr int kNormBlock = 1024;  // backward: threads of a work-group
+
+// Rows may start at any element: 16-byte accesses with the alignment of one element.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// 8 elements from p, of which the first n exist (the others are 0).
+__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    const u32x4 q = *reinterpret_cast<const u32x4_any*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __builtin_bit_cast(float, q[i] << 16);
+      v[2 * i + 1] = __builtin_bit_cast(float, q[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? __builtin_bit_cast(float, (uint32_t)p[i] << 16) : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = a[i];
+      v[4 + i] = b[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
+  const u32x4 q = pack_bf16x8(v);
+  if (n >= 8) {
+    *reinterpret_cast<u32x4_any*>(p) = q;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_any*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = v[i];
+  }
+}
+
+// Sums of N values over a group of NT threads, in every thread of it.  The
+// groups of a work-group call it together; `buf` alternates between two
+// regions, so one barrier a call is enough.
+template <int NT, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], float (*buf)[N]) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d);
+  if constexpr (NT > 64) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) buf[wave][i] = v[i];
+    __syncthreads();
+    constexpr int W = NT / 64;
+    const int first = wave / W * W;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += buf[first + w][i];
+      v[i] = s;
+    }
+  }
+}
+
+struct NormArgs {
+  const void* X;
+  const void* dY;
+  void* Y;          // forward: Y; backward: dX
+  const float* w;   // null: ones
+  const float* b;   // null: zeros
+  float* mean;      // forward: written (may be null); backward: read
+  float* rstd;
+  float* part;      // backward: [work-groups][2][H], or null
+  int64_t ldx, ldd, ldy;
+  int M, H;
+  float eps;
+};
+
+// NT threads a row, C pieces of 8 elements a thread: NT * 8 * C >= H.
+template <class XT, class YT, int NT, int C>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_norm_forward(const NormArgs a) {
+  constexpr int BLOCK = NT < 256 ? 256 : NT, GROUPS = BLOCK / NT;
+  __shared__ float buf[2][BLOCK / 64][1];
+  const int t = threadIdx.x % NT, group = threadIdx.x / NT;
+  const float inv = 1.0f / (float)a.H;
+  float w[C][8], b[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = 8 * (t + NT * c), n = a.H - col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[c][i] = 1.f;
+      b[c][i] = 0.f;
+    }
+    if (a.w && n > 0) load8(a.w + col, n, w[c]);
+    if (a.b && n > 0) load8(a.b + col, n, b[c]);
+  }
+  for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += gridDim.x * GROUPS) {
+    const int row = row0 + group;
+    const bool live = row < a.M;
+    const XT* x = (const XT*)a.X + (int64_t)(live ? row : row0) * a.ldx;
+    float v[C][8], s[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (t + NT * c), n = a.H - col;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] = 0.f;
+      if (n > 0) load8(x + col, n, v[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[0] += v[c][i];
+    }
+    group_sum<NT>(s, buf[0]);
+    const float mean = s[0] * inv;
+    s[0] = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int n = a.H - 8 * (t + NT * c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[c][i] -= mean;
+        s[0] += i < n ? v[c][i] * v[c][i] : 0.f;
+      }
+    }
+    group_sum<NT>(s, buf[1]);
+    const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
+    if (live && t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    YT* y = (YT*)a.Y + (int64_t)row * a.ldy;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (t + NT * c), n = a.H - col;
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = v[c][i] * rstd * w[c][i] + b[c][i];
+      if (live && n > 0) store8(y + col, n, o);
+    }
+  }
+}
+
+template <class XT, class YT, int NT, int C>
+__global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) {
+  constexpr int GROUPS = kNormBlock / NT;
+  __shared__ float buf[2][kNormBlock / 64][2];
+  const int t = threadIdx.x % NT, group = threadIdx.x / NT;
+  const float inv = 1.0f / (float)a.H;
+  float dw[C][8], db[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[c][i] = db[c][i] = 0.f;
+  int turn = 0;
+  for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += gridDim.x * GROUPS, turn ^= 1) {
+    const int row = row0 + group;
+    const bool live = row < a.M;
+    const int64_t at = live ? row : row0;
+    const XT* x = (const XT*)a.X + at * a.ldx;
+    const YT* dy = (const YT*)a.dY + at * a.ldd;
+    const float mean = a.mean[at], rstd = a.rstd[at];
+    float xh[C][8], g[C][8], s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (t + NT * c), n = live ? a.H - col : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) xh[c][i] = g[c][i] = 0.f;
+      if (n > 0) {
+        load8(x + col, n, xh[c]);
+        load8(dy + col, n, g[c]);
+      }
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = 1.f;
+      if (a.w && n > 0) load8(a.w + col, n, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        xh[c][i] = i < n ? (xh[c][i] - mean) * rstd : 0.f;
+        dw[c][i] += g[c][i] * xh[c][i];
+        db[c][i] += g[c][i];
+        g[c][i] *= w[i];
+        s[0] += g[c][i];
+        s[1] += g[c][i] * xh[c][i];
+      }
+    }
+    group_sum<NT>(s, buf[turn]);
+    const float m0 = s[0] * inv, m1 = s[1] * inv;
+    XT* dx = (XT*)a.Y + (int64_t)row * a.ldy;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (t + NT * c), n = a.H - col;
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = rstd * (g[c][i] - m0 - xh[c][i] * m1);
+      if (live && n > 0) store8(dx + col, n, o);
+    }
+  }
+  if (!a.part) return;
+  // The groups' sums of the same columns meet in LDS, one piece after the other.
+  __shared__ float sums[GROUPS > 1 ? GROUPS : 1][NT * 8 + 8];
+  float* to = a.part + (int64_t)blockIdx.x * 2 * a.H;
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (t + NT * c), n = a.H - col;
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = which ? db[c][i] : dw[c][i];
+      if constexpr (GROUPS > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[group][i * NT + t] = v[i];
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            v[i] = 0.f;
+            for (int g = 0; g < GROUPS; ++g) v[i] += sums[g][i * NT + t];
+          }
+        }
+      }
+      if (group == 0 && n > 0) store8(to + (int64_t)which * a.H + col, n, v);
+    }
+}
+
+// dw and db from the work-groups' partials: 64 columns of [parts][2 H] a work-group, 16 threads a column.
+__global__ __launch_bounds__(1024) void k_norm_reduce(const float* part, int parts, int H, float* dw, float* db) {
+  __shared__ float sums[16][65];
+  const int lane = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (col < 2 * (int64_t)H)
+    for (int p = y; p < parts; p += 16) s += part[(int64_t)p * 2 * H + col];
+  sums[y][lane] = s;
+  __syncthreads();
+  if (y == 0 && col < 2 * (int64_t)H) {
+    s = 0.f;
+    for (int i = 0; i < 16; ++i) s += sums[i][lane];
+    float* to = col < H ? dw : db;
+    if (to) to[col < H ? col : col - H] = s;
+  }
+}
+
+}  // namespace mlp2
+
+using namespace mlp2;
+
+struct mlp2_norm_s {
+  int64_t rows = 0, H = 0;
+  int x = 0, y = 0, device = -1, num_cus = 0;
+  float* part = nullptr;
+  int max_parts = 0;
+};
+
+namespace {
+
+// Threads of a row: the fewest of 64, 128, ... 1024 whose 16 elements each cover it.
+int row_threads(int64_t H) {
+  int nt = 64;
+  while (nt * 16 < H) nt *= 2;
+  return nt;
+}
+
+template <class XT, class YT, int NT, int C>
+void launch_norm(bool forward, const NormArgs& a, int grid, hipStream_t s) {
+  if (forward) k_norm_forward<XT, YT, NT, C><<<grid, NT < 256 ? 256 : NT, 0, s>>>(a);
+  else k_norm_backward<XT, YT, NT, C><<<grid, kNormBlock, 0, s>>>(a);
+}
+
+template <class XT, class YT>
+hipError_t launch_norm(bool forward, const NormArgs& a, int nt, int grid, hipStream_t s) {
+  if (a.H <= 512) launch_norm<XT, YT, 64, 1>(forward, a, grid, s);
+  else if (nt == 64) launch_norm<XT, YT, 64, 2>(forward, a, grid, s);
+  else if (nt == 128) launch_norm<XT, YT, 128, 2>(forward, a, grid, s);
+  else if (nt == 256) launch_norm<XT, YT, 256, 2>(forward, a, grid, s);
+  else if (nt == 512) launch_norm<XT, YT, 512, 2>(forward, a, grid, s);
+  else launch_norm<XT, YT, 1024, 2>(forward, a, grid, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm(const mlp2_norm_s* p, bool forward, const NormArgs& a, int grid, hipStream_t s) {
+  const int nt = row_threads(p->H);
+  if (p->x == MLP2_DTYPE_BF16) return launch_norm<uint16_t, uint16_t>(forward, a, nt, grid, s);
+  if (p->y == MLP2_DTYPE_BF16) return launch_norm<float, uint16_t>(forward, a, nt, grid, s);
+  return launch_norm<float, float>(forward, a, nt, grid, s);
+}
+
+int64_t size_of(int dtype) { return dtype == MLP2_DTYPE_BF16 ? 2 : 4; }
+
+// Bytes from a matrix's first element to its last.
+int64_t extent(int64_t M, int64_t H, int64_t ld, int dtype) { return M > 0 ? ((M - 1) * ld + H) * size_of(dtype) : 0; }
+
+bool aligned(const void* p, int64_t a) { return (uintptr_t)p % (uint64_t)a == 0; }
+
+}  // namespace
+
+extern "C" {
+
+mlp2_norm_t mlp2_norm_plan(int64_t max_rows, int64_t H, int x_dtype, int y_dtype) {
+  clear_error();
+  const bool known = (x_dtype == MLP2_DTYPE_BF16 || x_dtype == MLP2_DTYPE_F32) && (y_dtype == MLP2_DTYPE_BF16 || y_dtype == MLP2_DTYPE_F32);
+  if (max_rows < 1 || H < 1 || !known) {
+    record_error(MLP2_ERR_INVALID_ARG);
+    return nullptr;
+  }
+  if (max_rows > (1 << 24) || H > kNormMaxWidth || (x_dtype == MLP2_DTYPE_BF16 && y_dtype == MLP2_DTYPE_F32)) {
+    record_error(MLP2_ERR_UNSUPPORTED);
+    return nullptr;
+  }
+  int device = -1, cus = 0;
+  if (const int rc = current_device(&device, &cus)) {
+    record_error(rc);
+    return nullptr;
+  }
+  auto* p = new (std::nothrow) mlp2_norm_s();
+  if (!p) {
+    record_error(MLP2_ERR_HIP);
+    return nullptr;
+  }
+  p->rows = max_rows;
+  p->H = H;
+  p->x = x_dtype;
+  p->y = y_dtype;
+  p->device = device;
+  p->num_cus = cus;
+  p->max_parts = cus;  // one backward work-group per CU
+  if (hipMalloc((void**)&p->part, (size_t)p->max_parts * 2 * H * sizeof(float)) != hipSuccess) {
+    (void)hipGetLastError();
+    delete p;
+    record_error(MLP2_ERR_HIP);
+    return nullptr;
+  }
+  return p;
+}
+
+int mlp2_norm_forward(mlp2_norm_t p, int64_t M, const void* X, int64_t ldx, const float* weight, const float* bias, float eps,
+                      void* Y, int64_t ldy, float* mean, float* rstd, void* stream) {
+  if (!p || M < 0 || M > p->rows || !(eps >= 0.f)) return record_error(MLP2_ERR_INVALID_ARG);
+  if (M == 0) return MLP2_OK;
+  if (!X || !Y || ldx < p->H || ldy < p->H) return record_error(MLP2_ERR_INVALID_ARG);
+  if (!aligned(X, size_of(p->x)) || !aligned(Y, size_of(p->y)) || !aligned(weight, 4) || !aligned(bias, 4) || !aligned(mean, 4) ||
+      !aligned(rstd, 4))
+    return record_error(MLP2_ERR_ALIGNMENT);
+  const Span in[] = {{X, extent(M, p->H, ldx, p->x)}, {weight, p->H * 4}, {bias, p->H * 4}};
+  const Span out[] = {{Y, extent(M, p->H, ldy, p->y)}, {mean, M * 4}, {rstd, M * 4}};
+  if (outputs_overlap(in, out)) return record_error(MLP2_ERR_INVALID_ARG);
+  if (!on_device(p->device)) return record_error(MLP2_ERR_DEVICE);
+  NormArgs a{};
+  a.X = X;
+  a.Y = Y;
+  a.w = weight;
+  a.b = bias;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.ldx = ldx;
+  a.ldy = ldy;
+  a.M = (int)M;
+  a.H = (int)p->H;
+  a.eps = eps;
+  const int nt = row_threads(p->H), groups = nt < 256 ? 256 / nt : 1, block = nt < 256 ? 256 : nt;
+  const int64_t blocks = (M + groups - 1) / groups, most = (int64_t)p->num_cus * (2048 / block);
+  const hipError_t e = launch_norm(p, true, a, (int)(blocks < most ? blocks : most), (hipStream_t)stream);
+  return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP);
+}
+
+int mlp2_norm_backward(mlp2_norm_t p, int64_t M, const void* dY, int64_t lddy, const void* X, int64_t ldx, const float* weight,
+                       const float* mean, const float* rstd, void* dX, int64_t lddx, float* dweight, float* dbias, void* stream) {
+  if (!p || M < 0 || M > p->rows) return record_error(MLP2_ERR_INVALID_ARG);
+  if (M > 0 && (!dY || !X || !mean || !rstd || !dX || lddy < p->H || ldx < p->H || lddx < p->H)) return record_error(MLP2_ERR_INVALID_ARG);
+  if (!aligned(dY, size_of(p->y)) || !aligned(X, size_of(p->x)) || !aligned(dX, size_of(p->x)) || !aligned(weight, 4) ||
+      !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
+    return record_error(MLP2_ERR_ALIGNMENT);
+  const Span in[] = {{dY, extent(M, p->H, lddy, p->y)}, {X, extent(M, p->H, ldx, p->x)}, {weight, p->H * 4}, {mean, M * 4}, {rstd, M * 4}};
+  const Span out[] = {{dX, extent(M, p->H, lddx, p->x)}, {dweight, p->H * 4}, {dbias, p->H * 4}};
+  if (outputs_overlap(in, out)) return record_error(MLP2_ERR_INVALID_ARG);
+  if (!on_device(p->device)) return record_error(MLP2_ERR_DEVICE);
+  hipStream_t s = (hipStream_t)stream;
+  const bool grads = dweight || dbias;
+  int parts = 0;
+  if (M > 0) {
+    NormArgs a{};
+    a.X = X;
+    a.dY = dY;
+    a.Y = dX;
+    a.w = weight;
+    a.mean = const_cast<float*>(mean);
+    a.rstd = const_cast<float*>(rstd);
+    a.part = grads ? p->part : nullptr;
+    a.ldx = ldx;
+    a.ldd = lddy;
+    a.ldy = lddx;
+    a.M = (int)M;
+    a.H = (int)p->H;
+    const int groups = kNormBlock / row_threads(p->H);
+    const int64_t blocks = (M + groups - 1) / groups;
+    parts = (int)(blocks < p->max_parts ? blocks : p->max_parts);
+    const hipError_t e = launch_norm(p, false, a, parts, s);
+    if (e != hipSuccess) return record_error(MLP2_ERR_HIP);
+  }
+  if (grads) {
+    k_norm_reduce<<<(unsigned)((2 * p->H + 63) / 64), 1024, 0, s>>>(p->part, parts, (int)p->H, dweight, dbias);
+    if (hipGetLastError() != hipSuccess) return record_error(MLP2_ERR_HIP);
+  }
+  return MLP2_OK;
+}
+
+void mlp2_norm_destroy(mlp2_norm_t p) {
+  if (!p) return;
+  release_on(p->device, p->part);
+  delete p;
+}
+
+}  // extern "C"
