@@ -13,65 +13,13 @@
 // small kernel adds these in a fixed order: no atomics, the same bits each run.
 #include <new>
 
-#include "mlp2_device.hpp"
 #include "mlp2_host.h"
+#include "mlp2_vector.hpp"
 
 namespace mlp2 {
 
 constexpr int kNormMaxWidth = 16384;
 constexpr int kNormBlock = 1024;  // backward: threads of a work-group
-
-// Rows may start at any element: 16-byte accesses with the alignment of one element.
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-
-// 8 elements from p, of which the first n exist (the others are 0).
-__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    const u32x4 q = *reinterpret_cast<const u32x4_any*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __builtin_bit_cast(float, q[i] << 16);
-      v[2 * i + 1] = __builtin_bit_cast(float, q[i] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? __builtin_bit_cast(float, (uint32_t)p[i] << 16) : 0.f;
-  }
-}
-__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = a[i];
-      v[4 + i] = b[i];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
-  }
-}
-__device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
-  const u32x4 q = pack_bf16x8(v);
-  if (n >= 8) {
-    *reinterpret_cast<u32x4_any*>(p) = q;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
-  }
-}
-__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_any*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = v[i];
-  }
-}
 
 // Sums of N values over a group of NT threads, in every thread of it.  The
 // groups of a work-group call it together; `buf` alternates between two

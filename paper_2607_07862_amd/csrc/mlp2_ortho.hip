@@ -3,8 +3,10 @@
 //   X = G / (|G|_F + eps), then `steps` times
 //   A = X X^T,  B = b A + c A A,  X <- a X + B X
 //
-// on the short side: a tall matrix takes A = X^T X and X <- a X + X B, so
-// nothing is transposed.  Every product runs on the matrix cores in fp16 with
+// on the short side: a tall matrix is transposed where it is scaled, and its
+// result on the way out, so that A = X X^T has K contiguous in both operands
+// (the fastest order).  A and B are symmetric: only their tiles on and above the
+// diagonal are computed, and stored twice.  Every product runs on the matrix cores in fp16 with
 // fp32 sums.  fp16 rather than bf16 because the iteration lifts the small
 // singular values by up to a^steps, and with them what rounding leaves there:
 // the values are bounded (the singular values stay below about 1.3), so the
@@ -28,6 +30,7 @@
 
 #include "mlp2_host.h"
 #include "mlp2_product.hpp"
+#include "mlp2_vector.hpp"
 
 namespace mlp2 {
 
@@ -50,7 +53,10 @@ __device__ __forceinline__ void unpack_f16x8(u32x4 q, float (&v)[8]) {
 }
 // v as upper + lower fp16.
 __device__ __forceinline__ void store_split(uint16_t* hi, uint16_t* lo, const float (&v)[8]) {
-  const u32x4 h = pack_f16x8(v);
+  u32x4 h = pack_f16x8(v);
+  // The rest is taken from the bits that are stored: left to itself the compiler converts twice, once from v and once inside the
+  // instruction that makes v, which rounds differently in one element of some thousands.
+  asm volatile("" : "+v"(h));
   float up[8], rest[8];
   unpack_f16x8(h, up);
 #pragma unroll
@@ -58,9 +64,6 @@ __device__ __forceinline__ void store_split(uint16_t* hi, uint16_t* lo, const fl
   *reinterpret_cast<u32x4*>(hi) = h;
   *reinterpret_cast<u32x4*>(lo) = pack_f16x8(rest);
 }
-
-__device__ __forceinline__ float load_value(const uint16_t* p) { return __builtin_bit_cast(float, (uint32_t)*p << 16); }
-__device__ __forceinline__ float load_value(const float* p) { return *p; }
 
 __device__ __forceinline__ float block_sum(float v, float* buf) {
 #pragma unroll
@@ -78,57 +81,84 @@ __global__ __launch_bounds__(256) void k_ortho_squares(const T* G, int64_t n, fl
   __shared__ float buf[4];
   const T* g = G + (int64_t)blockIdx.y * n;
   float s = 0.f;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const float v = load_value(g + i);
-    s += v * v;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048) {
+    float v[8];
+    load8(g + i, (int)min(n - i, (int64_t)8), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += v[e] * v[e];
   }
   s = block_sum(s, buf);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * kOrthoParts + blockIdx.x] = s;
 }
 
-// The first X: G scaled, zeros in the padding.  One thread an 8-element piece of the padded matrix.
-template <class T>
-__global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int cols, int prows, int pcols, const float* part,
-                                                     int parts, float eps, float scale, uint16_t* hi, uint16_t* lo) {
+// The first X [n][m] (n <= m, padded to 64): G, transposed if it is tall, scaled, zeros in the padding.  One 64 x 64 block a work-group.
+template <class T, bool TALL>
+__global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int cols, int n, int m, const float* part, int parts,
+                                                     float eps, float scale, uint16_t* hi, uint16_t* lo) {
   __shared__ float buf[4];
+  __shared__ float block[64][65];
   const float* mine = part + (int64_t)blockIdx.y * kOrthoParts;
   const float norm = sqrtf(block_sum((int)threadIdx.x < parts ? mine[threadIdx.x] : 0.f, buf));
   const float by = scale / (norm + eps);
   const T* g = G + (int64_t)blockIdx.y * rows * cols;
-  const int64_t pieces = (int64_t)prows * (pcols / 8), base = (int64_t)blockIdx.y * prows * pcols;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
-    const int row = (int)(i / (pcols / 8)), col = (int)(i % (pcols / 8)) * 8;
-    float v[8];
+  const int64_t base = (int64_t)blockIdx.y * n * m;
+  const int across = m / 64, i0 = blockIdx.x / across * 64, j0 = blockIdx.x % across * 64;  // of X
+  float v[2][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = row < rows && col + e < cols ? load_value(g + (int64_t)row * cols + col + e) * by : 0.f;
-    store_split(hi + base + 8 * i, lo + base + 8 * i, v);
+  for (int h = 0; h < 2; ++h) {
+    const int r = threadIdx.x / 8 + 32 * h, c = threadIdx.x % 8 * 8;
+    const int row = (TALL ? j0 : i0) + r, col = (TALL ? i0 : j0) + c;  // of G
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[h][e] = 0.f;
+    if (row < rows && col < cols) load8(g + (int64_t)row * cols + col, cols - col, v[h]);
+    if constexpr (TALL) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) block[c + e][r] = v[h][e];
+    }
+  }
+  if constexpr (TALL) __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = threadIdx.x / 8 + 32 * h, c = threadIdx.x % 8 * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[h][e] = (TALL ? block[r][c + e] : v[h][e]) * by;
+    const int64_t at = base + (int64_t)(i0 + r) * m + j0 + c;
+    store_split(hi + at, lo + at, v[h]);
   }
 }
 
-// A = X X^T (or X^T X) in the scale of A.
+// A = X X^T in the scale of A.
 struct StoreGram {
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kSymmetric = true, kMirror = true;
   uint16_t* A;
-  int n;
+  int n, rows;  // rows: n
   float by;
-  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ void mirror(int batch, int row, int col, u32x4 q) const {
+    *reinterpret_cast<u32x4*>(A + ((int64_t)batch * n + row) * n + col) = q;
+  }
+  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8]) const {
     float o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = v[i] * by;
-    *reinterpret_cast<u32x4*>(A + ((int64_t)batch * n + row) * n + col) = pack_f16x8(o);
+    const u32x4 q = pack_f16x8(o);
+    mirror(batch, row, col, q);
+    return q;
   }
 };
 
 // B = b A + c A A, its diagonal apart in the last steps.
 struct StorePoly {
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kSymmetric = true, kMirror = true;
   const uint16_t* A;
   uint16_t* B;
   float* diag;  // [matrices][n]
-  int n;
+  int n, rows;  // rows: n
   float b, c;   // in the scales of the operands
   int apart;
-  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ void mirror(int batch, int row, int col, u32x4 q) const {
+    *reinterpret_cast<u32x4*>(B + ((int64_t)batch * n + row) * n + col) = q;
+  }
+  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8]) const {
     const int64_t at = ((int64_t)batch * n + row) * n + col;
     float o[8];
     unpack_f16x8(*reinterpret_cast<const u32x4*>(A + at), o);
@@ -140,51 +170,62 @@ struct StorePoly {
         if (apart) o[i] = 0.f;
       }
     }
-    *reinterpret_cast<u32x4*>(B + at) = pack_f16x8(o);
+    const u32x4 q = pack_f16x8(o);
+    *reinterpret_cast<u32x4*>(B + at) = q;
+    return q;
   }
 };
 
-// X <- (a + diag B) X + (the rest of B) X, or the last step's result in bf16.
-template <bool TALL, bool LAST>
-struct StoreUpdate {
-  static constexpr bool kGated = false;
+// X <- (a + diag B) X + (the rest of B) X.
+struct Update {
   const uint16_t *hi, *lo;
-  uint16_t *hi_out, *lo_out;
   const float* diag;
-  int64_t ld, plane;  // of the padded matrices
-  int n;
+  int64_t n, m;
   float a, by;
-  uint16_t* O;        // LAST: [matrices][rows][cols]
-  int rows, cols;
-  float out_by;
-  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8]) const {
-    const int64_t at = batch * plane + row * ld + col;
-    float h[8], l[8], d[8], o[8];
+  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8], float (&o)[8]) const {
+    const int64_t at = ((int64_t)batch * n + row) * m + col;
+    float h[8], l[8];
     unpack_f16x8(*reinterpret_cast<const u32x4*>(hi + at), h);
     unpack_f16x8(*reinterpret_cast<const u32x4*>(lo + at), l);
-    const float* dg = diag + (int64_t)batch * n + (TALL ? col : row);
+    const float d = a + diag[batch * n + row];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      d[i] = a + dg[TALL ? i : 0];
-      o[i] = d[i] * h[i] + (d[i] * l[i] + by * v[i]);
+    for (int i = 0; i < 8; ++i) o[i] = d * h[i] + (d * l[i] + by * v[i]);
+  }
+};
+struct StoreUpdate {
+  static constexpr bool kGated = false, kSymmetric = false, kMirror = false;
+  Update x;
+  uint16_t *hi, *lo;
+  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8]) const {
+    float o[8];
+    x(batch, row, col, v, o);
+    const int64_t at = ((int64_t)batch * x.n + row) * x.m + col;
+    store_split(hi + at, lo + at, o);
+  }
+};
+
+// The last step's result in bf16, transposed back if G is tall.
+template <bool TALL>
+struct StoreLast {
+  static constexpr bool kGated = false, kSymmetric = false, kMirror = TALL;
+  Update x;
+  uint16_t* O;  // [matrices][g_rows][g_cols]
+  int g_rows, g_cols;
+  int rows;     // TALL: of X, padded
+  float out_by;
+  __device__ __forceinline__ void mirror(int batch, int col, int row, u32x4 q) const {
+    if (col < g_rows && row < g_cols) store8_packed(O + ((int64_t)batch * g_rows + col) * g_cols + row, g_cols - row, q);
+  }
+  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8]) const {
+    float o[8];
+    x(batch, row, col, v, o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] *= out_by;
+    const u32x4 q = pack_bf16x8(o);
+    if constexpr (!TALL) {
+      if (row < g_rows && col < g_cols) store8_packed(O + ((int64_t)batch * g_rows + row) * g_cols + col, g_cols - col, q);
     }
-    if constexpr (!LAST) {
-      store_split(hi_out + at, lo_out + at, o);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] *= out_by;
-      if (row >= rows) return;
-      uint16_t* p = O + ((int64_t)batch * rows + row) * cols + col;
-      const u32x4 q = pack_bf16x8(o);
-      typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));  // odd widths: rows at any element
-      if (col + 8 <= cols) {
-        *reinterpret_cast<u32x4_any*>(p) = q;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (col + i < cols) p[i] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
-      }
-    }
+    return q;
   }
 };
 
@@ -194,68 +235,56 @@ using namespace mlp2;
 
 struct mlp2_ortho_s {
   int64_t count = 0, rows = 0, cols = 0;
-  int64_t prows = 0, pcols = 0, n = 0;  // padded to 64; n: the short side, padded
+  int64_t n = 0, m = 0;  // short and long side, padded to 64
   bool tall = false;
   int dtype = 0, device = -1, num_cus = 0;
   float scale = 1.f;  // of X, a power of two near the square root of the long side
   char* ws = nullptr;
-  uint16_t* X[2][2] = {};  // [buffer][upper, lower]: [count][prows][pcols]
+  uint16_t* X[2][2] = {};  // [buffer][upper, lower]: [count][n][m]
   uint16_t *A = nullptr, *B = nullptr;  // [count][n][n]
   float *part = nullptr, *diag = nullptr;
+  SplitSpace split{};
 };
 
 namespace {
 
-template <class Tile>
 hipError_t ortho_step(const mlp2_ortho_s* p, const float* coeff, bool apart, bool last, uint16_t* const (&X)[2],
                       uint16_t* const (&out)[2], void* O, hipStream_t s) {
-  const int64_t n = p->n, plane = p->prows * p->pcols, K = p->tall ? p->prows : p->pcols;
+  const int64_t n = p->n, m = p->m;
   const int count = (int)p->count;
-  Side x = make_side(X[0], p->pcols, count * plane * 2), sq = make_side(p->A, n, count * n * n * 2);
-  x.batch = plane;
+  Side x = make_side(X[0], m, count * n * m * 2), sq = make_side(p->A, n, count * n * n * 2);
+  x.batch = n * m;
   sq.batch = n * n;
-  const StoreGram gram{p->A, (int)n, kOrthoScaleA / (p->scale * p->scale)};
-  hipError_t e = p->tall ? launch_product<Tile, Fp16, true, true>(x, x, n, n, K, count, gram, s)
-                         : launch_product<Tile, Fp16, false, false>(x, x, n, n, K, count, gram, s);
+  const StoreGram gram{p->A, (int)n, (int)n, kOrthoScaleA / (p->scale * p->scale)};
+  hipError_t e = product<Fp16, false, false>(x, x, n, n, m, count, gram, p->split, p->num_cus, s);
   if (e != hipSuccess) return e;
-  const StorePoly poly{p->A, p->B, p->diag, (int)n, coeff[1] * kOrthoScaleB / kOrthoScaleA,
+  const StorePoly poly{p->A, p->B, p->diag, (int)n, (int)n, coeff[1] * kOrthoScaleB / kOrthoScaleA,
                        coeff[2] * kOrthoScaleB / (kOrthoScaleA * kOrthoScaleA), apart ? 1 : 0};
-  e = launch_product<Tile, Fp16, false, false>(sq, sq, n, n, n, count, poly, s);
+  e = product<Fp16, false, false>(sq, sq, n, n, n, count, poly, p->split, p->num_cus, s);
   if (e != hipSuccess) return e;
   sq.p = p->B;
-  auto update = [&](auto epi) {
-    epi.hi = X[0];
-    epi.lo = X[1];
-    epi.hi_out = out[0];
-    epi.lo_out = out[1];
-    epi.diag = p->diag;
-    epi.ld = p->pcols;
-    epi.plane = plane;
-    epi.n = (int)n;
-    epi.a = coeff[0];
-    epi.by = 1.f / kOrthoScaleB;
-    epi.O = (uint16_t*)O;
-    epi.rows = (int)p->rows;
-    epi.cols = (int)p->cols;
-    epi.out_by = 1.f / p->scale;
-    return epi;
-  };
-  if (p->tall) {
-    if (last) return launch_product<Tile, Fp16, false, false>(x, sq, p->prows, p->pcols, n, count, update(StoreUpdate<true, true>{}), s);
-    return launch_product<Tile, Fp16, false, false>(x, sq, p->prows, p->pcols, n, count, update(StoreUpdate<true, false>{}), s);
-  }
-  if (last) return launch_product<Tile, Fp16, false, true>(sq, x, p->prows, p->pcols, n, count, update(StoreUpdate<false, true>{}), s);
-  return launch_product<Tile, Fp16, false, true>(sq, x, p->prows, p->pcols, n, count, update(StoreUpdate<false, false>{}), s);
+  const Update update{X[0], X[1], p->diag, n, m, coeff[0], 1.f / kOrthoScaleB};
+  if (!last) return product<Fp16, false, true>(sq, x, n, m, n, count, StoreUpdate{update, out[0], out[1]}, p->split, p->num_cus, s);
+  const int rows = (int)p->rows, cols = (int)p->cols;
+  if (p->tall)
+    return product<Fp16, false, true>(sq, x, n, m, n, count, StoreLast<true>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
+                                      p->split, p->num_cus, s);
+  return product<Fp16, false, true>(sq, x, n, m, n, count, StoreLast<false>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
+                                    p->split, p->num_cus, s);
 }
 
 template <class T>
 void ortho_first(const mlp2_ortho_s* p, const void* G, float eps, hipStream_t s) {
-  const int64_t n = p->rows * p->cols, pieces = p->prows * p->pcols / 8;
-  const int parts = (int)((n + 4095) / 4096 < kOrthoParts ? (n + 4095) / 4096 : kOrthoParts);
+  const int64_t n = p->rows * p->cols, slices = (n + 8191) / 8192;
+  const int parts = (int)(slices < kOrthoParts ? slices : kOrthoParts);
   k_ortho_squares<T><<<dim3(parts, (unsigned)p->count), 256, 0, s>>>((const T*)G, n, p->part);
-  const int64_t blocks = (pieces + 255) / 256, most = 8 * p->num_cus;
-  k_ortho_scale<T><<<dim3((unsigned)(blocks < most ? blocks : most), (unsigned)p->count), 256, 0, s>>>(
-      (const T*)G, (int)p->rows, (int)p->cols, (int)p->prows, (int)p->pcols, p->part, parts, eps, p->scale, p->X[0][0], p->X[0][1]);
+  const dim3 grid((unsigned)(p->n / 64 * (p->m / 64)), (unsigned)p->count);
+  if (p->tall)
+    k_ortho_scale<T, true><<<grid, 256, 0, s>>>((const T*)G, (int)p->rows, (int)p->cols, (int)p->n, (int)p->m, p->part, parts, eps,
+                                                p->scale, p->X[0][0], p->X[0][1]);
+  else
+    k_ortho_scale<T, false><<<grid, 256, 0, s>>>((const T*)G, (int)p->rows, (int)p->cols, (int)p->n, (int)p->m, p->part, parts, eps,
+                                                 p->scale, p->X[0][0], p->X[0][1]);
 }
 
 }  // namespace
@@ -285,18 +314,20 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   p->count = count;
   p->rows = rows;
   p->cols = cols;
-  p->prows = round_up(rows, 64);
-  p->pcols = round_up(cols, 64);
   p->tall = rows > cols;
-  p->n = p->tall ? p->pcols : p->prows;
+  p->n = round_up(p->tall ? cols : rows, 64);
+  p->m = round_up(p->tall ? rows : cols, 64);
   p->dtype = dtype;
   p->device = device;
   p->num_cus = cus;
   p->scale = std::exp2(std::round(0.5f * std::log2((float)(rows > cols ? rows : cols))));
-  const int64_t x = round_up(count * p->prows * p->pcols * 2, 256), a = round_up(count * p->n * p->n * 2, 256);
+  const int64_t x = round_up(count * p->n * p->m * 2, 256), a = round_up(count * p->n * p->n * 2, 256);
   const int64_t part = round_up(count * kOrthoParts * 4, 256), diag = round_up(count * p->n * 4, 256);
-  if (hipMalloc((void**)&p->ws, (size_t)(4 * x + 2 * a + part + diag)) != hipSuccess) {
+  const int64_t parts = (int64_t)1 << 27, counters = 4096 * kLine * 4, fixed = 4 * x + 2 * a + part + diag;
+  if (hipMalloc((void**)&p->ws, (size_t)(fixed + parts + counters)) != hipSuccess ||
+      hipMemset(p->ws + fixed + parts, 0, (size_t)counters) != hipSuccess) {
     (void)hipGetLastError();
+    (void)hipFree(p->ws);
     delete p;
     record_error(MLP2_ERR_HIP);
     return nullptr;
@@ -307,6 +338,7 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   p->B = (uint16_t*)(at + a);
   p->part = (float*)(at + 2 * a);
   p->diag = (float*)(at + 2 * a + part);
+  p->split = SplitSpace{(float*)(p->ws + fixed), parts / 4, (uint32_t*)(p->ws + fixed + parts), 4096};
   return p;
 }
 
@@ -324,7 +356,7 @@ int mlp2_ortho_run(mlp2_ortho_t p, const void* G, void* O, int steps, const floa
   else ortho_first<uint16_t>(p, G, eps, s);
   hipError_t e = hipGetLastError();
   for (int k = 0; k < steps && e == hipSuccess; ++k)
-    e = ortho_step<Tile128>(p, coeffs + 3 * k, k >= steps - kOrthoDiagSteps, k == steps - 1, p->X[k & 1], p->X[~k & 1], O, s);
+    e = ortho_step(p, coeffs + 3 * k, k >= steps - kOrthoDiagSteps, k == steps - 1, p->X[k & 1], p->X[~k & 1], O, s);
   return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP);
 }
 

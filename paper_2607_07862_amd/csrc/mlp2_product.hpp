@@ -7,9 +7,9 @@
 // index.  Here each side of the product is staged through LDS in panels of
 // its own order:
 //
-//   inner panel (K contiguous in memory): [rows][64 k], 128-byte rows, read
+//   inner panel (K contiguous in memory): [rows][k], read
 //     by ds_read_b128 (8 consecutive k per lane);
-//   outer panel (K is the slow index): [64 k][columns], read transposed by
+//   outer panel (K is the slow index): [k][columns], read transposed by
 //     ds_read_b64_tr_b16.
 //
 // Both are XOR-swizzled in 16-byte chunks and filled by direct-to-LDS buffer
@@ -47,57 +47,60 @@ struct Fp16 {
 struct Side {
   const uint16_t* p;
   int64_t ld;
-  int64_t bytes;   // readable bytes from p; anything past them reads as zero
-  int64_t panel;   // elements from a tile's first panel to its second; 0: the next rows (columns) of the same matrix
-  int64_t jump;    // elements added to the base from stage `jump_at` on (K runs through a second matrix)
-  int jump_at;     // stage of 64 k, or INT_MAX
+  int64_t bytes;   // from p to the end of the matrix (outer: of its last matrix); what lies past it reads as zero
+  int64_t panel;   // outer: elements from a tile's first panel to its second, in another matrix; 0: the next columns
+  int64_t jump;    // inner: elements added to the base from unit `jump_at` of K on (K runs on in a second matrix)
+  int jump_at;     // in units of 64 k; 0: no second matrix
   int64_t batch;   // elements between the matrices of a batch
 };
 
-// A work-group tile: ROWP row panels and COLP column panels of E rows
-// (columns) each, WM x WN waves, an NS-deep ring of 64-deep stages.  Every
-// wave owns 32 columns of every column panel (so that the two panels of a
-// gated product, gate and up weights, meet in one lane) and 16 * TM rows.
-template <int E_, int ROWP_, int COLP_, int WM_, int WN_, int NS_>
+// A work-group tile: ROWP row panels of ER rows and COLP column panels of EC
+// columns, WM x WN waves, an NS-deep ring of BK-deep stages.  Every wave owns
+// 32 columns of every column panel (so that the two panels of a gated product,
+// gate and up weights, meet in one lane) and 16 * TM rows.
+template <int ER_, int ROWP_, int EC_, int COLP_, int WM_, int WN_, int BK_, int NS_>
 struct PTile {
-  static constexpr int E = E_, ROWP = ROWP_, COLP = COLP_, WM = WM_, WN = WN_, NS = NS_;
+  static constexpr int ER = ER_, ROWP = ROWP_, EC = EC_, COLP = COLP_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
   static constexpr int NWAVES = WM * WN, THREADS = 64 * NWAVES;
-  static constexpr int BM = E * ROWP, BN = E * COLP;
+  static constexpr int BM = ER * ROWP, BN = EC * COLP;
   static constexpr int TM = BM / WM / 16;             // 16-row blocks of a wave
-  static constexpr int PANEL = E * 128;               // bytes of a panel's stage
-  static constexpr int STAGE = (ROWP + COLP) * PANEL;
-  static constexpr int PIECES = PANEL / 1024 / NWAVES;  // 1 KB loads per wave and panel
-  static constexpr int LOADS = (ROWP + COLP) * PIECES;  // and per stage
+  static constexpr int KS = BK / 32;                  // MFMA steps of a stage
+  static constexpr int RPANEL = ER * BK * 2, CPANEL = EC * BK * 2;  // bytes of a panel's stage
+  static constexpr int STAGE = ROWP * RPANEL + COLP * CPANEL;
+  static constexpr int LOADS = STAGE / 1024 / NWAVES;  // 1 KB loads per wave and stage
   static constexpr int LDS = NS * STAGE;
-  static_assert(E == 32 * WN, "a wave owns 32 columns of every column panel");
-  // Wave wm's row block tm.  Two row panels: the wave's rows lie in both halves
-  // of an eight-wave tile, in panel wm of a four-wave one.
+  static_assert(BK == 32 || BK == 64, "stage depth");
+  static_assert(EC == 32 * WN, "a wave owns 32 columns of every column panel");
+  static_assert(RPANEL % (1024 * NWAVES) == 0 && CPANEL % (1024 * NWAVES) == 0, "every wave loads whole 1 KB pieces");
+  // Wave wm's row block tm: its rows lie in both halves of an eight-wave tile, together in a four-wave one.
   __device__ static constexpr int row_of(int wm, int tm) {
     return NWAVES == 8 ? 64 * wm + 16 * (tm & 3) + 128 * (tm >> 2) : wm * (BM / WM) + 16 * tm;
   }
 };
-using Tile64 = PTile<64, 1, 1, 2, 2, 8>;    // 64 x 64
-using Tile64G = PTile<64, 1, 2, 2, 2, 5>;   // 64 x (64 + 64): gated, or 64 x 128
-using Tile128 = PTile<64, 2, 2, 2, 2, 4>;   // 128 x 128, gated 128 x (64 + 64)
+using Tile64 = PTile<64, 1, 64, 1, 2, 2, 64, 4>;    // 64 x 64
+using Tile64G = PTile<64, 1, 64, 2, 2, 2, 64, 3>;   // 64 x (64 + 64): gated
+using Tile128 = PTile<64, 2, 64, 2, 2, 2, 64, 2>;   // 128 x 128, gated 128 x (64 + 64)
+using Tile256 = PTile<128, 2, 128, 2, 2, 4, 64, 2>;  // 256 x 256, gated 256 x (128 + 128): the ping-pong loop
 
 // ------------------------------------------------------------------ panel loads
-
-__device__ __forceinline__ u32x4 panel_rsrc(const char* base, int64_t left) {
-  const uint64_t b = (uint64_t)base;
-  const uint32_t n = left <= 0 ? 0u : left > 0xFFFFFFFFll ? 0xFFFFFFFFu : (uint32_t)left;
-  return u32x4{(uint32_t)b, (uint32_t)(b >> 32) & 0xFFFFu, n, 0x00027000u};
-}
 
 // One direct-to-LDS buffer load: lane i moves 16 bytes from base + voff to
 // lds_addr + 16 i, zeros where voff is past the descriptor's range.  The wait
 // states ahead of it cover a scalar operand that a vector instruction has just
-// written (the compiler keeps them for its own instructions, not for an asm's).
+// written (5; the compiler keeps them for its own instructions, not for an
+// asm's) and the write of M0 (1).
+template <int STATES>
 __device__ __forceinline__ void dma16_buffer(u32x4 rsrc, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds_addr) : "memory");
+  asm volatile("s_nop %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds_addr), "n"(STATES - 1) : "memory");
 }
 
-// The chunk swizzle of a panel's row (inner: row of 8 chunks; outer: k row of E / 8 chunks).
-__device__ __forceinline__ int swz_inner(int row) { return (row >> 1) & 7; }
+// The chunk swizzle of a panel's row.  Inner: rows of BK / 8 chunks, so that
+// the 16 rows of one ds_read_b128 group lie in different banks.  Outer: k rows
+// of E / 8 chunks, so that the 4 k rows of one ds_read_b64_tr_b16 group do.
+template <int BK>
+__device__ __forceinline__ int swz_inner(int row) {
+  return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
 template <int E>
 __device__ __forceinline__ int swz_outer(int k) {
   return E == 128 ? (4 * (k & 3)) ^ (2 * ((k >> 3) & 1)) : (4 * ((k >> 1) & 1)) ^ (2 * ((k >> 3) & 1));
@@ -107,81 +110,91 @@ __device__ __forceinline__ int swz_outer(int k) {
 // hold their rows permuted within every 32 (LDS row 16 t + i is matrix row
 // 8 (i / 4) + 4 t + i % 4), so that a pair of blocks gives a lane 8 consecutive
 // columns; outer panels get the same from the fragment addresses.
-template <class T, bool OUTER, bool COL>
+//
+// The base moves on by one stage a load; the range is kept as follows.
+//   inner: every stage may read the rows that exist, rows * ld elements from
+//     the panel's first row; the columns of a stage always exist (K is a
+//     multiple of 64), so the range does not change.
+//   outer: a stage may read its own BK rows of k, the last one those that are
+//     left.  Columns past the matrix's width read the next row's, or zeros;
+//     either way they belong to results that are not stored.
+template <class T, bool OUTER, bool COL, bool JUMP>
 struct PanelLoad {
+  static constexpr int E = COL ? T::EC : T::ER, BK = T::BK, BYTES = COL ? T::CPANEL : T::RPANEL;
+  static constexpr int PIECES = BYTES / 1024 / T::NWAVES;
+  static_assert(!JUMP || !OUTER, "a second matrix along K is inner");
   const char* base;
-  int64_t left, step, jump;
-  int to_jump;
-  uint32_t voff, piece_step;
-  uint32_t lds;  // of this wave's first piece, from the stage's base
+  uint32_t range, tail;  // of every stage; outer: of the last stage
+  uint32_t step;
+  int64_t jump;
+  int left;              // outer: stages before the last; inner: before the second matrix
+  uint32_t voff[PIECES];
+  uint32_t lds;          // of this wave's first piece, from the stage's base
 
-  __device__ __forceinline__ PanelLoad(const Side& s, int64_t batch, int i0, int panel, int stage0, uint32_t lds_off) {
+  __device__ static __forceinline__ uint32_t clamp(int64_t v) { return v <= 0 ? 0u : v > 0xFFFFFFFFll ? 0xFFFFFFFFu : (uint32_t)v; }
+
+  // Stages stage0 .. stage0 + nk - 1 (of BK) of the panel of rows (columns) from i0 + panel * E on.
+  __device__ __forceinline__ PanelLoad(const Side& s, int64_t batch, int i0, int panel, int stage0, int nk, uint32_t lds_off) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, wave = uniform(tid >> 6);
-    constexpr int E = T::E;
-    int64_t first = batch * s.batch + (int64_t)panel * (s.panel ? s.panel : OUTER ? E : E * s.ld);
-    first += OUTER ? i0 + (int64_t)stage0 * 64 * s.ld : (int64_t)i0 * s.ld + (int64_t)stage0 * 64;
-    step = (OUTER ? 64 * s.ld : 64) * 2;
-    jump = s.jump * 2;
-    to_jump = s.jump_at - stage0;
-    if (to_jump <= 0) first += s.jump;
-    base = (const char*)(s.p + first);
-    left = s.bytes - 2 * first;
-    int row, chunk;
+    uint32_t piece_step;
     if constexpr (OUTER) {
+      const int col = i0 + (s.panel ? 0 : panel * E);
+      const int64_t first = batch * s.batch + (s.panel ? panel * s.panel : 0) + col + (int64_t)stage0 * BK * s.ld;
+      base = (const char*)(s.p + first);
+      step = (uint32_t)(BK * s.ld * 2);
+      range = clamp((int64_t)step - 2 * col);
+      tail = min(range, clamp(s.bytes - 2 * (first + (int64_t)(nk - 1) * BK * s.ld)));
+      left = nk - 1;
+      if (left == 0) range = tail;
       constexpr int CPR = E / 8, RPP = 64 / CPR;  // chunks per k row, k rows per piece
-      row = RPP * wave + lane / CPR;
-      chunk = (lane % CPR) ^ swz_outer<E>(row);
+      const int row = RPP * wave + lane / CPR;
+      static_assert(T::NWAVES * RPP % 16 == 0, "the swizzle repeats from piece to piece");
+      const int chunk = (lane % CPR) ^ swz_outer<E>(row);
       piece_step = (uint32_t)(T::NWAVES * RPP * s.ld * 2);
-      voff = (uint32_t)((row * s.ld + 8 * chunk) * 2);
+      voff[0] = (uint32_t)((row * s.ld + 8 * chunk) * 2);
     } else {
-      row = 8 * wave + lane / 8;
-      chunk = (lane & 7) ^ swz_inner(row);
+      const int64_t rows = batch * s.batch + (int64_t)(i0 + panel * E) * s.ld;
+      base = (const char*)(s.p + rows + (int64_t)stage0 * BK);
+      step = BK * 2;
+      // the end of this batch's matrix: the next one's start, or the end of all
+      range = clamp((s.batch ? (batch + 1) * s.batch * 2 : s.bytes) - 2 * rows);
+      if constexpr (JUMP) {
+        jump = s.jump * 2;
+        left = s.jump_at * (64 / BK) - stage0;
+        if (left <= 0) base += jump;
+      }
+      constexpr int CPR = BK / 8, RPP = 64 / CPR;  // chunks per row, rows per piece
+      const int row = RPP * wave + lane / CPR;
+      static_assert(T::NWAVES * RPP % 32 == 0, "so do swizzle and permutation");
+      const int chunk = (lane % CPR) ^ swz_inner<BK>(row);
       const int i = row & 15;
       const int at = COL ? (row & ~31) + 8 * (i >> 2) + 4 * ((row >> 4) & 1) + (i & 3) : row;
-      piece_step = (uint32_t)(T::NWAVES * 8 * s.ld * 2);
-      voff = (uint32_t)((at * s.ld + 8 * chunk) * 2);
+      piece_step = (uint32_t)(T::NWAVES * RPP * s.ld * 2);
+      voff[0] = (uint32_t)((at * s.ld + 8 * chunk) * 2);
     }
+#pragma unroll
+    for (int j = 1; j < PIECES; ++j) voff[j] = voff[0] + j * piece_step;
     lds = lds_off + (uint32_t)wave * 1024u;
   }
+  // The next stage, into the ring slot at stage_lds.
   __device__ __forceinline__ void load(uint32_t stage_lds) {
-    const u32x4 r = panel_rsrc(base, left);
+    const uint64_t b = (uint64_t)base;  // 48 bits
+    const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32), range, 0x00027000u};
 #pragma unroll
-    for (int j = 0; j < T::PIECES; ++j)
-      dma16_buffer(r, voff + j * piece_step, uniform(stage_lds + lds + (uint32_t)(j * T::NWAVES * 1024)));
-    const int64_t by = --to_jump == 0 ? step + jump : step;
-    base += by;
-    left -= by;
+    for (int j = 0; j < PIECES; ++j) {
+      const uint32_t to = uniform(stage_lds + lds + (uint32_t)(j * T::NWAVES * 1024));
+      if (j == 0) dma16_buffer<5>(r, voff[j], to);
+      else dma16_buffer<1>(r, voff[j], to);
+    }
+    base += step;
+    if constexpr (OUTER) range = --left == 0 ? tail : range;
+    if constexpr (JUMP) base += --left == 0 ? jump : 0;
   }
 };
 
 // ------------------------------------------------------------------ fragments
-
-// Row side: lane holds row (lane % 16) of a 16-row block, k = 8 (lane / 16) .. + 7 of a 32-deep slice.
-template <class T, bool OUTER>
-struct RowFrag {
-  uint32_t off[2];  // inner: one per K slice; outer: one
-  __device__ __forceinline__ RowFrag(int wm) {
-    int tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));
-    const int lane = tid & 63;
-    const int r0 = T::NWAVES == 8 ? 64 * wm : (wm * (T::BM / T::WM)) % T::E;
-    const uint32_t panel = T::NWAVES == 8 ? 0u : (uint32_t)((wm * (T::BM / T::WM)) / T::E * T::PANEL);
-    if constexpr (OUTER) {
-      // lane 4 r + c of group g addresses k row 8 g + r, columns 4 c .. + 3 of the block
-      const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), c = lane & 3;
-      off[0] = panel + (uint32_t)(k * (2 * T::E) + ((((r0 >> 3) + (c >> 1)) ^ swz_outer<T::E>(k)) << 4) + 8 * (c & 1));
-      off[1] = 0;
-    } else {
-      const int row = r0 + (lane & 15);
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) off[ks] = panel + (uint32_t)(row * 128 + (((4 * ks + (lane >> 4)) ^ swz_inner(row)) << 4));
-    }
-  }
-  // block tm of K slice ks; `stage` is the address of the stage's row panels
-  __device__ __forceinline__ u32x4 read(const char* stage, int ks, int tm) const;
-};
 
 __device__ __forceinline__ u32x4 read_tr(const char* p, int upper) {
   const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(p));
@@ -190,21 +203,45 @@ __device__ __forceinline__ u32x4 read_tr(const char* p, int upper) {
   return __builtin_bit_cast(u32x4, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Row side: lane holds row (lane % 16) of a 16-row block, k = 8 (lane / 16) .. + 7 of a 32-deep slice.
 template <class T, bool OUTER>
-__device__ __forceinline__ u32x4 RowFrag<T, OUTER>::read(const char* stage, int ks, int tm) const {
-  const int half = T::NWAVES == 8 ? tm >> 2 : 0, blk = T::NWAVES == 8 ? tm & 3 : tm;
-  if constexpr (OUTER) {
-    // Block blk is 2 blk chunks further on; the swizzle touches chunk bits 1 to 3, so the offset is XORed, not added.
-    return read_tr(stage + half * T::PANEL + (off[0] ^ (uint32_t)(32 * blk)) + ks * 64 * T::E, 8 * T::E);
-  } else {
-    return *reinterpret_cast<const u32x4*>(stage + half * T::PANEL + off[ks] + blk * 2048);
+struct RowFrag {
+  static constexpr int E = T::ER;
+  uint32_t off[T::KS];  // inner: one per K slice; outer: the first
+  __device__ __forceinline__ RowFrag(int wm) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63;
+    const int first = T::row_of(wm, 0), r0 = first % E;
+    const uint32_t panel = (uint32_t)(first / E * T::RPANEL);
+    if constexpr (OUTER) {
+      // lane 4 r + c of group g addresses k row 8 g + r, columns 4 c .. + 3 of the block
+      const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), c = lane & 3;
+      off[0] = panel + (uint32_t)(k * (2 * E) + ((((r0 >> 3) + (c >> 1)) ^ swz_outer<E>(k)) << 4) + 8 * (c & 1));
+    } else {
+      const int row = r0 + (lane & 15);
+#pragma unroll
+      for (int ks = 0; ks < T::KS; ++ks)
+        off[ks] = panel + (uint32_t)(row * (2 * T::BK) + (((4 * ks + (lane >> 4)) ^ swz_inner<T::BK>(row)) << 4));
+    }
   }
-}
+  // Block tm of K slice ks; `stage` is the address of the stage's row panels.
+  __device__ __forceinline__ u32x4 read(const char* stage, int ks, int tm) const {
+    const int half = T::NWAVES == 8 ? tm >> 2 : 0, blk = T::NWAVES == 8 ? tm & 3 : tm;
+    if constexpr (OUTER) {
+      // Block blk is 2 blk chunks further on; the swizzle touches chunk bits 1 to 3, so the offset is XORed, not added.
+      return read_tr(stage + half * T::RPANEL + (off[0] ^ (uint32_t)(32 * blk)) + ks * 64 * E, 8 * E);
+    } else {
+      return *reinterpret_cast<const u32x4*>(stage + half * T::RPANEL + off[ks] + blk * 32 * T::BK);
+    }
+  }
+};
 
 // Column side: block i of the pair that covers the wave's 32 columns of a panel.
 template <class T, bool OUTER>
 struct ColFrag {
-  uint32_t off[2];
+  static constexpr int E = T::EC;
+  uint32_t off[T::KS];
   __device__ __forceinline__ ColFrag(int wn) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
@@ -212,17 +249,17 @@ struct ColFrag {
     if constexpr (OUTER) {
       // columns 8 c + 4 i .. + 3 of the pair: the interleave that leaves 8 consecutive columns in a lane
       const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
-      off[0] = (uint32_t)(k * (2 * T::E) + (((4 * wn + (lane & 3)) ^ swz_outer<T::E>(k)) << 4));
-      off[1] = 0;
+      off[0] = (uint32_t)(k * (2 * E) + (((4 * wn + (lane & 3)) ^ swz_outer<E>(k)) << 4));
     } else {
       const int row = 32 * wn + (lane & 15);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) off[ks] = (uint32_t)(row * 128 + (((4 * ks + (lane >> 4)) ^ swz_inner(row)) << 4));
+      for (int ks = 0; ks < T::KS; ++ks)
+        off[ks] = (uint32_t)(row * (2 * T::BK) + (((4 * ks + (lane >> 4)) ^ swz_inner<T::BK>(row)) << 4));
     }
   }
   __device__ __forceinline__ u32x4 read(const char* panel, int ks, int i) const {
-    if constexpr (OUTER) return read_tr(panel + off[0] + 8 * i + ks * 64 * T::E, 8 * T::E);
-    else return *reinterpret_cast<const u32x4*>(panel + off[ks] + i * 2048);
+    if constexpr (OUTER) return read_tr(panel + off[0] + 8 * i + ks * 64 * E, 8 * E);
+    else return *reinterpret_cast<const u32x4*>(panel + off[ks] + i * 32 * T::BK);
   }
 };
 
@@ -231,8 +268,9 @@ struct ColFrag {
 template <class T>
 using Acc = f32x4[T::COLP][2][T::TM];
 
-// The plain loop: NS - 1 stages in flight, one barrier a stage.
-template <class T, class Elem, bool RO, bool CO>
+// The plain loop: NS - 1 stages in flight, one barrier a stage.  st0 and nk
+// count stages of BK.
+template <class T, class Elem, bool RO, bool CO, bool JUMP>
 __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
                                              Acc<T>& acc, char* lds) {
   const int wave = uniform((int)threadIdx.x >> 6);
@@ -245,35 +283,37 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
       for (int j = 0; j < T::TM; ++j) acc[p][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (nk <= 0) return;
   const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-  PanelLoad<T, RO, false> r0(rs, batch, m0, 0, st0, 0), r1(rs, batch, m0, T::ROWP - 1, st0, (T::ROWP - 1) * T::PANEL);
-  PanelLoad<T, CO, true> c0(cs, batch, n0, 0, st0, T::ROWP * T::PANEL),
-      c1(cs, batch, n0, T::COLP - 1, st0, (T::ROWP + T::COLP - 1) * T::PANEL);
-  auto issue = [&](int st) {
-    const uint32_t dst = lds_base + (uint32_t)((st % T::NS) * T::STAGE);
-    r0.load(dst);
-    if constexpr (T::ROWP == 2) r1.load(dst);
-    c0.load(dst);
-    if constexpr (T::COLP == 2) c1.load(dst);
+  constexpr int C0 = T::ROWP * T::RPANEL;  // the column panels of a stage
+  PanelLoad<T, RO, false, false> r0(rs, batch, m0, 0, st0, nk, 0), r1(rs, batch, m0, T::ROWP - 1, st0, nk, (T::ROWP - 1) * T::RPANEL);
+  PanelLoad<T, CO, true, JUMP> c0(cs, batch, n0, 0, st0, nk, C0),
+      c1(cs, batch, n0, T::COLP - 1, st0, nk, C0 + (T::COLP - 1) * T::CPANEL);
+  uint32_t at = lds_base;  // the ring slot that is requested next
+  auto issue = [&]() {
+    r0.load(at);
+    if constexpr (T::ROWP == 2) r1.load(at);
+    c0.load(at);
+    if constexpr (T::COLP == 2) c1.load(at);
+    at = at == lds_base + (T::NS - 1) * T::STAGE ? lds_base : at + T::STAGE;
   };
   const RowFrag<T, RO> rf(wm);
   const ColFrag<T, CO> cf(wn);
 #pragma unroll
   for (int st = 0; st < T::NS - 1; ++st)
-    if (st < nk) issue(st);
+    if (st < nk) issue();
+  const char* stage = lds;
   for (int it = 0; it < nk; ++it) {
     wait_stages_behind<T::LOADS, T::NS - 2>(min(T::NS - 2, nk - 1 - it));
     __syncthreads();
-    if (it + T::NS - 1 < nk) issue(it + T::NS - 1);
-    const char* stage = lds + (it % T::NS) * T::STAGE;
+    if (it + T::NS - 1 < nk) issue();
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int ks = 0; ks < T::KS; ++ks) {
       u32x4 x[T::TM], w[T::COLP][2];
 #pragma unroll
       for (int tm = 0; tm < T::TM; ++tm) x[tm] = rf.read(stage, ks, tm);
 #pragma unroll
       for (int p = 0; p < T::COLP; ++p)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) w[p][i] = cf.read(stage + (T::ROWP + p) * T::PANEL, ks, i);
+        for (int i = 0; i < 2; ++i) w[p][i] = cf.read(stage + C0 + p * T::CPANEL, ks, i);
 #pragma unroll
       for (int p = 0; p < T::COLP; ++p)
 #pragma unroll
@@ -281,35 +321,223 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
 #pragma unroll
           for (int tm = 0; tm < T::TM; ++tm) acc[p][i][tm] = Elem::mfma(w[p][i], x[tm], acc[p][i][tm]);
     }
+    stage = stage == lds + (T::NS - 1) * T::STAGE ? lds : stage + T::STAGE;
   }
   __syncthreads();
 }
 
-// ------------------------------------------------------------------ the kernel
+// The ping-pong loop of the 256 x 256 tile, eight waves, two to a SIMD.
+//
+// What bounds a large tile: a 64-deep stage is 2048 cycles of MFMA per SIMD
+// and its fragment reads and LDS writes take about three quarters of that, so
+// the two must overlap.  As in the forward kernels' quadrant loop the two
+// waves of a SIMD alternate (waves 0-3 run half a phase ahead of 4-7): while one
+// multiplies, the other reads its next fragments and requests loads.  A stage
+// is four phases of one output quadrant each, (A0, B0), (A0, B1), (A1, B1),
+// (A1, B0) with A the row panels and B the column panels, and a phase is a
+// memory slot and a product slot, each ended by a barrier.
+//   memory slot 0 of stage it: request A1 of stage it + 1, read B0 of stage it
+//               1:             request A0 of it + 2,       read B1 of it
+//               2:             request B0 of it + 2,       read A1 of it
+//               3:             request B1 of it + 2,       read A0 of it + 1
+//   * Visibility: a wave waits for its own pieces of a panel at the end of the
+//     memory slot before the one that reads it; a barrier lies between, and the
+//     trailing waves reach that wait one slot before the leading waves read.
+//   * Reuse: a panel read in memory slot p is complete in registers at product
+//     slot p (lgkmcnt(0)) and its ring slot is requested again in memory slot
+//     p + 2, after the barrier that ends the trailing waves' product slot p.
+// Here the two sides may have either storage order, and every panel carries
+// its own 64-bit base and range.
+template <class T, class Elem, bool RO, bool CO, bool JUMP>
+__device__ __forceinline__ void product_pingpong(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
+                                                 Acc<T>& acc, char* lds) {
+  static_assert(T::ER == 128 && T::EC == 128 && T::ROWP == 2 && T::COLP == 2 && T::NWAVES == 8 && T::BK == 64 && T::NS == 2 && T::TM == 8, "256 x 256 tile");
+  const int wave = uniform((int)threadIdx.x >> 6);
+  const int wm = wave % T::WM, wn = wave / T::WM;
+  const bool trailing = wave >= 4;
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[p][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (nk <= 0) return;
 
-// Output tiles of M x N (COLS columns of every column panel's matrix), walked
-// so that an XCD's work-groups (blockIdx % 8) share operand panels: each XCD
-// takes a contiguous range of an order that goes down `band` row tiles before
-// the next column tile.
+  const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+  PanelLoad<T, RO, false, false> pa[2] = {{rs, batch, m0, 0, st0, nk, 0}, {rs, batch, m0, 1, st0, nk, T::RPANEL}};
+  PanelLoad<T, CO, true, JUMP> pb[2] = {{cs, batch, n0, 0, st0, nk, 2 * T::RPANEL},
+                                        {cs, batch, n0, 1, st0, nk, 2 * T::RPANEL + T::CPANEL}};
+  auto load_a = [&](int half, int st) { pa[half].load(lds_base + (uint32_t)(st & 1) * T::STAGE); };  // a panel's stages come in order
+  auto load_b = [&](int half, int st) { pb[half].load(lds_base + (uint32_t)(st & 1) * T::STAGE); };
+
+  const RowFrag<T, RO> rf(wm);
+  const ColFrag<T, CO> cf(wn);
+  u32x4 xa[2][4], xb[2][4], w0[2][2], w1[2][2];
+  auto read_a = [&](u32x4 (&x)[2][4], int half, int st) {
+    const char* stage = lds + (st & 1) * T::STAGE;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int tm = 0; tm < 4; ++tm) x[ks][tm] = rf.read(stage, ks, 4 * half + tm);
+  };
+  auto read_b = [&](u32x4 (&w)[2][2], int half, int st) {
+    const char* panel = lds + (st & 1) * T::STAGE + 2 * T::RPANEL + half * T::CPANEL;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[ks][i] = cf.read(panel, ks, i);
+  };
+  auto mma = [&](const u32x4 (&w)[2][2], const u32x4 (&x)[2][4], auto bh, auto ah) {
+    constexpr int b = decltype(bh)::value, a = 4 * decltype(ah)::value;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int tm = 0; tm < 4; ++tm) acc[b][i][a + tm] = Elem::mfma(w[ks][i], x[ks][tm], acc[b][i][a + tm]);
+  };
+  using Lo = int_constant<0>;
+  using Hi = int_constant<1>;
+
+  auto slot_end = [&]() {  // a barrier that neither the compiler's memory operations nor its products cross
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto vm_wait = [&](auto n) { wait_vm<decltype(n)::value>(); };
+  auto products_begin = [&]() {  // this wave's fragment reads are complete
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+  };
+  auto products_end = [&]() {
+    __builtin_amdgcn_s_setprio(0);
+    slot_end();
+  };
+
+  // One stage.  LEFT: stages after it, counted up to 2 (fewer loads to request
+  // and to leave in flight).
+  auto stage = [&](int it, auto left_) {
+    constexpr int LEFT = decltype(left_)::value;
+    read_b(w0, 0, it);
+    if constexpr (LEFT >= 1) load_a(1, it + 1);
+    vm_wait(int_constant<LEFT >= 1 ? 10 : 2>());  // B1 of this stage
+    slot_end();
+    products_begin();
+    mma(w0, xa, Lo(), Lo());
+    products_end();
+
+    read_b(w1, 1, it);
+    if constexpr (LEFT >= 2) load_a(0, it + 2);
+    vm_wait(int_constant<LEFT >= 2 ? 10 : LEFT == 1 ? 8 : 0>());  // A1 of this stage
+    slot_end();
+    products_begin();
+    mma(w1, xa, Hi(), Lo());
+    products_end();
+
+    read_a(xb, 1, it);
+    if constexpr (LEFT >= 2) load_b(0, it + 2);
+    if constexpr (LEFT >= 1) vm_wait(int_constant<LEFT >= 2 ? 10 : 6>());  // A0 of the next stage
+    slot_end();
+    products_begin();
+    mma(w1, xb, Hi(), Hi());
+    products_end();
+
+    if constexpr (LEFT >= 1) read_a(xa, 0, it + 1);
+    if constexpr (LEFT >= 2) load_b(1, it + 2);
+    if constexpr (LEFT >= 1) {
+      vm_wait(int_constant<LEFT >= 2 ? 10 : 4>());  // B0 of the next stage
+    }
+    slot_end();
+    products_begin();
+    mma(w0, xb, Lo(), Hi());
+    products_end();
+  };
+
+  // Prologue: the first stage and all of the second but A1.
+  const bool two = nk > 1;
+  load_a(0, 0);
+  load_b(0, 0);
+  load_b(1, 0);
+  load_a(1, 0);
+  if (two) {
+    load_a(0, 1);
+    load_b(0, 1);
+    load_b(1, 1);
+    wait_vm<10>();  // A0, B0
+  } else {
+    wait_vm<4>();
+  }
+  slot_end();
+  read_a(xa, 0, 0);
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+
+  if (trailing) slot_end();
+  for (int it = 0; it < nk - 2; ++it) stage(it, int_constant<2>());
+  if (two) stage(nk - 2, int_constant<1>());
+  stage(nk - 1, int_constant<0>());
+  if (!trailing) slot_end();
+  __syncthreads();  // every wave is done reading the ring before it is reused
+}
+
+// ------------------------------------------------------------------ one product of a launch
+
+// Output tiles in launch order.  Work-groups land on the XCDs round-robin, so
+// item i runs on XCD i % 8 (up to a rotation): every XCD takes a contiguous
+// range of an order that goes down `band` row tiles before the next column
+// tile, and so shares operand panels in its L2.  `sym`: the tiles on and above
+// the diagonal only.
 struct TileWalk {
-  int tiles_m, tiles_n, band;
+  int tiles_m, tiles_n, band, sym;
+  __host__ __device__ int total() const { return sym ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n; }
   __device__ __forceinline__ void at(int item, int& tm, int& tn) const {
-    const int total = tiles_m * tiles_n, q = total / 8, r = total % 8, x = item % 8;
-    const int t = x * q + min(x, r) + item / 8;
-    const int per = band * tiles_n, g = t / per, in = t - g * per;
-    const int rows = min(band, tiles_m - g * band);
-    tn = in / rows;
-    tm = g * band + (in - tn * rows);
+    const int n = total(), q = n / 8, r = n % 8, x = item % 8;
+    int t = x * q + min(x, r) + item / 8;
+    if (!sym) {
+      const int per = band * tiles_n, g = t / per, in = t - g * per;
+      const int rows = min(band, tiles_m - g * band);
+      tn = in / rows;
+      tm = g * band + (in - tn * rows);
+      return;
+    }
+    // a band of rows i0 .. : its triangle on the diagonal, column by column, then whole columns
+    for (int i0 = 0;; i0 += band) {
+      const int rows = min(band, tiles_m - i0), tri = rows * (rows + 1) / 2, all = tri + rows * (tiles_m - i0 - rows);
+      if (t >= all) {
+        t -= all;
+        continue;
+      }
+      if (t < tri) {
+        int j = 0;
+        while (t > j) t -= ++j;
+        tn = i0 + j;
+        tm = i0 + t;
+      } else {
+        t -= tri;
+        tn = i0 + rows + t / rows;
+        tm = i0 + t % rows;
+      }
+      return;
+    }
   }
 };
 
-template <class Epi>
-struct ProductArgs {
+// RO, CO: outer sides; JUMP: the column side runs on in a second matrix.
+template <bool RO_, bool CO_, class Epi_, bool JUMP_ = false>
+struct Problem {
+  static constexpr bool RO = RO_, CO = CO_, JUMP = JUMP_;
+  using Epi = Epi_;
   Side r, c;
   int M, N;          // rows and columns of the result (of each matrix of a gated product)
-  int nk;            // 64-deep stages of K
+  int nk;            // K in units of 64
+  int split, per;    // parts of K, units of each (the last one may have fewer)
+  float* part;       // the parts' sums, fragment by fragment (split > 1)
+  uint32_t* arrived; // parts of a tile that are done, one counter a line; zero between launches
   TileWalk walk;
   Epi epi;
+  __host__ __device__ int items() const { return walk.total() * split; }
 };
 
 // 8 consecutive values of a lane: block pair (p, tm).
@@ -322,23 +550,89 @@ __device__ __forceinline__ void lane_values(const Acc<T>& acc, int p, int tm, fl
   }
 }
 
+// Split K: every part stores its fp32 sums "fragment by fragment" (1 KB runs
+// of a wave), written through to the device's point of coherence, and counts
+// its arrival; the part that arrives last adds all parts in the order 0, 1, ...
+// and goes on to the epilogue, so the bits do not depend on which one it is,
+// and no part waits.  Returns whether this work-group goes on.
+template <class T>
+__device__ __forceinline__ bool join_parts(Acc<T>& acc, float* part, uint32_t* arrived, int64_t tile, int split, int s, char* lds) {
+  constexpr int BLOCKS = T::COLP * 2 * T::TM, ITEM = T::NWAVES * BLOCKS * 256;  // floats of a part
+  const int tid = thread_here(), lane = tid & 63, wave = uniform(tid >> 6);
+  const uint32_t off = (uint32_t)(wave * BLOCKS * 1024 + lane * 16);
+  float* mine = part + (tile * split + s) * ITEM;
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i)
+    store_through16(mine, off, __builtin_bit_cast(u32x4, acc[i / (2 * T::TM)][i / T::TM % 2][i % T::TM]), i * 1024);
+  wait_all_mem();
+  __syncthreads();
+  uint32_t* last = reinterpret_cast<uint32_t*>(lds);
+  if (tid == 0) {
+    uint32_t* count = arrived + tile * kLine;
+    const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *last = before;
+    if (before == (uint32_t)split - 1) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (uniform(*last) != (uint32_t)split - 1) return false;
+  // Device-scope loads: this XCD's L2 may hold lines of an earlier launch.
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(part + tile * split * ITEM, 0, -1, 0x00027000);
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) acc[i / (2 * T::TM)][i / T::TM % 2][i % T::TM] = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int R = BLOCKS < 8 ? BLOCKS : 8;  // loads in flight
+  static_assert(BLOCKS % R == 0, "whole rounds");
+  for (int q = 0; q < split; ++q) {
+    const uint32_t from = off + (uint32_t)q * (uint32_t)(ITEM * 4);
+#pragma unroll
+    for (int i0 = 0; i0 < BLOCKS; i0 += R) {
+      u32x4 v[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)from, (i0 + i) * 1024, 16);
+#pragma unroll
+      for (int i = 0; i < R; ++i) acc[(i0 + i) / (2 * T::TM)][(i0 + i) / T::TM % 2][(i0 + i) % T::TM] += __builtin_bit_cast(f32x4, v[i]);
+    }
+  }
+  return true;
+}
+
+template <class T>
+constexpr int mirror_pitch() { return T::BM * 2 + 16; }  // bytes of a column of the tile, kept apart in banks
+template <class T, class P>
+constexpr int lds_of() {
+  constexpr int mirror = P::Epi::kMirror ? T::BN * mirror_pitch<T>() : 0;
+  return mirror > T::LDS ? mirror : T::LDS;
+}
+
 // Epi::kGated: the two column panels are the same columns of two matrices and
 // the epilogue takes both values; otherwise they are consecutive columns.
-template <class T, class Elem, bool RO, bool CO, class Epi>
-__global__ __launch_bounds__(T::THREADS) void k_product(const ProductArgs<Epi> a) {
-  __shared__ __align__(1024) char lds[T::LDS];
-  constexpr int COLS = Epi::kGated ? T::E : T::BN;  // result columns of a tile
+// Epi::kMirror: the epilogue returns 16-bit values whose transpose goes out too,
+// through LDS and Epi::mirror, in 16-byte pieces of 8 rows.
+// Epi::kSymmetric (with kMirror): the result is symmetric and only the tiles on
+// and above the diagonal are computed; those on it are not mirrored.
+// The transpose goes out for rows below Epi's `rows`: M, or M padded, where
+// zeros go out for the rows past M.
+template <class T, class Elem, class P>
+__device__ __forceinline__ void run_product(const P& a, int item, int batch, char* lds) {
+  using Epi = typename P::Epi;
+  static_assert(!Epi::kSymmetric || (Epi::kMirror && T::BM == T::BN), "square tiles on the diagonal");
+  constexpr int COLS = Epi::kGated ? T::EC : T::BN;  // result columns of a tile
+  constexpr int UNIT = 64 / T::BK;                   // stages of a unit of K
+  const int total = a.walk.total(), s = item / total, tile = item - s * total;
   int tm_, tn_;
-  a.walk.at(blockIdx.x, tm_, tn_);
+  a.walk.at(tile, tm_, tn_);
   const int m0 = tm_ * T::BM, n0 = tn_ * COLS;
-  const int batch = blockIdx.y;
+  const int st0 = s * a.per * UNIT, nk = min(a.per * UNIT, a.nk * UNIT - st0);
   Acc<T> acc;
-  product_loop<T, Elem, RO, CO>(a.r, a.c, batch, m0, n0, 0, a.nk, acc, lds);
+  if constexpr (T::NWAVES == 8) product_pingpong<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  else product_loop<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  if (a.split > 1 && !join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, lds)) return;
   const int tid = thread_here(), lane = tid & 63, wave = uniform(tid >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
+  const bool mirrored = !Epi::kSymmetric || tm_ != tn_;
+  if constexpr (Epi::kMirror) __syncthreads();  // join_parts' flag is read before the LDS is written again
 #pragma unroll
   for (int tm = 0; tm < T::TM; ++tm) {
-    const int row = m0 + T::row_of(wm, tm) + (lane & 15);
+    const int in_row = T::row_of(wm, tm) + (lane & 15), row = m0 + in_row;
     if constexpr (Epi::kGated) {
       const int block = n0 + 32 * wn;
       float g[8], u[8];
@@ -348,41 +642,232 @@ __global__ __launch_bounds__(T::THREADS) void k_product(const ProductArgs<Epi> a
     } else {
 #pragma unroll
       for (int p = 0; p < T::COLP; ++p) {
-        const int block = n0 + p * T::E + 32 * wn;
+        const int in_block = p * T::EC + 32 * wn, block = n0 + in_block;
         float v[8];
         lane_values<T>(acc, p, tm, v);
-        if (block < a.N && row < a.M) a.epi(batch, row, block + 8 * (lane >> 4), v);
+        if constexpr (Epi::kMirror) {
+          u32x4 q = {0, 0, 0, 0};
+          if (block < a.N && row < a.M) q = a.epi(batch, row, block + 8 * (lane >> 4), v);
+          uint16_t* to = reinterpret_cast<uint16_t*>(lds + (in_block + 8 * (lane >> 4)) * mirror_pitch<T>()) + in_row;
+          if (mirrored)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i * (mirror_pitch<T>() / 2)] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
+        } else {
+          if (block < a.N && row < a.M) a.epi(batch, row, block + 8 * (lane >> 4), v);
+        }
       }
     }
   }
+  if constexpr (Epi::kMirror) {
+    if (!mirrored) return;
+    __syncthreads();
+    constexpr int CH = T::BM / 8;  // 16-byte pieces of a column of the tile
+    for (int i = tid; i < T::BN * CH; i += T::THREADS) {
+      const int col = i / CH, piece = i % CH;
+      if (n0 + col < a.N && m0 + 8 * piece < a.epi.rows)
+        a.epi.mirror(batch, n0 + col, m0 + 8 * piece, *reinterpret_cast<const u32x4*>(lds + col * mirror_pitch<T>() + 16 * piece));
+    }
+  }
 }
+
+template <class T, class Elem, class P>
+__global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_product(const P a) {
+  __shared__ __align__(1024) char lds[lds_of<T, P>()];
+  run_product<T, Elem>(a, blockIdx.x, blockIdx.y, lds);
+}
+
+// Three products in one launch: the items of `a` first, then b's and c's.
+template <class T, class Elem, class PA, class PB, class PC>
+__global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_products(const PA a, const PB b, const PC c) {
+  __shared__ __align__(1024) char lds[T::LDS];
+  static_assert(!PA::Epi::kMirror && !PB::Epi::kMirror && !PC::Epi::kMirror, "no room for a transpose");
+  const int na = a.items(), nb = b.items(), item = blockIdx.x;
+  if (item < na) run_product<T, Elem>(a, item, 0, lds);
+  else if (item < na + nb) run_product<T, Elem>(b, item - na, 0, lds);
+  else run_product<T, Elem>(c, item - na - nb, 0, lds);
+}
+
+// ------------------------------------------------------------------ host side
 
 inline Side make_side(const void* p, int64_t ld, int64_t bytes) {
   Side s{};
   s.p = (const uint16_t*)p;
   s.ld = ld;
   s.bytes = bytes;
-  s.jump_at = 0x7FFFFFFF;
   return s;
 }
 
-template <class T, class Elem, bool RO, bool CO, class Epi>
-hipError_t launch_product(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const Epi& epi,
-                          hipStream_t stream) {
-  constexpr int COLS = Epi::kGated ? T::E : T::BN;
-  ProductArgs<Epi> a;
+// What a plan lends its products for split K.
+struct SplitSpace {
+  float* part;
+  int64_t part_floats;
+  uint32_t* arrived;
+  int64_t counters;
+};
+
+enum { TILE_64, TILE_128, TILE_256, TILES };
+
+// The sizes that tile and split are chosen by.
+struct Shape {
+  int64_t M, N, K;  // N: columns of a result (of each of a gated product's two)
+  int batches;
+  bool gated, symmetric;
+};
+
+// What a tile costs a work-group, in microseconds: `unit` for 64 of K with every
+// slot of the chip taken, `alone` with at most one work-group to a CU, `item`
+// once (prologue and epilogue), `join` for meeting the other parts of K and
+// `part` for each of them.  Measured with the products of 2048 x 4096 x 14336
+// (every slot taken), 24 x 4096 x 14336 and 64 x 512 x 2048.
+struct TileCost {
+  int rows, cols, slots;  // slots: work-groups to a CU
+  double unit, alone, item, join, part;
+};
+inline TileCost tile_cost(int tile, bool gated) {
+  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 8.0, 12.0, 4.0};
+  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 6.0, 1.0};
+  return {64, 64, 2, gated ? 0.80 : 0.48, gated ? 0.50 : 0.30, 2.5, 4.0, 0.5};
+}
+
+struct Choice {
+  int tile, split;
+};
+
+inline int64_t tiles_of(const Shape& s, const TileCost& t) {
+  const int64_t m = (s.M + t.rows - 1) / t.rows, n = (s.N + t.cols - 1) / t.cols;
+  return s.batches * (s.symmetric ? m * (m + 1) / 2 : m * n);
+}
+inline int64_t units_of(const Shape& s) { return (s.K + 63) / 64; }
+
+// The most parts that the workspace has room for.
+inline int64_t split_room(const Shape& s, const TileCost& t, const SplitSpace& ws) {
+  const int64_t tiles = tiles_of(s, t);
+  if (tiles < 1 || tiles > ws.counters) return 1;
+  const int64_t room = ws.part_floats / (tiles * t.rows * t.cols * (s.gated ? 2 : 1));
+  return room < 1 ? 1 : room;
+}
+
+// Time of `tiles` * split items: whole rounds of the chip's slots, then the rest.
+inline double product_time(const Shape& s, const TileCost& t, int64_t split, int num_cus) {
+  const int64_t items = tiles_of(s, t) * split, slots = (int64_t)num_cus * t.slots, per = (units_of(s) + split - 1) / split;
+  const int64_t rest = items % slots;
+  double time = (double)(items / slots) * (per * t.unit + t.item);
+  if (rest) time += per * (rest <= num_cus ? t.alone : t.unit) + t.item;
+  return split > 1 ? time + t.join + t.part * split : time;
+}
+
+// The tile and split of one product: the least of the estimates.
+inline Choice choose(const Shape& s, const SplitSpace& ws, int num_cus) {
+  Choice best{TILE_64, 1};
+  double least = 1e30;
+  for (int tile = 0; tile < TILES; ++tile) {
+    const TileCost t = tile_cost(tile, s.gated);
+    const int64_t units = units_of(s), room = split_room(s, t, ws), most = units < 32 ? units : 32;
+    for (int64_t split = 1; split <= most && split <= room; ++split) {
+      const double time = product_time(s, t, split, num_cus);
+      if (time < least) {
+        least = time;
+        best = Choice{tile, (int)split};
+      }
+    }
+  }
+  return best;
+}
+
+// One tile for products that share a launch, and the split of each: every
+// slot gets about the same work, so an item should not last longer than that.
+template <int N>
+int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&split)[N]) {
+  int best = TILE_64;
+  double least = 1e30;
+  for (int tile = 0; tile < TILES; ++tile) {
+    int parts[N];
+    double work = 0.0;
+    const TileCost t = tile_cost(tile, false);
+    int64_t items = 0;
+    for (int i = 0; i < N; ++i) {
+      items += tiles_of(s[i], t);
+      work += tiles_of(s[i], t) * (units_of(s[i]) * t.unit + t.item);
+    }
+    const double slots = (double)num_cus * t.slots, share = work / slots;
+    double longest = 0.0, extra = 0.0;
+    for (int i = 0; i < N; ++i) {
+      const int64_t tiles = tiles_of(s[i], t), units = units_of(s[i]);
+      parts[i] = 1;
+      if (!tiles) continue;
+      const double unit = items <= num_cus ? t.alone : t.unit;
+      // An item may take its share, or what it takes for the overheads not to outweigh the work.
+      const double limit = share > 3 * t.item ? share : 3 * t.item;
+      int64_t want = (int64_t)(units * unit / limit + 0.999);
+      const int64_t room = split_room(s[i], t, ws) / N;
+      if (want > room) want = room;
+      if (want > units) want = units;
+      if (want > 1) parts[i] = (int)want;
+      const double one = (double)((units + parts[i] - 1) / parts[i]) * unit + t.item + (parts[i] > 1 ? t.join + t.part * parts[i] : 0.0);
+      if (one > longest) longest = one;
+      if (parts[i] > 1) extra += (double)tiles * (parts[i] - 1) * t.item;
+    }
+    const double even = share + extra / slots, time = even > longest ? even + 0.3 * longest : longest + 0.3 * even;
+    if (time < least) {
+      least = time;
+      best = tile;
+      for (int i = 0; i < N; ++i) split[i] = parts[i];
+    }
+  }
+  return best;
+}
+
+template <class T, class P>
+P make_problem(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const typename P::Epi& epi, int split,
+               const SplitSpace& ws) {
+  constexpr int COLS = P::Epi::kGated ? T::EC : T::BN;
+  P a{};
   a.r = r;
   a.c = c;
   a.M = (int)M;
   a.N = (int)N;
   a.nk = (int)((K + 63) / 64);
+  a.part = ws.part;
+  a.arrived = ws.arrived;
   a.walk.tiles_m = (int)((M + T::BM - 1) / T::BM);
   a.walk.tiles_n = (int)((N + COLS - 1) / COLS);
-  a.walk.band = 8;
+  a.walk.band = P::Epi::kSymmetric ? 4 : 8;
+  a.walk.sym = P::Epi::kSymmetric;
+  // No part is empty, and every part of every tile has its place in the workspace.
+  const int64_t tiles = (int64_t)a.walk.total() * batches;
+  const int64_t room = tiles >= 1 && tiles <= ws.counters ? ws.part_floats / (tiles * T::BM * T::BN) : 1;
+  if (split > room) split = (int)room;
+  if (split > a.nk) split = a.nk;
+  a.per = split > 1 ? (a.nk + split - 1) / split : a.nk;
+  a.split = split > 1 ? (a.nk + a.per - 1) / a.per : 1;
   a.epi = epi;
-  auto kernel = k_product<T, Elem, RO, CO, Epi>;
-  kernel<<<dim3((unsigned)(a.walk.tiles_m * a.walk.tiles_n), (unsigned)batches), T::THREADS, 0, stream>>>(a);
+  return a;
+}
+
+template <class T, class Elem, class P>
+hipError_t launch_product(const P& a, int batches, hipStream_t stream) {
+  k_product<T, Elem, P><<<dim3((unsigned)a.items(), (unsigned)batches), T::THREADS, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+// Calls f with the tile type of a choice.
+template <bool GATED, class F>
+auto with_tile(int tile, F&& f) {
+  if (tile == TILE_256) return f(Tile256{});
+  if (tile == TILE_128) return f(Tile128{});
+  if constexpr (GATED) return f(Tile64G{});
+  else return f(Tile64{});
+}
+
+// One product with the tile and split that suit it.
+template <class Elem, bool RO, bool CO, class Epi>
+hipError_t product(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const Epi& epi, const SplitSpace& ws,
+                   int num_cus, hipStream_t stream) {
+  const Choice ch = choose({M, N, K, batches, Epi::kGated, Epi::kSymmetric}, ws, num_cus);
+  return with_tile<Epi::kGated>(ch.tile, [&](auto tile) {
+    using T = decltype(tile);
+    return launch_product<T, Elem>(make_problem<T, Problem<RO, CO, Epi>>(r, c, M, N, K, batches, epi, ch.split, ws), batches, stream);
+  });
 }
 
 }  // namespace mlp2

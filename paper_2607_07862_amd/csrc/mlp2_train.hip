@@ -10,21 +10,22 @@
 // forward one stores P and Z from one pass over X and both weights; the
 // backward one turns a tile of dZ into dP without storing dZ, and recomputes Z
 // from P there, so the forward pass keeps nothing but P.
+//
+// The weight gradients are sums over rows: both operands of Z^T dY and X^T dP
+// have K as the slow index.  Read that way on both sides (ds_read_b64_tr_b16
+// moves half of what ds_read_b128 does in the same time) they run at 1.19
+// PFLOP/s; with K contiguous on the row side at 1.47 (8192 x 8192 x 8192).  So
+// Z leaves its epilogue transposed, through LDS, and spare work-groups of the
+// same launch transpose X.  The pass is two launches: dZ with both transposes,
+// then dX, dW1 and dW2 together, whose items fill each other's last round.
 #include <climits>
 #include <new>
 
 #include "mlp2_host.h"
 #include "mlp2_product.hpp"
+#include "mlp2_vector.hpp"
 
 namespace mlp2 {
-
-__device__ __forceinline__ void unpack_bf16x8(u32x4 q, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __builtin_bit_cast(float, q[i] << 16);
-    v[2 * i + 1] = __builtin_bit_cast(float, q[i] & 0xFFFF0000u);
-  }
-}
 
 __device__ __forceinline__ float sigmoid(float t) { return 1.0f / (1.0f + exp_neg(t)); }
 
@@ -41,7 +42,7 @@ __device__ __forceinline__ void gelu_and_slope(float z, float& value, float& slo
 // P (and Z) of a tile of X W1.  Z is computed from the fp32 sums, before P is rounded.
 template <int ACT>
 struct StoreForward {
-  static constexpr bool kGated = ACT == ACT_SWIGLU;
+  static constexpr bool kGated = ACT == ACT_SWIGLU, kSymmetric = false, kMirror = false;
   uint16_t* P;  // [M, F], gated [2, M, F]
   uint16_t* Z;  // [M, F] (identity: unused, P is Z)
   int64_t plane;  // elements of one P
@@ -67,21 +68,27 @@ struct StoreForward {
   }
 };
 
-// dP and Z of a tile of dZ = dY W2^T and the P that the forward pass kept.
+// dP and Z (transposed) of a tile of dZ = dY W2^T and the P that the forward pass kept.
 template <int ACT>
 struct StoreBackward {
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kSymmetric = false, kMirror = true;
   const uint16_t* P;
   uint16_t* dP;   // [M, F], gated [M, 2 F] (gate columns, then up columns)
-  uint16_t* Z;    // [M, F] (identity: unused)
+  uint16_t* Zt;   // [F, rows]
   int64_t plane, F;
-  __device__ __forceinline__ void operator()(int, int row, int col, const float (&d)[8]) const {
+  int rows;       // M, padded to whole units of K
+  __device__ __forceinline__ void mirror(int, int col, int row, u32x4 q) const {
+    *reinterpret_cast<u32x4*>(Zt + (int64_t)col * rows + row) = q;
+  }
+  __device__ __forceinline__ u32x4 operator()(int, int row, int col, const float (&d)[8]) const {
     const int64_t at = (int64_t)row * F + col;
+    const u32x4 first = *reinterpret_cast<const u32x4*>(P + at);
     if constexpr (ACT == ACT_IDENTITY) {
       *reinterpret_cast<u32x4*>(dP + at) = pack_bf16x8(d);
+      return first;
     } else if constexpr (ACT == ACT_GELU_TANH) {
       float p[8], z[8], dp[8];
-      unpack_bf16x8(*reinterpret_cast<const u32x4*>(P + at), p);
+      unpack_bf16x8(first, p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float slope;
@@ -89,10 +96,10 @@ struct StoreBackward {
         dp[i] = d[i] * slope;
       }
       *reinterpret_cast<u32x4*>(dP + at) = pack_bf16x8(dp);
-      *reinterpret_cast<u32x4*>(Z + at) = pack_bf16x8(z);
+      return pack_bf16x8(z);
     } else {
       float g[8], u[8], z[8], dg[8], du[8];
-      unpack_bf16x8(*reinterpret_cast<const u32x4*>(P + at), g);
+      unpack_bf16x8(first, g);
       unpack_bf16x8(*reinterpret_cast<const u32x4*>(P + plane + at), u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -104,14 +111,51 @@ struct StoreBackward {
       const int64_t to = (int64_t)row * 2 * F + col;
       *reinterpret_cast<u32x4*>(dP + to) = pack_bf16x8(dg);
       *reinterpret_cast<u32x4*>(dP + to + F) = pack_bf16x8(du);
-      *reinterpret_cast<u32x4*>(Z + at) = pack_bf16x8(z);
+      return pack_bf16x8(z);
     }
   }
 };
 
+// X^T: [H, rows] from X [M, H], zeros for the rows past M.
+struct Transpose {
+  const uint16_t* X;
+  uint16_t* Xt;
+  int64_t H;
+  int M, rows;
+  __host__ __device__ int items() const { return Xt ? (int)(H / 64) * (rows / 64) : 0; }
+  // Item: one 64 x 64 block, through LDS.
+  template <int THREADS>
+  __device__ __forceinline__ void run(int item, char* lds) const {
+    constexpr int PITCH = 64 + 8;  // elements
+    uint16_t* t = reinterpret_cast<uint16_t*>(lds);
+    const int across = (int)(H / 64), h0 = item % across * 64, m0 = item / across * 64;
+    for (int i = thread_here(); i < 512; i += THREADS) {
+      const int m = i / 8, h = i % 8 * 8;
+      u32x4 q = {0, 0, 0, 0};
+      if (m0 + m < M) q = *reinterpret_cast<const u32x4*>(X + (int64_t)(m0 + m) * H + h0 + h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[(h + e) * PITCH + m] = (uint16_t)(q[e / 2] >> (16 * (e & 1)));
+    }
+    __syncthreads();
+    for (int i = thread_here(); i < 512; i += THREADS) {
+      const int h = i / 8, m = i % 8 * 8;
+      *reinterpret_cast<u32x4*>(Xt + (int64_t)(h0 + h) * rows + m0 + m) = *reinterpret_cast<const u32x4*>(t + h * PITCH + m);
+    }
+  }
+};
+
+// The first launch of the backward pass: the items of dZ, then the blocks of X^T.
+template <class T, class P>
+__global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_backward_first(const P a, const Transpose x) {
+  __shared__ __align__(1024) char lds[lds_of<T, P>()];
+  const int n = a.items(), item = blockIdx.x;
+  if (item < n) run_product<T, Bf16>(a, item, 0, lds);
+  else x.template run<T::THREADS>(item - n, lds);
+}
+
 // A bf16 result [M, N], or the two halves of its columns as matrices of their own (dW1 of a gated MLP).
 struct StorePlain {
-  static constexpr bool kGated = false;
+  static constexpr bool kGated = false, kSymmetric = false, kMirror = false;
   uint16_t* C;
   int64_t ld;
   int64_t second;  // elements from the first matrix to the second
@@ -130,32 +174,68 @@ struct mlp2_train_s {
   int64_t rows = 0, H = 0, F = 0;  // rows: the most of a call
   int act = 0, device = -1, num_cus = 0, nb = 1;
   char* ws = nullptr;
-  uint16_t* Z = nullptr;   // [rows, F]
+  uint16_t* Z = nullptr;   // forward: [rows, F]; backward: its transpose, rows padded to 64
   uint16_t* dP = nullptr;  // [rows, nb F]
+  uint16_t* Xt = nullptr;  // X^T, rows padded
+  SplitSpace split{};
 };
 
 namespace {
 
-template <class Tile, int ACT>
+template <int ACT>
 hipError_t forward_first(const mlp2_train_s* p, int64_t M, const void* X, const void* W1, void* P, hipStream_t s) {
   const int64_t H = p->H, F = p->F;
   StoreForward<ACT> epi{(uint16_t*)P, p->Z, M * F, F};
   const Side r = make_side(X, H, M * H * 2);
   Side c = make_side(W1, F, p->nb * H * F * 2);
   if (p->nb == 2) c.panel = H * F;
-  return launch_product<Tile, Bf16, false, true>(r, c, M, F, H, 1, epi, s);
+  return product<Bf16, false, true>(r, c, M, F, H, 1, epi, p->split, p->num_cus, s);
 }
 
-template <class Tile, int ACT>
-hipError_t backward_first(const mlp2_train_s* p, int64_t M, const void* dY, const void* W2, const void* P, hipStream_t s) {
+template <int ACT>
+hipError_t backward_first(const mlp2_train_s* p, int64_t M, const void* dY, const void* W2, const void* P, const Transpose& x, hipStream_t s) {
   const int64_t H = p->H, F = p->F;
-  StoreBackward<ACT> epi{(const uint16_t*)P, p->dP, p->Z, M * F, F};
-  return launch_product<Tile, Bf16, false, false>(make_side(dY, H, M * H * 2), make_side(W2, H, F * H * 2), M, F, H, 1, epi, s);
+  StoreBackward<ACT> epi{(const uint16_t*)P, p->dP, p->Z, M * F, F, (int)round_up(M, 64)};
+  const Choice ch = choose({M, F, H, 1, false, false}, p->split, p->num_cus);
+  return with_tile<false>(ch.tile, [&](auto tile) {
+    using T = decltype(tile);
+    using Dz = Problem<false, false, StoreBackward<ACT>>;
+    const Dz a = make_problem<T, Dz>(make_side(dY, H, M * H * 2), make_side(W2, H, F * H * 2), M, F, H, 1, epi, ch.split, p->split);
+    k_backward_first<T, Dz><<<a.items() + x.items(), T::THREADS, 0, s>>>(a, x);
+    return hipGetLastError();
+  });
 }
 
-template <class Tile, bool RO, bool CO>
-hipError_t plain(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, const StorePlain& epi, hipStream_t s) {
-  return launch_product<Tile, Bf16, RO, CO>(r, c, M, N, K, 1, epi, s);
+// dX = sum dP_i W1_i^T, dW1 = X^T dP and dW2 = Z^T dY in one launch.
+hipError_t backward_second(const mlp2_train_s* p, int64_t M, const void* dY, const void* W1, void* dX, void* dW1, void* dW2, hipStream_t s) {
+  using Dx = Problem<false, false, StorePlain, true>;
+  using Dw = Problem<false, true, StorePlain>;
+  const int64_t H = p->H, F = p->F, nb = p->nb, rows = round_up(M, 64);
+  // A gradient that is not asked for has no rows, and so no items.
+  const int64_t mx = dX ? M : 0, m1 = dW1 ? H : 0, m2 = dW2 ? F : 0;
+  int split[3];
+  const Shape shapes[3] = {{mx, H, nb * F, 1, false, false}, {m1, nb * F, M, 1, false, false}, {m2, H, M, 1, false, false}};
+  const int tile = choose_shared(shapes, p->split, p->num_cus, split);
+  Side w1 = make_side(W1, F, H * F * 2);
+  w1.jump_at = (int)(F / 64);  // without a gate K ends there
+  w1.jump = H * F - F;
+  // Each product has a third of the workspace for its parts.
+  SplitSpace ws[3];
+  for (int i = 0; i < 3; ++i) {
+    ws[i] = SplitSpace{p->split.part + i * (p->split.part_floats / 3 / 64 * 64), p->split.part_floats / 3 / 64 * 64,
+                       p->split.arrived + i * (p->split.counters / 3) * kLine, p->split.counters / 3};
+  }
+  return with_tile<false>(tile, [&](auto t) {
+    using T = decltype(t);
+    const Dx x = make_problem<T, Dx>(make_side(p->dP, nb * F, M * nb * F * 2), w1, mx, H, nb * F, 1, StorePlain{(uint16_t*)dX, H, 0, INT_MAX},
+                                     split[0], ws[0]);
+    const Dw a = make_problem<T, Dw>(make_side(p->Xt, rows, H * rows * 2), make_side(p->dP, nb * F, M * nb * F * 2), m1, nb * F, M, 1,
+                                     StorePlain{(uint16_t*)dW1, F, H * F, nb == 2 ? (int)F : INT_MAX}, split[1], ws[1]);
+    const Dw b = make_problem<T, Dw>(make_side(p->Z, rows, F * rows * 2), make_side(dY, H, M * H * 2), m2, H, M, 1,
+                                     StorePlain{(uint16_t*)dW2, H, 0, INT_MAX}, split[2], ws[2]);
+    k_products<T, Bf16, Dx, Dw, Dw><<<x.items() + a.items() + b.items(), T::THREADS, 0, s>>>(x, a, b);
+    return hipGetLastError();
+  });
 }
 
 int status(hipError_t e) { return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP); }
@@ -191,15 +271,20 @@ mlp2_train_t mlp2_train_plan(int64_t max_rows, int64_t H, int64_t F, int act, in
   p->nb = act == MLP2_ACT_SWIGLU ? 2 : 1;
   p->device = device;
   p->num_cus = cus;
-  const int64_t z = round_up(max_rows * F * 2, 256), dp = round_up(max_rows * F * 2 * p->nb, 256);
-  if (hipMalloc((void**)&p->ws, (size_t)(z + dp)) != hipSuccess) {
+  const int64_t padded = round_up(max_rows, 64), z = padded * F * 2, dp = z * p->nb, xt = padded * H * 2;
+  const int64_t parts = (int64_t)1 << 27, counters = 4096 * kLine * 4;
+  if (hipMalloc((void**)&p->ws, (size_t)(z + dp + xt + parts + counters)) != hipSuccess ||
+      hipMemset(p->ws + z + dp + xt + parts, 0, (size_t)counters) != hipSuccess) {
     (void)hipGetLastError();
+    (void)hipFree(p->ws);
     delete p;
     record_error(MLP2_ERR_HIP);
     return nullptr;
   }
   p->Z = (uint16_t*)p->ws;
   p->dP = (uint16_t*)(p->ws + z);
+  p->Xt = (uint16_t*)(p->ws + z + dp);
+  p->split = SplitSpace{(float*)(p->ws + z + dp + xt), parts / 4, (uint32_t*)(p->ws + z + dp + xt + parts), 4096};
   return p;
 }
 
@@ -214,13 +299,13 @@ int mlp2_train_forward(mlp2_train_t p, int64_t M, const void* X, const void* W1,
   if (!on_device(p->device)) return record_error(MLP2_ERR_DEVICE);
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
-  if (p->act == MLP2_ACT_SWIGLU) e = forward_first<Tile128, ACT_SWIGLU>(p, M, X, W1, P, s);
-  else if (p->act == MLP2_ACT_GELU_TANH) e = forward_first<Tile128, ACT_GELU_TANH>(p, M, X, W1, P, s);
-  else e = forward_first<Tile128, ACT_IDENTITY>(p, M, X, W1, P, s);
+  if (p->act == MLP2_ACT_SWIGLU) e = forward_first<ACT_SWIGLU>(p, M, X, W1, P, s);
+  else if (p->act == MLP2_ACT_GELU_TANH) e = forward_first<ACT_GELU_TANH>(p, M, X, W1, P, s);
+  else e = forward_first<ACT_IDENTITY>(p, M, X, W1, P, s);
   if (e != hipSuccess) return status(e);
   const void* Z = p->act == MLP2_ACT_IDENTITY ? P : p->Z;
-  return status(plain<Tile128, false, true>(make_side(Z, F, M * F * 2), make_side(W2, H, F * H * 2), M, H, F,
-                                            StorePlain{(uint16_t*)Y, H, 0, INT_MAX}, s));
+  return status(product<Bf16, false, true>(make_side(Z, F, M * F * 2), make_side(W2, H, F * H * 2), M, H, F, 1,
+                                           StorePlain{(uint16_t*)Y, H, 0, INT_MAX}, p->split, p->num_cus, s));
 }
 
 int mlp2_train_backward(mlp2_train_t p, int64_t M, const void* dY, const void* X, const void* W1, const void* W2, const void* P,
@@ -237,35 +322,18 @@ int mlp2_train_backward(mlp2_train_t p, int64_t M, const void* dY, const void* X
   if (outputs_overlap(in, out)) return record_error(MLP2_ERR_INVALID_ARG);
   if (!on_device(p->device)) return record_error(MLP2_ERR_DEVICE);
   hipStream_t s = (hipStream_t)stream;
-  hipError_t e = hipSuccess;
   if (M > 0) {
-    if (p->act == MLP2_ACT_SWIGLU) e = backward_first<Tile128, ACT_SWIGLU>(p, M, dY, W2, P, s);
-    else if (p->act == MLP2_ACT_GELU_TANH) e = backward_first<Tile128, ACT_GELU_TANH>(p, M, dY, W2, P, s);
-    else e = backward_first<Tile128, ACT_IDENTITY>(p, M, dY, W2, P, s);
+    const Transpose x{(const uint16_t*)X, dW1 ? p->Xt : nullptr, H, (int)M, (int)round_up(M, 64)};
+    hipError_t e;
+    if (p->act == MLP2_ACT_SWIGLU) e = backward_first<ACT_SWIGLU>(p, M, dY, W2, P, x, s);
+    else if (p->act == MLP2_ACT_GELU_TANH) e = backward_first<ACT_GELU_TANH>(p, M, dY, W2, P, x, s);
+    else e = backward_first<ACT_IDENTITY>(p, M, dY, W2, P, x, s);
     if (e != hipSuccess) return status(e);
+  } else if (!dW1 && !dW2) {
+    return MLP2_OK;
   }
   // With no rows the weight gradients are sums over nothing: the products run no stage and store zeros.
-  if (dW2) {
-    const void* Z = p->act == MLP2_ACT_IDENTITY ? P : p->Z;
-    e = plain<Tile128, true, true>(make_side(Z, F, M * F * 2), make_side(dY, H, M * H * 2), F, H, M,
-                                   StorePlain{(uint16_t*)dW2, H, 0, INT_MAX}, s);
-    if (e != hipSuccess) return status(e);
-  }
-  if (dW1) {
-    e = plain<Tile128, true, true>(make_side(X, H, M * H * 2), make_side(p->dP, nb * F, M * nb * F * 2), H, nb * F, M,
-                                   StorePlain{(uint16_t*)dW1, F, H * F, nb == 2 ? (int)F : INT_MAX}, s);
-    if (e != hipSuccess) return status(e);
-  }
-  if (dX && M > 0) {
-    Side c = make_side(W1, F, nb * H * F * 2);
-    if (nb == 2) {
-      c.jump_at = (int)(F / 64);
-      c.jump = H * F - F;
-    }
-    e = plain<Tile128, false, false>(make_side(p->dP, nb * F, M * nb * F * 2), c, M, H, nb * F,
-                                     StorePlain{(uint16_t*)dX, H, 0, INT_MAX}, s);
-  }
-  return status(e);
+  return status(backward_second(p, M, dY, W1, dX, dW1, dW2, s));
 }
 
 void mlp2_train_destroy(mlp2_train_t p) {
