@@ -435,6 +435,8 @@ def _dtype_code(dtype) -> int:
 
 def _check_shape(t, name, shape, dtype, device, rows=False):
     """``t`` is a ``dtype`` tensor of ``shape`` on ``device``; contiguous, or with ``rows`` a matrix of contiguous rows."""
+    if t.dtype == dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return  # (the smallest calls last no longer than a dozen such checks)
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, is {t.dtype}")
     if t.device != device:
@@ -444,12 +446,12 @@ def _check_shape(t, name, shape, dtype, device, rows=False):
     if rows:
         if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
             raise ValueError(f"{name}'s rows must be contiguous and apart from each other")
-    elif not t.is_contiguous():
+    else:
         raise ValueError(f"{name} must be contiguous")
 
 
 def _row_stride(t) -> int:
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 class _Owned:
@@ -462,6 +464,9 @@ class _Owned:
 
         self.lib = load()
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._bf16, self._f32 = torch.bfloat16, torch.float32
+        # torch's own call for the current stream's handle; torch.cuda.current_stream() makes an object of it first
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         h = getattr(self.lib, f"mlp2_{self._name}_plan")(*args)
         if not h:
             raise Mlp2Error(self.lib.mlp2_last_error(), f"mlp2_{self._name}_plan")
@@ -477,6 +482,11 @@ class _Owned:
             self.close()
         except Exception:
             pass
+
+    def _on(self, stream) -> int:
+        if stream is None and self._raw_stream is not None:
+            return self._raw_stream(self.device.index)
+        return _stream(stream, self.device)
 
     def _done(self, rc, call):
         if rc != OK:
@@ -498,12 +508,10 @@ class TrainPlan(_Owned):
         self._create(self.max_rows, self.H, self.F, self.act, DTYPE_BF16)
 
     def _check(self, t, name, *shape):
-        import torch
-
         lead = 2 if self.act == ACT_SWIGLU else 1
         if name in ("W1", "P", "dW1") and (lead == 2 or t.dim() == 3):
             shape = (lead,) + shape
-        _check_shape(t, name, shape, torch.bfloat16, self.device)
+        _check_shape(t, name, shape, self._bf16, self.device)
 
     def forward(self, X, W1, W2, P, Y, stream=None) -> None:
         """Enqueue ``P = X @ W1`` and ``Y = act(P) @ W2`` on ``stream`` (default: torch's current stream)."""
@@ -511,7 +519,7 @@ class TrainPlan(_Owned):
         for t, name, shape in ((X, "X", (M, H)), (W1, "W1", (H, F)), (W2, "W2", (F, H)), (P, "P", (M, F)), (Y, "Y", (M, H))):
             self._check(t, name, *shape)
         self._done(self.lib.mlp2_train_forward(self.handle, M, _ptr(X), _ptr(W1), _ptr(W2), _ptr(P), _ptr(Y),
-                                               _stream(stream, self.device)), "forward")
+                                               self._on(stream)), "forward")
 
     def backward(self, dY, X, W1, W2, P, dX=None, dW1=None, dW2=None, stream=None) -> None:
         """Enqueue the gradients that are asked for (None: not computed)."""
@@ -521,7 +529,7 @@ class TrainPlan(_Owned):
             if t is not None or not name.startswith(("dX", "dW")):
                 self._check(t, name, *shape)
         self._done(self.lib.mlp2_train_backward(self.handle, M, _ptr(dY), _ptr(X), _ptr(W1), _ptr(W2), _ptr(P), _ptr(dX),
-                                                _ptr(dW1), _ptr(dW2), _stream(stream, self.device)), "backward")
+                                                _ptr(dW1), _ptr(dW2), self._on(stream)), "backward")
 
 
 class NormPlan(_Owned):
@@ -542,33 +550,37 @@ class NormPlan(_Owned):
         self.y_dtype = self.x_dtype if y_dtype is None else y_dtype
         self._create(self.max_rows, self.H, _dtype_code(self.x_dtype), _dtype_code(self.y_dtype))
 
-    def _vectors(self, **named):
-        import torch
-
-        for name, (t, n) in named.items():
-            if t is not None:
-                _check_shape(t, name, (n,), torch.float32, self.device)
+    def _vector(self, t, name, n):
+        if t is not None:
+            _check_shape(t, name, (n,), self._f32, self.device)
 
     def forward(self, X, weight, bias, Y, mean=None, rstd=None, eps=1e-5, stream=None) -> None:
         """Enqueue ``Y = (X - mean) * rstd * weight + bias`` (None: no weight, no bias, statistics not written)."""
-        M = int(X.shape[0])
-        _check_shape(X, "X", (M, self.H), self.x_dtype, self.device, rows=True)
-        _check_shape(Y, "Y", (M, self.H), self.y_dtype, self.device, rows=True)
-        self._vectors(weight=(weight, self.H), bias=(bias, self.H), mean=(mean, M), rstd=(rstd, M))
+        M, H = X.shape[0], self.H
+        _check_shape(X, "X", (M, H), self.x_dtype, self.device, rows=True)
+        _check_shape(Y, "Y", (M, H), self.y_dtype, self.device, rows=True)
+        self._vector(weight, "weight", H)
+        self._vector(bias, "bias", H)
+        self._vector(mean, "mean", M)
+        self._vector(rstd, "rstd", M)
         self._done(self.lib.mlp2_norm_forward(self.handle, M, _ptr(X), _row_stride(X), _ptr(weight), _ptr(bias), float(eps),
                                               _ptr(Y), _row_stride(Y), _ptr(mean), _ptr(rstd),
-                                              _stream(stream, self.device)), "forward")
+                                              self._on(stream)), "forward")
 
     def backward(self, dY, X, weight, mean, rstd, dX, dweight=None, dbias=None, stream=None) -> None:
         """Enqueue the gradients of X, and of weight and bias where asked for."""
-        M = int(X.shape[0])
-        _check_shape(dY, "dY", (M, self.H), self.y_dtype, self.device, rows=True)
-        _check_shape(X, "X", (M, self.H), self.x_dtype, self.device, rows=True)
-        _check_shape(dX, "dX", (M, self.H), self.x_dtype, self.device, rows=True)
-        self._vectors(weight=(weight, self.H), mean=(mean, M), rstd=(rstd, M), dweight=(dweight, self.H), dbias=(dbias, self.H))
+        M, H = X.shape[0], self.H
+        _check_shape(dY, "dY", (M, H), self.y_dtype, self.device, rows=True)
+        _check_shape(X, "X", (M, H), self.x_dtype, self.device, rows=True)
+        _check_shape(dX, "dX", (M, H), self.x_dtype, self.device, rows=True)
+        self._vector(weight, "weight", H)
+        self._vector(mean, "mean", M)
+        self._vector(rstd, "rstd", M)
+        self._vector(dweight, "dweight", H)
+        self._vector(dbias, "dbias", H)
         self._done(self.lib.mlp2_norm_backward(self.handle, M, _ptr(dY), _row_stride(dY), _ptr(X), _row_stride(X), _ptr(weight),
                                                _ptr(mean), _ptr(rstd), _ptr(dX), _row_stride(dX), _ptr(dweight), _ptr(dbias),
-                                               _stream(stream, self.device)), "backward")
+                                               self._on(stream)), "backward")
 
 
 #: The quintic of the Muon optimiser: five steps bring singular values of (0.003, 1] to about (0.7, 1.2).
@@ -591,15 +603,13 @@ class OrthoPlan(_Owned):
         """Enqueue ``steps`` steps on the matrices G (``[count, rows, cols]``; ``[rows, cols]`` for one) into the bf16 O.
 
         ``coeffs``: three numbers for every step, or ``steps`` triples."""
-        import torch
-
         flat = [float(v) for c in coeffs for v in (c if hasattr(c, "__len__") else (c,))]
         if len(flat) == 3:
             flat = flat * int(steps)
         if len(flat) != 3 * int(steps):
             raise ValueError(f"coeffs must hold 3 or {3 * int(steps)} numbers")
-        for t, name, dtype in ((G, "G", self.dtype), (O, "O", torch.bfloat16)):
+        for t, name, dtype in ((G, "G", self.dtype), (O, "O", self._bf16)):
             _check_shape(t, name, self.shape[1:] if self.shape[0] == 1 and t.dim() == 2 else self.shape, dtype, self.device)
         arr = (ctypes.c_float * len(flat))(*flat)
         self._done(self.lib.mlp2_ortho_run(self.handle, _ptr(G), _ptr(O), int(steps), arr, float(eps),
-                                           _stream(stream, self.device)), "run")
+                                           self._on(stream)), "run")

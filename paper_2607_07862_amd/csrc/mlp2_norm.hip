@@ -5,7 +5,7 @@
 //   dw = sum over rows of dy xhat,   db = sum over rows of dy
 //
 // Both directions are bound by memory traffic.  A row is held in registers by
-// a group of 64 to 1024 threads (up to 16 elements a thread), so each input is
+// a group of 16 to 1024 threads (up to 16 elements a thread), so each input is
 // read once; the variance is taken around the mean in a second pass over the
 // registers.  The groups of a persistent grid walk the rows with the weights
 // (forward) or the running dw and db of their columns (backward) in registers.
@@ -27,7 +27,7 @@ constexpr int kNormBlock = 1024;  // backward: threads of a work-group
 template <int NT, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float (*buf)[N]) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1)
+  for (int d = (NT < 64 ? NT : 64) / 2; d > 0; d >>= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d);
   if constexpr (NT > 64) {
@@ -125,44 +125,90 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_norm_forward(const Norm
   }
 }
 
+// Every group requests its next row before it works on the present one, so a
+// row's latency passes during the sums and stores of the row ahead of it (with
+// 16 elements a thread the registers do not reach for that).
 template <class XT, class YT, int NT, int C>
 __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) {
   constexpr int GROUPS = kNormBlock / NT;
   __shared__ float buf[2][kNormBlock / 64][2];
   const int t = threadIdx.x % NT, group = threadIdx.x / NT;
   const float inv = 1.0f / (float)a.H;
+  // dw and db of this thread's columns: in registers, with 16 elements a thread in LDS (its own words, no other thread's)
+  constexpr bool IN_LDS = C > 1;
+  static_assert(!IN_LDS || GROUPS == 1, "one row at a time");
   float dw[C][8], db[C][8];
+  __shared__ f32x4 kept[IN_LDS ? 4 * C : 1][IN_LDS ? kNormBlock : 1];
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[c][i] = db[c][i] = 0.f;
+  if constexpr (IN_LDS)
+#pragma unroll
+    for (int i = 0; i < 4 * C; ++i) kept[i][threadIdx.x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Row {
+    Piece<XT> x[C];
+    Piece<YT> d[C];
+    float mean, rstd;
+  };
+  auto request = [&](Row& r, int row) {
+    const int64_t at = row < a.M ? row : a.M - 1;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = 8 * (t + NT * c), n = a.H - col;
+      if (n > 0) {
+        r.x[c].load((const XT*)a.X + at * a.ldx + col, n);
+        r.d[c].load((const YT*)a.dY + at * a.ldd + col, n);
+      }
+    }
+    r.mean = a.mean[at];
+    r.rstd = a.rstd[at];
+  };
+  constexpr bool AHEAD = C == 1;
+  const int step = gridDim.x * GROUPS;
+  Row now, next;
+  if constexpr (AHEAD) request(now, blockIdx.x * GROUPS + group);
   int turn = 0;
-  for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += gridDim.x * GROUPS, turn ^= 1) {
+  for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += step, turn ^= 1) {
     const int row = row0 + group;
     const bool live = row < a.M;
-    const int64_t at = live ? row : row0;
-    const XT* x = (const XT*)a.X + at * a.ldx;
-    const YT* dy = (const YT*)a.dY + at * a.ldd;
-    const float mean = a.mean[at], rstd = a.rstd[at];
+    if constexpr (!AHEAD) request(now, row);
+    else if (row0 + step < a.M) request(next, row + step);
+    const float mean = now.mean, rstd = now.rstd;
     float xh[C][8], g[C][8], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = 8 * (t + NT * c), n = live ? a.H - col : 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) xh[c][i] = g[c][i] = 0.f;
-      if (n > 0) {
-        load8(x + col, n, xh[c]);
-        load8(dy + col, n, g[c]);
-      }
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = 1.f;
       if (a.w && n > 0) load8(a.w + col, n, w);
+      now.x[c].values(xh[c]);
+      now.d[c].values(g[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         xh[c][i] = i < n ? (xh[c][i] - mean) * rstd : 0.f;
-        dw[c][i] += g[c][i] * xh[c][i];
-        db[c][i] += g[c][i];
+        g[c][i] = i < n ? g[c][i] : 0.f;
+        if constexpr (!IN_LDS) {
+          dw[c][i] += g[c][i] * xh[c][i];
+          db[c][i] += g[c][i];
+        }
+      }
+      if constexpr (IN_LDS) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f32x4 p = kept[4 * c + h][threadIdx.x], q = kept[4 * c + 2 + h][threadIdx.x];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i] += g[c][4 * h + i] * xh[c][4 * h + i];
+            q[i] += g[c][4 * h + i];
+          }
+          kept[4 * c + h][threadIdx.x] = p;
+          kept[4 * c + 2 + h][threadIdx.x] = q;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
         g[c][i] *= w[i];
         s[0] += g[c][i];
         s[1] += g[c][i] * xh[c][i];
@@ -179,10 +225,19 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
       for (int i = 0; i < 8; ++i) o[i] = rstd * (g[c][i] - m0 - xh[c][i] * m1);
       if (live && n > 0) store8(dx + col, n, o);
     }
+    if constexpr (AHEAD) now = next;
   }
   if (!a.part) return;
+  if constexpr (IN_LDS)
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        dw[c][i] = kept[4 * c + i / 4][threadIdx.x][i % 4];
+        db[c][i] = kept[4 * c + 2 + i / 4][threadIdx.x][i % 4];
+      }
   // The groups' sums of the same columns meet in LDS, one piece after the other.
-  __shared__ float sums[GROUPS > 1 ? GROUPS : 1][NT * 8 + 8];
+  __shared__ float sums[GROUPS][GROUPS > 1 ? NT * 8 : 1];
   float* to = a.part + (int64_t)blockIdx.x * 2 * a.H;
 #pragma unroll
   for (int which = 0; which < 2; ++which)
@@ -209,19 +264,22 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
     }
 }
 
-// dw and db from the work-groups' partials: 64 columns of [parts][2 H] a work-group, 16 threads a column.
+// dw and db from the work-groups' partials: 32 columns of [parts][2 H] a work-group, 32 threads a column.
 __global__ __launch_bounds__(1024) void k_norm_reduce(const float* part, int parts, int H, float* dw, float* db) {
-  __shared__ float sums[16][65];
-  const int lane = threadIdx.x & 63, y = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  __shared__ float sums[32][33];
+  const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int64_t width = 2 * (int64_t)H, col = (int64_t)blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (col < 2 * (int64_t)H)
-    for (int p = y; p < parts; p += 16) s += part[(int64_t)p * 2 * H + col];
+  if (col < width) {
+#pragma unroll 8
+    for (int p = y; p < parts; p += 32) s += part[p * width + col];
+  }
   sums[y][lane] = s;
   __syncthreads();
-  if (y == 0 && col < 2 * (int64_t)H) {
+  if (y == 0 && col < width) {
     s = 0.f;
-    for (int i = 0; i < 16; ++i) s += sums[i][lane];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += sums[i][lane];
     float* to = col < H ? dw : db;
     if (to) to[col < H ? col : col - H] = s;
   }
@@ -240,32 +298,42 @@ struct mlp2_norm_s {
 
 namespace {
 
-// Threads of a row: the fewest of 64, 128, ... 1024 whose 16 elements each cover it.
-int row_threads(int64_t H) {
-  int nt = 64;
-  while (nt * 16 < H) nt *= 2;
+// Threads of a row: the fewest of 16, 32, ... 1024 whose `each` elements cover
+// it.  Forward 16 elements a thread; backward, where a thread also keeps its
+// columns' dw and db and the next row, 8 as far as 1024 threads reach.
+int row_threads(int64_t H, int each) {
+  int nt = 16;
+  while (nt < 1024 && nt * each < H) nt *= 2;
   return nt;
 }
+int backward_threads(int64_t H) { return row_threads(H, 8); }
 
-template <class XT, class YT, int NT, int C>
+// (C = 1 forward: only where a second piece would lie past every row)
+template <class XT, class YT, int NT>
 void launch_norm(bool forward, const NormArgs& a, int grid, hipStream_t s) {
-  if (forward) k_norm_forward<XT, YT, NT, C><<<grid, NT < 256 ? 256 : NT, 0, s>>>(a);
-  else k_norm_backward<XT, YT, NT, C><<<grid, kNormBlock, 0, s>>>(a);
+  if (forward) {
+    if (NT == 16 && a.H <= 128) k_norm_forward<XT, YT, NT, 1><<<grid, NT < 256 ? 256 : NT, 0, s>>>(a);
+    else k_norm_forward<XT, YT, NT, 2><<<grid, NT < 256 ? 256 : NT, 0, s>>>(a);
+  } else {
+    if (NT == 1024 && a.H > 8192) k_norm_backward<XT, YT, 1024, 2><<<grid, kNormBlock, 0, s>>>(a);
+    else k_norm_backward<XT, YT, NT, 1><<<grid, kNormBlock, 0, s>>>(a);
+  }
 }
 
 template <class XT, class YT>
 hipError_t launch_norm(bool forward, const NormArgs& a, int nt, int grid, hipStream_t s) {
-  if (a.H <= 512) launch_norm<XT, YT, 64, 1>(forward, a, grid, s);
-  else if (nt == 64) launch_norm<XT, YT, 64, 2>(forward, a, grid, s);
-  else if (nt == 128) launch_norm<XT, YT, 128, 2>(forward, a, grid, s);
-  else if (nt == 256) launch_norm<XT, YT, 256, 2>(forward, a, grid, s);
-  else if (nt == 512) launch_norm<XT, YT, 512, 2>(forward, a, grid, s);
-  else launch_norm<XT, YT, 1024, 2>(forward, a, grid, s);
+  if (nt == 16) launch_norm<XT, YT, 16>(forward, a, grid, s);
+  else if (nt == 32) launch_norm<XT, YT, 32>(forward, a, grid, s);
+  else if (nt == 64) launch_norm<XT, YT, 64>(forward, a, grid, s);
+  else if (nt == 128) launch_norm<XT, YT, 128>(forward, a, grid, s);
+  else if (nt == 256) launch_norm<XT, YT, 256>(forward, a, grid, s);
+  else if (nt == 512) launch_norm<XT, YT, 512>(forward, a, grid, s);
+  else launch_norm<XT, YT, 1024>(forward, a, grid, s);
   return hipGetLastError();
 }
 
 hipError_t launch_norm(const mlp2_norm_s* p, bool forward, const NormArgs& a, int grid, hipStream_t s) {
-  const int nt = row_threads(p->H);
+  const int nt = forward ? row_threads(p->H, 16) : backward_threads(p->H);
   if (p->x == MLP2_DTYPE_BF16) return launch_norm<uint16_t, uint16_t>(forward, a, nt, grid, s);
   if (p->y == MLP2_DTYPE_BF16) return launch_norm<float, uint16_t>(forward, a, nt, grid, s);
   return launch_norm<float, float>(forward, a, nt, grid, s);
@@ -343,7 +411,7 @@ int mlp2_norm_forward(mlp2_norm_t p, int64_t M, const void* X, int64_t ldx, cons
   a.M = (int)M;
   a.H = (int)p->H;
   a.eps = eps;
-  const int nt = row_threads(p->H), groups = nt < 256 ? 256 / nt : 1, block = nt < 256 ? 256 : nt;
+  const int nt = row_threads(p->H, 16), groups = nt < 256 ? 256 / nt : 1, block = nt < 256 ? 256 : nt;
   const int64_t blocks = (M + groups - 1) / groups, most = (int64_t)p->num_cus * (2048 / block);
   const hipError_t e = launch_norm(p, true, a, (int)(blocks < most ? blocks : most), (hipStream_t)stream);
   return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP);
@@ -377,14 +445,14 @@ int mlp2_norm_backward(mlp2_norm_t p, int64_t M, const void* dY, int64_t lddy, c
     a.ldy = lddx;
     a.M = (int)M;
     a.H = (int)p->H;
-    const int groups = kNormBlock / row_threads(p->H);
+    const int groups = kNormBlock / backward_threads(p->H);
     const int64_t blocks = (M + groups - 1) / groups;
     parts = (int)(blocks < p->max_parts ? blocks : p->max_parts);
     const hipError_t e = launch_norm(p, false, a, parts, s);
     if (e != hipSuccess) return record_error(MLP2_ERR_HIP);
   }
   if (grads) {
-    k_norm_reduce<<<(unsigned)((2 * p->H + 63) / 64), 1024, 0, s>>>(p->part, parts, (int)p->H, dweight, dbias);
+    k_norm_reduce<<<(unsigned)((2 * p->H + 31) / 32), 1024, 0, s>>>(p->part, parts, (int)p->H, dweight, dbias);
     if (hipGetLastError() != hipSuccess) return record_error(MLP2_ERR_HIP);
   }
   return MLP2_OK;

@@ -129,6 +129,7 @@ __global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int c
 
 // A = X X^T in the scale of A.
 struct StoreGram {
+  using Read = Nothing;
   static constexpr bool kGated = false, kSymmetric = true, kMirror = true;
   uint16_t* A;
   int n, rows;  // rows: n
@@ -136,7 +137,8 @@ struct StoreGram {
   __device__ __forceinline__ void mirror(int batch, int row, int col, u32x4 q) const {
     *reinterpret_cast<u32x4*>(A + ((int64_t)batch * n + row) * n + col) = q;
   }
-  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ Nothing read(int, int, int) const { return {}; }
+  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8], Nothing) const {
     float o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = v[i] * by;
@@ -148,6 +150,7 @@ struct StoreGram {
 
 // B = b A + c A A, its diagonal apart in the last steps.
 struct StorePoly {
+  using Read = u32x4;  // A's values
   static constexpr bool kGated = false, kSymmetric = true, kMirror = true;
   const uint16_t* A;
   uint16_t* B;
@@ -158,10 +161,13 @@ struct StorePoly {
   __device__ __forceinline__ void mirror(int batch, int row, int col, u32x4 q) const {
     *reinterpret_cast<u32x4*>(B + ((int64_t)batch * n + row) * n + col) = q;
   }
-  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ u32x4 read(int batch, int row, int col) const {
+    return *reinterpret_cast<const u32x4*>(A + ((int64_t)batch * n + row) * n + col);
+  }
+  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8], u32x4 r) const {
     const int64_t at = ((int64_t)batch * n + row) * n + col;
     float o[8];
-    unpack_f16x8(*reinterpret_cast<const u32x4*>(A + at), o);
+    unpack_f16x8(r, o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       o[i] = b * o[i] + c * v[i];
@@ -182,23 +188,32 @@ struct Update {
   const float* diag;
   int64_t n, m;
   float a, by;
-  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8], float (&o)[8]) const {
+  struct Read {
+    u32x4 hi, lo;
+    float diag;
+  };
+  __device__ __forceinline__ Read read(int batch, int row, int col) const {
     const int64_t at = ((int64_t)batch * n + row) * m + col;
+    return {*reinterpret_cast<const u32x4*>(hi + at), *reinterpret_cast<const u32x4*>(lo + at), diag[batch * n + row]};
+  }
+  __device__ __forceinline__ void operator()(const float (&v)[8], const Read& r, float (&o)[8]) const {
     float h[8], l[8];
-    unpack_f16x8(*reinterpret_cast<const u32x4*>(hi + at), h);
-    unpack_f16x8(*reinterpret_cast<const u32x4*>(lo + at), l);
-    const float d = a + diag[batch * n + row];
+    unpack_f16x8(r.hi, h);
+    unpack_f16x8(r.lo, l);
+    const float d = a + r.diag;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = d * h[i] + (d * l[i] + by * v[i]);
   }
 };
 struct StoreUpdate {
   static constexpr bool kGated = false, kSymmetric = false, kMirror = false;
+  using Read = Update::Read;
   Update x;
   uint16_t *hi, *lo;
-  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ Read read(int batch, int row, int col) const { return x.read(batch, row, col); }
+  __device__ __forceinline__ void operator()(int batch, int row, int col, const float (&v)[8], const Read& r) const {
     float o[8];
-    x(batch, row, col, v, o);
+    x(v, r, o);
     const int64_t at = ((int64_t)batch * x.n + row) * x.m + col;
     store_split(hi + at, lo + at, o);
   }
@@ -208,6 +223,7 @@ struct StoreUpdate {
 template <bool TALL>
 struct StoreLast {
   static constexpr bool kGated = false, kSymmetric = false, kMirror = TALL;
+  using Read = Update::Read;
   Update x;
   uint16_t* O;  // [matrices][g_rows][g_cols]
   int g_rows, g_cols;
@@ -216,9 +232,10 @@ struct StoreLast {
   __device__ __forceinline__ void mirror(int batch, int col, int row, u32x4 q) const {
     if (col < g_rows && row < g_cols) store8_packed(O + ((int64_t)batch * g_rows + col) * g_cols + row, g_cols - row, q);
   }
-  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ Read read(int batch, int row, int col) const { return x.read(batch, row, col); }
+  __device__ __forceinline__ u32x4 operator()(int batch, int row, int col, const float (&v)[8], const Read& r) const {
     float o[8];
-    x(batch, row, col, v, o);
+    x(v, r, o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] *= out_by;
     const u32x4 q = pack_bf16x8(o);
@@ -323,7 +340,8 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   p->scale = std::exp2(std::round(0.5f * std::log2((float)(rows > cols ? rows : cols))));
   const int64_t x = round_up(count * p->n * p->m * 2, 256), a = round_up(count * p->n * p->n * 2, 256);
   const int64_t part = round_up(count * kOrthoParts * 4, 256), diag = round_up(count * p->n * 4, 256);
-  const int64_t parts = (int64_t)1 << 27, counters = 4096 * kLine * 4, fixed = 4 * x + 2 * a + part + diag;
+  const int64_t floats = split_floats(p->n, p->m, count), parts = floats * 4, counters = kSplitCounters * kLine * 4;
+  const int64_t fixed = 4 * x + 2 * a + part + diag;
   if (hipMalloc((void**)&p->ws, (size_t)(fixed + parts + counters)) != hipSuccess ||
       hipMemset(p->ws + fixed + parts, 0, (size_t)counters) != hipSuccess) {
     (void)hipGetLastError();
@@ -338,7 +356,7 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   p->B = (uint16_t*)(at + a);
   p->part = (float*)(at + 2 * a);
   p->diag = (float*)(at + 2 * a + part);
-  p->split = SplitSpace{(float*)(p->ws + fixed), parts / 4, (uint32_t*)(p->ws + fixed + parts), 4096};
+  p->split = SplitSpace{(float*)(p->ws + fixed), floats, (uint32_t*)(p->ws + fixed + parts), kSplitCounters};
   return p;
 }
 

@@ -24,6 +24,7 @@
 #pragma once
 
 #include "mlp2_device.hpp"
+#include "mlp2_host.h"
 
 namespace mlp2 {
 
@@ -524,6 +525,8 @@ struct TileWalk {
   }
 };
 
+struct Nothing {};  // an epilogue's Read where it reads nothing
+
 // RO, CO: outer sides; JUMP: the column side runs on in a second matrix.
 template <bool RO_, bool CO_, class Epi_, bool JUMP_ = false>
 struct Problem {
@@ -554,16 +557,27 @@ __device__ __forceinline__ void lane_values(const Acc<T>& acc, int p, int tm, fl
 // of a wave), written through to the device's point of coherence, and counts
 // its arrival; the part that arrives last adds all parts in the order 0, 1, ...
 // and goes on to the epilogue, so the bits do not depend on which one it is,
-// and no part waits.  Returns whether this work-group goes on.
+// and no part waits.  Row blocks from `rows` on hold nothing.  Returns whether
+// this work-group goes on.
 template <class T>
-__device__ __forceinline__ bool join_parts(Acc<T>& acc, float* part, uint32_t* arrived, int64_t tile, int split, int s, char* lds) {
+__device__ __forceinline__ bool join_parts(Acc<T>& acc, float* part, uint32_t* arrived, int64_t tile, int split, int s, int rows,
+                                           char* lds) {
   constexpr int BLOCKS = T::COLP * 2 * T::TM, ITEM = T::NWAVES * BLOCKS * 256;  // floats of a part
+  constexpr int kSc1 = 16;  // device scope: stores written through, loads past this XCD's L2 (it may hold lines of an earlier launch)
   const int tid = thread_here(), lane = tid & 63, wave = uniform(tid >> 6);
-  const uint32_t off = (uint32_t)(wave * BLOCKS * 1024 + lane * 16);
-  float* mine = part + (tile * split + s) * ITEM;
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(part + tile * split * ITEM, 0, split * ITEM * 4, 0x00027000);
+  // Row blocks that hold nothing get an offset past the range: their stores are dropped, their loads return zeros.
+  uint32_t off[T::TM];
 #pragma unroll
-  for (int i = 0; i < BLOCKS; ++i)
-    store_through16(mine, off, __builtin_bit_cast(u32x4, acc[i / (2 * T::TM)][i / T::TM % 2][i % T::TM]), i * 1024);
+  for (int tm = 0; tm < T::TM; ++tm)
+    off[tm] = T::row_of(wave % T::WM, tm) < rows ? (uint32_t)(wave * BLOCKS * 1024 + lane * 16) : 0x80000000u;
+  const int mine = s * ITEM * 4;
+#pragma unroll
+  for (int c = 0; c < T::COLP * 2; ++c)
+#pragma unroll
+    for (int tm = 0; tm < T::TM; ++tm)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[c / 2][c % 2][tm]), rsrc, (int)(off[tm] + mine + (c * T::TM + tm) * 1024),
+                                             0, kSc1);
   wait_all_mem();
   __syncthreads();
   uint32_t* last = reinterpret_cast<uint32_t*>(lds);
@@ -575,21 +589,19 @@ __device__ __forceinline__ bool join_parts(Acc<T>& acc, float* part, uint32_t* a
   }
   __syncthreads();
   if (uniform(*last) != (uint32_t)split - 1) return false;
-  // Device-scope loads: this XCD's L2 may hold lines of an earlier launch.
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(part + tile * split * ITEM, 0, -1, 0x00027000);
 #pragma unroll
-  for (int i = 0; i < BLOCKS; ++i) acc[i / (2 * T::TM)][i / T::TM % 2][i % T::TM] = f32x4{0.f, 0.f, 0.f, 0.f};
-  constexpr int R = BLOCKS < 8 ? BLOCKS : 8;  // loads in flight
-  static_assert(BLOCKS % R == 0, "whole rounds");
+  for (int c = 0; c < T::COLP * 2; ++c)
+#pragma unroll
+    for (int tm = 0; tm < T::TM; ++tm) acc[c / 2][c % 2][tm] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int q = 0; q < split; ++q) {
-    const uint32_t from = off + (uint32_t)q * (uint32_t)(ITEM * 4);
 #pragma unroll
-    for (int i0 = 0; i0 < BLOCKS; i0 += R) {
-      u32x4 v[R];
+    for (int c = 0; c < T::COLP * 2; ++c) {
+      u32x4 v[T::TM];  // in flight together
 #pragma unroll
-      for (int i = 0; i < R; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)from, (i0 + i) * 1024, 16);
+      for (int tm = 0; tm < T::TM; ++tm)
+        v[tm] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(off[tm] + q * (ITEM * 4) + (c * T::TM + tm) * 1024), 0, kSc1);
 #pragma unroll
-      for (int i = 0; i < R; ++i) acc[(i0 + i) / (2 * T::TM)][(i0 + i) / T::TM % 2][(i0 + i) % T::TM] += __builtin_bit_cast(f32x4, v[i]);
+      for (int tm = 0; tm < T::TM; ++tm) acc[c / 2][c % 2][tm] += __builtin_bit_cast(f32x4, v[tm]);
     }
   }
   return true;
@@ -603,6 +615,8 @@ constexpr int lds_of() {
   return mirror > T::LDS ? mirror : T::LDS;
 }
 
+// Epi::read: what the epilogue has to read for 8 values of a row; Epi::Read
+// goes back to it with the sums.
 // Epi::kGated: the two column panels are the same columns of two matrices and
 // the epilogue takes both values; otherwise they are consecutive columns.
 // Epi::kMirror: the epilogue returns 16-bit values whose transpose goes out too,
@@ -625,36 +639,50 @@ __device__ __forceinline__ void run_product(const P& a, int item, int batch, cha
   Acc<T> acc;
   if constexpr (T::NWAVES == 8) product_pingpong<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
   else product_loop<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
-  if (a.split > 1 && !join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, lds)) return;
+  if (a.split > 1 && !join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, a.M - m0, lds)) return;
   const int tid = thread_here(), lane = tid & 63, wave = uniform(tid >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
   const bool mirrored = !Epi::kSymmetric || tm_ != tn_;
   if constexpr (Epi::kMirror) __syncthreads();  // join_parts' flag is read before the LDS is written again
+  // Units: block pair p of row block tm.  What an epilogue reads for a group
+  // of units is requested before the group ahead of it is stored: a load
+  // behind a store of unknown address would otherwise wait for it, one round
+  // trip a unit.
+  constexpr int PAIRS = Epi::kGated ? 1 : T::COLP, UNITS = PAIRS * T::TM, GROUP = UNITS < 4 ? UNITS : 4;
+  auto row_at = [&](int u) { return T::row_of(wm, u / PAIRS) + (lane & 15); };
+  auto block_at = [&](int u) { return u % PAIRS * T::EC + 32 * wn; };
+  auto inside = [&](int u) { return n0 + block_at(u) < a.N && m0 + row_at(u) < a.M; };
+  typename Epi::Read read[2][GROUP];
+  auto request = [&](int g) {
 #pragma unroll
-  for (int tm = 0; tm < T::TM; ++tm) {
-    const int in_row = T::row_of(wm, tm) + (lane & 15), row = m0 + in_row;
-    if constexpr (Epi::kGated) {
-      const int block = n0 + 32 * wn;
-      float g[8], u[8];
-      lane_values<T>(acc, 0, tm, g);
-      lane_values<T>(acc, 1, tm, u);
-      if (block < a.N && row < a.M) a.epi(batch, row, block + 8 * (lane >> 4), g, u);
-    } else {
+    for (int i = 0; i < GROUP; ++i) {
+      const int u = g * GROUP + i;
+      if (inside(u)) read[g & 1][i] = a.epi.read(batch, m0 + row_at(u), n0 + block_at(u) + 8 * (lane >> 4));
+    }
+  };
+  request(0);
 #pragma unroll
-      for (int p = 0; p < T::COLP; ++p) {
-        const int in_block = p * T::EC + 32 * wn, block = n0 + in_block;
-        float v[8];
-        lane_values<T>(acc, p, tm, v);
-        if constexpr (Epi::kMirror) {
-          u32x4 q = {0, 0, 0, 0};
-          if (block < a.N && row < a.M) q = a.epi(batch, row, block + 8 * (lane >> 4), v);
-          uint16_t* to = reinterpret_cast<uint16_t*>(lds + (in_block + 8 * (lane >> 4)) * mirror_pitch<T>()) + in_row;
-          if (mirrored)
+  for (int g = 0; g < UNITS / GROUP; ++g) {
+    if (g + 1 < UNITS / GROUP) request(g + 1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) to[i * (mirror_pitch<T>() / 2)] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
-        } else {
-          if (block < a.N && row < a.M) a.epi(batch, row, block + 8 * (lane >> 4), v);
-        }
+    for (int i = 0; i < GROUP; ++i) {
+      const int u = g * GROUP + i, p = u % PAIRS, tm = u / PAIRS;
+      const int row = m0 + row_at(u), col = n0 + block_at(u) + 8 * (lane >> 4);
+      float v[8];
+      lane_values<T>(acc, p, tm, v);
+      if constexpr (Epi::kGated) {
+        float w[8];
+        lane_values<T>(acc, 1, tm, w);
+        if (inside(u)) a.epi(batch, row, col, v, w);
+      } else if constexpr (Epi::kMirror) {
+        u32x4 q = {0, 0, 0, 0};
+        if (inside(u)) q = a.epi(batch, row, col, v, read[g & 1][i]);
+        uint16_t* to = reinterpret_cast<uint16_t*>(lds + (block_at(u) + 8 * (lane >> 4)) * mirror_pitch<T>()) + row_at(u);
+        if (mirrored)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) to[e * (mirror_pitch<T>() / 2)] = (uint16_t)(q[e / 2] >> (16 * (e & 1)));
+      } else {
+        if (inside(u)) a.epi(batch, row, col, v, read[g & 1][i]);
       }
     }
   }
@@ -705,6 +733,17 @@ struct SplitSpace {
   int64_t counters;
 };
 
+constexpr int kMaxSplit = 32;
+constexpr int64_t kSplitCounters = 4096;
+
+// Floats of the parts of any product with up to M x N results: all that the
+// splits can ask for, but 96 MB at most (a part and slot of the largest tile is
+// 64 MB; a launch of several products holds the parts of each).
+inline int64_t split_floats(int64_t M, int64_t N, int64_t batches) {
+  const int64_t most = (int64_t)24 << 20, all = kMaxSplit * batches * round_up(M, 256) * round_up(N, 256);
+  return all < most ? all : most;
+}
+
 enum { TILE_64, TILE_128, TILE_256, TILES };
 
 // The sizes that tile and split are chosen by.
@@ -716,18 +755,19 @@ struct Shape {
 
 // What a tile costs a work-group, in microseconds: `unit` for 64 of K with every
 // slot of the chip taken, `alone` with at most one work-group to a CU, `item`
-// once (prologue and epilogue), `join` for meeting the other parts of K and
-// `part` for each of them.  Measured with the products of 2048 x 4096 x 14336
+// once (prologue and epilogue), `join` for meeting the other parts of K beside
+// the traffic of their sums.  Measured with the products of 2048 x 4096 x 14336
 // (every slot taken), 24 x 4096 x 14336 and 64 x 512 x 2048.
 struct TileCost {
   int rows, cols, slots;  // slots: work-groups to a CU
-  double unit, alone, item, join, part;
+  double unit, alone, item, join;
 };
 inline TileCost tile_cost(int tile, bool gated) {
-  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 8.0, 12.0, 4.0};
-  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 6.0, 1.0};
-  return {64, 64, 2, gated ? 0.80 : 0.48, gated ? 0.50 : 0.30, 2.5, 4.0, 0.5};
+  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 12.0, 4.0};
+  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 4.0};
+  return {64, 64, 2, gated ? 0.80 : 0.48, gated ? 0.50 : 0.30, 2.5, 4.0};
 }
+constexpr double kBytesPerUs = 4.5e6;  // what products stream, about nine tenths of a large copy's rate
 
 struct Choice {
   int tile, split;
@@ -747,22 +787,33 @@ inline int64_t split_room(const Shape& s, const TileCost& t, const SplitSpace& w
   return room < 1 ? 1 : room;
 }
 
-// Time of `tiles` * split items: whole rounds of the chip's slots, then the rest.
+// Microseconds for the parts' sums, written and read.
+inline double join_time(const Shape& s, const TileCost& t, int64_t split) {
+  const int64_t rows = s.M < t.rows ? round_up(s.M, 16) : t.rows;
+  return split > 1 ? t.join + 8.0 * tiles_of(s, t) * split * rows * t.cols * (s.gated ? 2 : 1) / kBytesPerUs : 0.0;
+}
+
+// Time of the tiles' items: whole rounds of the chip's slots, then the rest, but no less than the operands' traffic.
 inline double product_time(const Shape& s, const TileCost& t, int64_t split, int num_cus) {
   const int64_t items = tiles_of(s, t) * split, slots = (int64_t)num_cus * t.slots, per = (units_of(s) + split - 1) / split;
   const int64_t rest = items % slots;
   double time = (double)(items / slots) * (per * t.unit + t.item);
   if (rest) time += per * (rest <= num_cus ? t.alone : t.unit) + t.item;
-  return split > 1 ? time + t.join + t.part * split : time;
+  const double bytes = 2.0 * s.batches * ((double)s.M * s.K + (s.symmetric ? 0.0 : (double)s.N * s.K * (s.gated ? 2 : 1)));
+  if (time < bytes / kBytesPerUs + t.item) time = bytes / kBytesPerUs + t.item;
+  return time + join_time(s, t, split);
 }
 
-// The tile and split of one product: the least of the estimates.
+// The tile and split of one product: the least of the estimates.  (Splitting
+// only the tiles of a last round that leaves half of the CUs idle was tried:
+// 441 -> 463 us for the forward pass's first product of 2048 x 4096 x 14336,
+// 454 -> 437 us for an orthogonalisation's update; busy halves clock higher.)
 inline Choice choose(const Shape& s, const SplitSpace& ws, int num_cus) {
   Choice best{TILE_64, 1};
   double least = 1e30;
   for (int tile = 0; tile < TILES; ++tile) {
     const TileCost t = tile_cost(tile, s.gated);
-    const int64_t units = units_of(s), room = split_room(s, t, ws), most = units < 32 ? units : 32;
+    const int64_t units = units_of(s), room = split_room(s, t, ws), most = units < kMaxSplit ? units : kMaxSplit;
     for (int64_t split = 1; split <= most && split <= room; ++split) {
       const double time = product_time(s, t, split, num_cus);
       if (time < least) {
@@ -795,19 +846,21 @@ int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&
       const int64_t tiles = tiles_of(s[i], t), units = units_of(s[i]);
       parts[i] = 1;
       if (!tiles) continue;
-      const double unit = items <= num_cus ? t.alone : t.unit;
-      // An item may take its share, or what it takes for the overheads not to outweigh the work.
-      const double limit = share > 3 * t.item ? share : 3 * t.item;
+      // (a long item shares its CU with short ones that mostly move data)
+      const double unit = items <= num_cus ? t.alone : 0.5 * (t.alone + t.unit);
+      // An item may take two fifths of its slot's share, or what it takes for the overheads not to outweigh the work.
+      const double limit = 0.4 * share > 3 * t.item ? 0.4 * share : 3 * t.item;
       int64_t want = (int64_t)(units * unit / limit + 0.999);
-      const int64_t room = split_room(s[i], t, ws) / N;
+      const int64_t room = split_room(s[i], t, ws);
       if (want > room) want = room;
       if (want > units) want = units;
+      if (want > kMaxSplit) want = kMaxSplit;
       if (want > 1) parts[i] = (int)want;
-      const double one = (double)((units + parts[i] - 1) / parts[i]) * unit + t.item + (parts[i] > 1 ? t.join + t.part * parts[i] : 0.0);
+      const double one = (double)((units + parts[i] - 1) / parts[i]) * unit + t.item + (parts[i] > 1 ? t.join : 0.0);
       if (one > longest) longest = one;
-      if (parts[i] > 1) extra += (double)tiles * (parts[i] - 1) * t.item;
+      if (parts[i] > 1) extra += (double)tiles * (parts[i] - 1) * t.item / slots + 0.5 * join_time(s[i], t, parts[i]);
     }
-    const double even = share + extra / slots, time = even > longest ? even + 0.3 * longest : longest + 0.3 * even;
+    const double even = share + extra, time = even > longest ? even + 0.3 * longest : longest + 0.3 * even;
     if (time < least) {
       least = time;
       best = tile;
@@ -818,7 +871,7 @@ int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&
 }
 
 template <class T, class P>
-P make_problem(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const typename P::Epi& epi, int split,
+P make_problem(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const typename P::Epi& epi, int parts,
                const SplitSpace& ws) {
   constexpr int COLS = P::Epi::kGated ? T::EC : T::BN;
   P a{};
@@ -836,12 +889,20 @@ P make_problem(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, in
   // No part is empty, and every part of every tile has its place in the workspace.
   const int64_t tiles = (int64_t)a.walk.total() * batches;
   const int64_t room = tiles >= 1 && tiles <= ws.counters ? ws.part_floats / (tiles * T::BM * T::BN) : 1;
-  if (split > room) split = (int)room;
+  int64_t split = parts < room ? parts : room;
   if (split > a.nk) split = a.nk;
-  a.per = split > 1 ? (a.nk + split - 1) / split : a.nk;
+  a.per = split > 1 ? (int)((a.nk + split - 1) / split) : a.nk;
   a.split = split > 1 ? (a.nk + a.per - 1) / a.per : 1;
   a.epi = epi;
   return a;
+}
+
+// What is left of the workspace behind a product's parts.
+template <class T, class P>
+SplitSpace behind(const SplitSpace& ws, const P& a) {
+  if (a.split == 1) return ws;
+  const int64_t tiles = a.walk.total(), floats = tiles * a.split * T::BM * T::BN;
+  return {ws.part + floats, ws.part_floats - floats, ws.arrived + tiles * kLine, ws.counters - tiles};
 }
 
 template <class T, class Elem, class P>

@@ -42,11 +42,13 @@ __device__ __forceinline__ void gelu_and_slope(float z, float& value, float& slo
 // P (and Z) of a tile of X W1.  Z is computed from the fp32 sums, before P is rounded.
 template <int ACT>
 struct StoreForward {
+  using Read = Nothing;
   static constexpr bool kGated = ACT == ACT_SWIGLU, kSymmetric = false, kMirror = false;
   uint16_t* P;  // [M, F], gated [2, M, F]
   uint16_t* Z;  // [M, F] (identity: unused, P is Z)
   int64_t plane;  // elements of one P
   int64_t F;
+  __device__ __forceinline__ Nothing read(int, int, int) const { return {}; }
   __device__ __forceinline__ void operator()(int, int row, int col, const float (&g)[8], const float (&u)[8]) const {
     float z[8];
 #pragma unroll
@@ -56,7 +58,7 @@ struct StoreForward {
     *reinterpret_cast<u32x4*>(P + plane + at) = pack_bf16x8(u);
     *reinterpret_cast<u32x4*>(Z + at) = pack_bf16x8(z);
   }
-  __device__ __forceinline__ void operator()(int, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ void operator()(int, int row, int col, const float (&v)[8], Nothing) const {
     const int64_t at = (int64_t)row * F + col;
     *reinterpret_cast<u32x4*>(P + at) = pack_bf16x8(v);
     if constexpr (ACT == ACT_GELU_TANH) {
@@ -80,15 +82,24 @@ struct StoreBackward {
   __device__ __forceinline__ void mirror(int, int col, int row, u32x4 q) const {
     *reinterpret_cast<u32x4*>(Zt + (int64_t)col * rows + row) = q;
   }
-  __device__ __forceinline__ u32x4 operator()(int, int row, int col, const float (&d)[8]) const {
+  struct Read {
+    u32x4 p[ACT == ACT_SWIGLU ? 2 : 1];
+  };
+  __device__ __forceinline__ Read read(int, int row, int col) const {
     const int64_t at = (int64_t)row * F + col;
-    const u32x4 first = *reinterpret_cast<const u32x4*>(P + at);
+    Read r;
+    r.p[0] = *reinterpret_cast<const u32x4*>(P + at);
+    if constexpr (ACT == ACT_SWIGLU) r.p[1] = *reinterpret_cast<const u32x4*>(P + plane + at);
+    return r;
+  }
+  __device__ __forceinline__ u32x4 operator()(int, int row, int col, const float (&d)[8], const Read& r) const {
+    const int64_t at = (int64_t)row * F + col;
     if constexpr (ACT == ACT_IDENTITY) {
       *reinterpret_cast<u32x4*>(dP + at) = pack_bf16x8(d);
-      return first;
+      return r.p[0];
     } else if constexpr (ACT == ACT_GELU_TANH) {
       float p[8], z[8], dp[8];
-      unpack_bf16x8(first, p);
+      unpack_bf16x8(r.p[0], p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float slope;
@@ -99,8 +110,8 @@ struct StoreBackward {
       return pack_bf16x8(z);
     } else {
       float g[8], u[8], z[8], dg[8], du[8];
-      unpack_bf16x8(first, g);
-      unpack_bf16x8(*reinterpret_cast<const u32x4*>(P + plane + at), u);
+      unpack_bf16x8(r.p[0], g);
+      unpack_bf16x8(r.p[1], u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float s = sigmoid(g[i]), h = g[i] * s;
@@ -155,12 +166,14 @@ __global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 
 // A bf16 result [M, N], or the two halves of its columns as matrices of their own (dW1 of a gated MLP).
 struct StorePlain {
+  using Read = Nothing;
   static constexpr bool kGated = false, kSymmetric = false, kMirror = false;
   uint16_t* C;
   int64_t ld;
   int64_t second;  // elements from the first matrix to the second
   int split;       // first column of the second matrix (INT_MAX: none)
-  __device__ __forceinline__ void operator()(int, int row, int col, const float (&v)[8]) const {
+  __device__ __forceinline__ Nothing read(int, int, int) const { return {}; }
+  __device__ __forceinline__ void operator()(int, int row, int col, const float (&v)[8], Nothing) const {
     uint16_t* p = col >= split ? C + second - split : C;
     *reinterpret_cast<u32x4*>(p + (int64_t)row * ld + col) = pack_bf16x8(v);
   }
@@ -200,7 +213,8 @@ hipError_t backward_first(const mlp2_train_s* p, int64_t M, const void* dY, cons
   return with_tile<false>(ch.tile, [&](auto tile) {
     using T = decltype(tile);
     using Dz = Problem<false, false, StoreBackward<ACT>>;
-    const Dz a = make_problem<T, Dz>(make_side(dY, H, M * H * 2), make_side(W2, H, F * H * 2), M, F, H, 1, epi, ch.split, p->split);
+    const Dz a = make_problem<T, Dz>(make_side(dY, H, M * H * 2), make_side(W2, H, F * H * 2), M, F, H, 1, epi, ch.split,
+                                 p->split);
     k_backward_first<T, Dz><<<a.items() + x.items(), T::THREADS, 0, s>>>(a, x);
     return hipGetLastError();
   });
@@ -219,20 +233,16 @@ hipError_t backward_second(const mlp2_train_s* p, int64_t M, const void* dY, con
   Side w1 = make_side(W1, F, H * F * 2);
   w1.jump_at = (int)(F / 64);  // without a gate K ends there
   w1.jump = H * F - F;
-  // Each product has a third of the workspace for its parts.
-  SplitSpace ws[3];
-  for (int i = 0; i < 3; ++i) {
-    ws[i] = SplitSpace{p->split.part + i * (p->split.part_floats / 3 / 64 * 64), p->split.part_floats / 3 / 64 * 64,
-                       p->split.arrived + i * (p->split.counters / 3) * kLine, p->split.counters / 3};
-  }
   return with_tile<false>(tile, [&](auto t) {
     using T = decltype(t);
     const Dx x = make_problem<T, Dx>(make_side(p->dP, nb * F, M * nb * F * 2), w1, mx, H, nb * F, 1, StorePlain{(uint16_t*)dX, H, 0, INT_MAX},
-                                     split[0], ws[0]);
+                                     split[0], p->split);
+    SplitSpace ws = behind<T>(p->split, x);
     const Dw a = make_problem<T, Dw>(make_side(p->Xt, rows, H * rows * 2), make_side(p->dP, nb * F, M * nb * F * 2), m1, nb * F, M, 1,
-                                     StorePlain{(uint16_t*)dW1, F, H * F, nb == 2 ? (int)F : INT_MAX}, split[1], ws[1]);
+                                     StorePlain{(uint16_t*)dW1, F, H * F, nb == 2 ? (int)F : INT_MAX}, split[1], ws);
+    ws = behind<T>(ws, a);
     const Dw b = make_problem<T, Dw>(make_side(p->Z, rows, F * rows * 2), make_side(dY, H, M * H * 2), m2, H, M, 1,
-                                     StorePlain{(uint16_t*)dW2, H, 0, INT_MAX}, split[2], ws[2]);
+                                     StorePlain{(uint16_t*)dW2, H, 0, INT_MAX}, split[2], ws);
     k_products<T, Bf16, Dx, Dw, Dw><<<x.items() + a.items() + b.items(), T::THREADS, 0, s>>>(x, a, b);
     return hipGetLastError();
   });
@@ -272,7 +282,9 @@ mlp2_train_t mlp2_train_plan(int64_t max_rows, int64_t H, int64_t F, int act, in
   p->device = device;
   p->num_cus = cus;
   const int64_t padded = round_up(max_rows, 64), z = padded * F * 2, dp = z * p->nb, xt = padded * H * 2;
-  const int64_t parts = (int64_t)1 << 27, counters = 4096 * kLine * 4;
+  const int64_t wide = H > p->nb * F ? H : p->nb * F;  // of any result
+  const int64_t tall = padded > H ? (padded > F ? padded : F) : (H > F ? H : F);
+  const int64_t floats = split_floats(tall, wide, 1), parts = floats * 4, counters = kSplitCounters * kLine * 4;
   if (hipMalloc((void**)&p->ws, (size_t)(z + dp + xt + parts + counters)) != hipSuccess ||
       hipMemset(p->ws + z + dp + xt + parts, 0, (size_t)counters) != hipSuccess) {
     (void)hipGetLastError();
@@ -284,7 +296,7 @@ mlp2_train_t mlp2_train_plan(int64_t max_rows, int64_t H, int64_t F, int act, in
   p->Z = (uint16_t*)p->ws;
   p->dP = (uint16_t*)(p->ws + z);
   p->Xt = (uint16_t*)(p->ws + z + dp);
-  p->split = SplitSpace{(float*)(p->ws + z + dp + xt), parts / 4, (uint32_t*)(p->ws + z + dp + xt + parts), 4096};
+  p->split = SplitSpace{(float*)(p->ws + z + dp + xt), floats, (uint32_t*)(p->ws + z + dp + xt + parts), kSplitCounters};
   return p;
 }
 

@@ -40,6 +40,32 @@ __device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
   }
 }
 
+// The same 8 elements as they are stored, for loads that run ahead of their use.
+template <class T>
+struct Piece;
+template <>
+struct Piece<uint16_t> {
+  u32x4 q;
+  __device__ __forceinline__ void load(const uint16_t* p, int n) {
+    if (n >= 8) {
+      q = *reinterpret_cast<const u32x4_any*>(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const { unpack_bf16x8(q, v); }
+};
+template <>
+struct Piece<float> {
+  float f[8];
+  __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, f); }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = f[i];
+  }
+};
+
 // The first n of 8 packed 16-bit values (or fp32 values) to p.
 __device__ __forceinline__ void store8_packed(uint16_t* p, int n, u32x4 q) {
   if (n >= 8) {
