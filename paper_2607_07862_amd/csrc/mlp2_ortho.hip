@@ -16,7 +16,8 @@
 // whatever the spectrum (Gaussian, power-law, low-rank and rank-one matrices
 // against 64 bits; the narrowest matrices are the worst):
 //   * X is held as two fp16 (22 bits); the products read the upper one, and
-//     a X is added from both.  B X rounds only inside B's columns, so the error
+//     a X is added from both (but in the last step, after which no error grows
+//     any more).  B X rounds only inside B's columns, so the error
 //     of a product does not feed the directions that are still small.  (With
 //     X in one fp16, a rank-one matrix came out 15 % off.)
 //   * A and B are scaled by 2^12 and 2^10, X by about the square root of its
@@ -51,9 +52,11 @@ __device__ __forceinline__ void unpack_f16x8(u32x4 q, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
 }
-// v as upper + lower fp16.
+// v as upper + lower fp16 (a null `lo`: the upper one alone).
 __device__ __forceinline__ void store_split(uint16_t* hi, uint16_t* lo, const float (&v)[8]) {
   u32x4 h = pack_f16x8(v);
+  *reinterpret_cast<u32x4*>(hi) = h;
+  if (!lo) return;
   // The rest is taken from the bits that are stored: left to itself the compiler converts twice, once from v and once inside the
   // instruction that makes v, which rounds differently in one element of some thousands.
   asm volatile("" : "+v"(h));
@@ -61,7 +64,6 @@ __device__ __forceinline__ void store_split(uint16_t* hi, uint16_t* lo, const fl
   unpack_f16x8(h, up);
 #pragma unroll
   for (int i = 0; i < 8; ++i) rest[i] = v[i] - up[i];
-  *reinterpret_cast<u32x4*>(hi) = h;
   *reinterpret_cast<u32x4*>(lo) = pack_f16x8(rest);
 }
 
@@ -77,11 +79,12 @@ __device__ __forceinline__ float block_sum(float v, float* buf) {
 
 // part[matrix][blockIdx.x]: sums of squares of a slice of the matrix.
 template <class T>
-__global__ __launch_bounds__(256) void k_ortho_squares(const T* G, int64_t n, float* part) {
-  __shared__ float buf[4];
+__global__ __launch_bounds__(1024) void k_ortho_squares(const T* G, int64_t n, float* part) {
+  __shared__ float buf[16];
   const T* g = G + (int64_t)blockIdx.y * n;
   float s = 0.f;
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048) {
+#pragma unroll 2
+  for (int64_t i = ((int64_t)blockIdx.x * 1024 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 8192) {
     float v[8];
     load8(g + i, (int)min(n - i, (int64_t)8), v);
 #pragma unroll
@@ -184,7 +187,7 @@ struct StorePoly {
 
 // X <- (a + diag B) X + (the rest of B) X.
 struct Update {
-  const uint16_t *hi, *lo;
+  const uint16_t *hi, *lo;  // lo: null where X is taken from its upper half alone
   const float* diag;
   int64_t n, m;
   float a, by;
@@ -194,7 +197,8 @@ struct Update {
   };
   __device__ __forceinline__ Read read(int batch, int row, int col) const {
     const int64_t at = ((int64_t)batch * n + row) * m + col;
-    return {*reinterpret_cast<const u32x4*>(hi + at), *reinterpret_cast<const u32x4*>(lo + at), diag[batch * n + row]};
+    return {*reinterpret_cast<const u32x4*>(hi + at), lo ? *reinterpret_cast<const u32x4*>(lo + at) : u32x4{0, 0, 0, 0},
+            diag[batch * n + row]};
   }
   __device__ __forceinline__ void operator()(const float (&v)[8], const Read& r, float (&o)[8]) const {
     float h[8], l[8];
@@ -215,7 +219,7 @@ struct StoreUpdate {
     float o[8];
     x(v, r, o);
     const int64_t at = ((int64_t)batch * x.n + row) * x.m + col;
-    store_split(hi + at, lo + at, o);
+    store_split(hi + at, lo ? lo + at : nullptr, o);
   }
 };
 
@@ -265,10 +269,11 @@ struct mlp2_ortho_s {
 
 namespace {
 
-hipError_t ortho_step(const mlp2_ortho_s* p, const float* coeff, bool apart, bool last, uint16_t* const (&X)[2],
+hipError_t ortho_step(const mlp2_ortho_s* p, const float* coeff, bool apart, int left, uint16_t* const (&X)[2],
                       uint16_t* const (&out)[2], void* O, hipStream_t s) {
   const int64_t n = p->n, m = p->m;
   const int count = (int)p->count;
+  const bool last = left == 0;  // steps after this one
   Side x = make_side(X[0], m, count * n * m * 2), sq = make_side(p->A, n, count * n * n * 2);
   x.batch = n * m;
   sq.batch = n * n;
@@ -280,8 +285,8 @@ hipError_t ortho_step(const mlp2_ortho_s* p, const float* coeff, bool apart, boo
   e = product<Fp16, false, false>(sq, sq, n, n, n, count, poly, p->split, p->num_cus, s);
   if (e != hipSuccess) return e;
   sq.p = p->B;
-  const Update update{X[0], X[1], p->diag, n, m, coeff[0], 1.f / kOrthoScaleB};
-  if (!last) return product<Fp16, false, true>(sq, x, n, m, n, count, StoreUpdate{update, out[0], out[1]}, p->split, p->num_cus, s);
+  const Update update{X[0], last ? nullptr : X[1], p->diag, n, m, coeff[0], 1.f / kOrthoScaleB};
+  if (!last) return product<Fp16, false, true>(sq, x, n, m, n, count, StoreUpdate{update, out[0], left == 1 ? nullptr : out[1]}, p->split, p->num_cus, s);
   const int rows = (int)p->rows, cols = (int)p->cols;
   if (p->tall)
     return product<Fp16, false, true>(sq, x, n, m, n, count, StoreLast<true>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
@@ -294,7 +299,7 @@ template <class T>
 void ortho_first(const mlp2_ortho_s* p, const void* G, float eps, hipStream_t s) {
   const int64_t n = p->rows * p->cols, slices = (n + 8191) / 8192;
   const int parts = (int)(slices < kOrthoParts ? slices : kOrthoParts);
-  k_ortho_squares<T><<<dim3(parts, (unsigned)p->count), 256, 0, s>>>((const T*)G, n, p->part);
+  k_ortho_squares<T><<<dim3(parts, (unsigned)p->count), 1024, 0, s>>>((const T*)G, n, p->part);
   const dim3 grid((unsigned)(p->n / 64 * (p->m / 64)), (unsigned)p->count);
   if (p->tall)
     k_ortho_scale<T, true><<<grid, 256, 0, s>>>((const T*)G, (int)p->rows, (int)p->cols, (int)p->n, (int)p->m, p->part, parts, eps,
@@ -374,7 +379,7 @@ int mlp2_ortho_run(mlp2_ortho_t p, const void* G, void* O, int steps, const floa
   else ortho_first<uint16_t>(p, G, eps, s);
   hipError_t e = hipGetLastError();
   for (int k = 0; k < steps && e == hipSuccess; ++k)
-    e = ortho_step(p, coeffs + 3 * k, k >= steps - kOrthoDiagSteps, k == steps - 1, p->X[k & 1], p->X[~k & 1], O, s);
+    e = ortho_step(p, coeffs + 3 * k, k >= steps - kOrthoDiagSteps, steps - 1 - k, p->X[k & 1], p->X[~k & 1], O, s);
   return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP);
 }
 

@@ -639,7 +639,9 @@ __device__ __forceinline__ void run_product(const P& a, int item, int batch, cha
   Acc<T> acc;
   if constexpr (T::NWAVES == 8) product_pingpong<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
   else product_loop<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
-  if (a.split > 1 && !join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, a.M - m0, lds)) return;
+  int go = 1;
+  if (a.split > 1) go = join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, a.M - m0, lds);
+  if (uniform(go) == 0) return;  // a scalar branch: barriers follow
   const int tid = thread_here(), lane = tid & 63, wave = uniform(tid >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
   const bool mirrored = !Epi::kSymmetric || tm_ != tn_;
@@ -690,8 +692,9 @@ __device__ __forceinline__ void run_product(const P& a, int item, int batch, cha
     if (!mirrored) return;
     __syncthreads();
     constexpr int CH = T::BM / 8;  // 16-byte pieces of a column of the tile
-    for (int i = tid; i < T::BN * CH; i += T::THREADS) {
-      const int col = i / CH, piece = i % CH;
+    static_assert(T::BN * CH % T::THREADS == 0, "whole rounds");
+    for (int j = 0; j < T::BN * CH / T::THREADS; ++j) {
+      const int i = tid + j * T::THREADS, col = i / CH, piece = i % CH;
       if (n0 + col < a.N && m0 + 8 * piece < a.epi.rows)
         a.epi.mirror(batch, n0 + col, m0 + 8 * piece, *reinterpret_cast<const u32x4*>(lds + col * mirror_pitch<T>() + 16 * piece));
     }

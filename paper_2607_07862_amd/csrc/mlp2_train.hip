@@ -140,16 +140,19 @@ struct Transpose {
     constexpr int PITCH = 64 + 8;  // elements
     uint16_t* t = reinterpret_cast<uint16_t*>(lds);
     const int across = (int)(H / 64), h0 = item % across * 64, m0 = item / across * 64;
-    for (int i = thread_here(); i < 512; i += THREADS) {
-      const int m = i / 8, h = i % 8 * 8;
+    static_assert(512 % THREADS == 0, "whole rounds");
+#pragma unroll
+    for (int j = 0; j < 512 / THREADS; ++j) {
+      const int i = thread_here() + j * THREADS, m = i / 8, h = i % 8 * 8;
       u32x4 q = {0, 0, 0, 0};
       if (m0 + m < M) q = *reinterpret_cast<const u32x4*>(X + (int64_t)(m0 + m) * H + h0 + h);
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[(h + e) * PITCH + m] = (uint16_t)(q[e / 2] >> (16 * (e & 1)));
     }
     __syncthreads();
-    for (int i = thread_here(); i < 512; i += THREADS) {
-      const int h = i / 8, m = i % 8 * 8;
+#pragma unroll
+    for (int j = 0; j < 512 / THREADS; ++j) {
+      const int i = thread_here() + j * THREADS, h = i / 8, m = i % 8 * 8;
       *reinterpret_cast<u32x4*>(Xt + (int64_t)(h0 + h) * rows + m0 + m) = *reinterpret_cast<const u32x4*>(t + h * PITCH + m);
     }
   }
