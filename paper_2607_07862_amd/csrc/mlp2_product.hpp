@@ -73,9 +73,10 @@ struct PTile {
   static_assert(BK == 32 || BK == 64, "stage depth");
   static_assert(EC == 32 * WN, "a wave owns 32 columns of every column panel");
   static_assert(RPANEL % (1024 * NWAVES) == 0 && CPANEL % (1024 * NWAVES) == 0, "every wave loads whole 1 KB pieces");
-  // Wave wm's row block tm: its rows lie in both halves of an eight-wave tile, together in a four-wave one.
+  // Wave wm's row block tm: in the quadrant tile its rows lie in both halves, elsewhere together.
+  static constexpr bool QUAD = NWAVES == 8 && COLP * EC == 256;
   __device__ static constexpr int row_of(int wm, int tm) {
-    return NWAVES == 8 ? 64 * wm + 16 * (tm & 3) + 128 * (tm >> 2) : wm * (BM / WM) + 16 * tm;
+    return QUAD ? 64 * wm + 16 * (tm & 3) + 128 * (tm >> 2) : wm * (BM / WM) + 16 * tm;
   }
 };
 using Tile64 = PTile<64, 1, 64, 1, 2, 2, 64, 4>;    // 64 x 64
@@ -228,7 +229,7 @@ struct RowFrag {
   }
   // Block tm of K slice ks; `stage` is the address of the stage's row panels.
   __device__ __forceinline__ u32x4 read(const char* stage, int ks, int tm) const {
-    const int half = T::NWAVES == 8 ? tm >> 2 : 0, blk = T::NWAVES == 8 ? tm & 3 : tm;
+    const int half = T::QUAD ? tm >> 2 : 0, blk = T::QUAD ? tm & 3 : tm;
     if constexpr (OUTER) {
       // Block blk is 2 blk chunks further on; the swizzle touches chunk bits 1 to 3, so the offset is XORed, not added.
       return read_tr(stage + half * T::RPANEL + (off[0] ^ (uint32_t)(32 * blk)) + ks * 64 * E, 8 * E);
@@ -269,8 +270,14 @@ struct ColFrag {
 template <class T>
 using Acc = f32x4[T::COLP][2][T::TM];
 
-// The plain loop: NS - 1 stages in flight, one barrier a stage.  st0 and nk
-// count stages of BK.
+// The plain loop.  st0 and nk count stages of BK.
+//
+// A stage's fragments are read from LDS while the stage before it is
+// multiplied (two register sets that swap roles, two stages a trip): the
+// latency of the reads, which one or two waves to a SIMD would otherwise wait
+// out once a stage, passes behind the products.  Stage it's ring slot is free
+// once every wave holds its fragments, at the barrier for stage it + 1, and
+// takes the loads of stage it + NS.
 template <class T, class Elem, bool RO, bool CO, bool JUMP>
 __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
                                              Acc<T>& acc, char* lds) {
@@ -288,41 +295,70 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
   PanelLoad<T, RO, false, false> r0(rs, batch, m0, 0, st0, nk, 0), r1(rs, batch, m0, T::ROWP - 1, st0, nk, (T::ROWP - 1) * T::RPANEL);
   PanelLoad<T, CO, true, JUMP> c0(cs, batch, n0, 0, st0, nk, C0),
       c1(cs, batch, n0, T::COLP - 1, st0, nk, C0 + (T::COLP - 1) * T::CPANEL);
-  uint32_t at = lds_base;  // the ring slot that is requested next
+  uint32_t to = lds_base;  // the ring slot that is requested next
   auto issue = [&]() {
-    r0.load(at);
-    if constexpr (T::ROWP == 2) r1.load(at);
-    c0.load(at);
-    if constexpr (T::COLP == 2) c1.load(at);
-    at = at == lds_base + (T::NS - 1) * T::STAGE ? lds_base : at + T::STAGE;
+    r0.load(to);
+    if constexpr (T::ROWP == 2) r1.load(to);
+    c0.load(to);
+    if constexpr (T::COLP == 2) c1.load(to);
+    to = to == lds_base + (T::NS - 1) * T::STAGE ? lds_base : to + T::STAGE;
   };
   const RowFrag<T, RO> rf(wm);
   const ColFrag<T, CO> cf(wn);
-#pragma unroll
-  for (int st = 0; st < T::NS - 1; ++st)
-    if (st < nk) issue();
-  const char* stage = lds;
-  for (int it = 0; it < nk; ++it) {
-    wait_stages_behind<T::LOADS, T::NS - 2>(min(T::NS - 2, nk - 1 - it));
-    __syncthreads();
-    if (it + T::NS - 1 < nk) issue();
+  struct Frags {
+    u32x4 x[T::KS][T::TM], w[T::KS][T::COLP][2];
+  };
+  const char* stage = lds;  // the ring slot that is read next
+  auto read = [&](Frags& f) {
 #pragma unroll
     for (int ks = 0; ks < T::KS; ++ks) {
-      u32x4 x[T::TM], w[T::COLP][2];
 #pragma unroll
-      for (int tm = 0; tm < T::TM; ++tm) x[tm] = rf.read(stage, ks, tm);
+      for (int tm = 0; tm < T::TM; ++tm) f.x[ks][tm] = rf.read(stage, ks, tm);
 #pragma unroll
       for (int p = 0; p < T::COLP; ++p)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) w[p][i] = cf.read(stage + C0 + p * T::CPANEL, ks, i);
+        for (int i = 0; i < 2; ++i) f.w[ks][p][i] = cf.read(stage + C0 + p * T::CPANEL, ks, i);
+    }
+    stage = stage == lds + (T::NS - 1) * T::STAGE ? lds : stage + T::STAGE;
+  };
+  auto mma = [&](const Frags& f) {
+#pragma unroll
+    for (int ks = 0; ks < T::KS; ++ks)
 #pragma unroll
       for (int p = 0; p < T::COLP; ++p)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int tm = 0; tm < T::TM; ++tm) acc[p][i][tm] = Elem::mfma(w[p][i], x[tm], acc[p][i][tm]);
-    }
-    stage = stage == lds + (T::NS - 1) * T::STAGE ? lds : stage + T::STAGE;
+          for (int tm = 0; tm < T::TM; ++tm) acc[p][i][tm] = Elem::mfma(f.w[ks][p][i], f.x[ks][tm], acc[p][i][tm]);
+  };
+  // Every wave's loads of stage st have arrived, and every wave holds the fragments of the stages before it.
+  auto resident = [&](int st) {
+    wait_stages_behind<T::LOADS, T::NS - 2>(min(T::NS - 2, nk - 1 - st));
+    __syncthreads();
+  };
+#pragma unroll
+  for (int st = 0; st < T::NS - 1; ++st)
+    if (st < nk) issue();
+  resident(0);
+  if (T::NS - 1 < nk) issue();
+  Frags fa, fb;
+  read(fa);
+  auto advance = [&](int it, Frags& now, Frags& next) {  // stage it is multiplied, stage it + 1 (< nk) read
+    resident(it + 1);
+    if (it + T::NS < nk) issue();
+    read(next);
+    mma(now);
+  };
+  int it = 0;
+  for (; it + 2 < nk; it += 2) {
+    advance(it, fa, fb);
+    advance(it + 1, fb, fa);
+  }
+  if (it + 1 < nk) {
+    advance(it, fa, fb);
+    mma(fb);
+  } else {
+    mma(fa);
   }
   __syncthreads();
 }
@@ -637,7 +673,7 @@ __device__ __forceinline__ void run_product(const P& a, int item, int batch, cha
   const int m0 = tm_ * T::BM, n0 = tn_ * COLS;
   const int st0 = s * a.per * UNIT, nk = min(a.per * UNIT, a.nk * UNIT - st0);
   Acc<T> acc;
-  if constexpr (T::NWAVES == 8) product_pingpong<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  if constexpr (T::QUAD) product_pingpong<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
   else product_loop<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
   int go = 1;
   if (a.split > 1) go = join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, a.M - m0, lds);
@@ -707,12 +743,14 @@ __global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   run_product<T, Elem>(a, blockIdx.x, blockIdx.y, lds);
 }
 
-// Three products in one launch: the items of `a` first, then b's and c's.
+// Three products in one launch: the items of a, b and c, from item `first` of
+// that order on and round to it (the longest items go first).
 template <class T, class Elem, class PA, class PB, class PC>
-__global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_products(const PA a, const PB b, const PC c) {
+__global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_products(const PA a, const PB b, const PC c,
+                                                                                                   int first) {
   __shared__ __align__(1024) char lds[T::LDS];
   static_assert(!PA::Epi::kMirror && !PB::Epi::kMirror && !PC::Epi::kMirror, "no room for a transpose");
-  const int na = a.items(), nb = b.items(), item = blockIdx.x;
+  const int na = a.items(), nb = b.items(), all = gridDim.x, from = blockIdx.x + first, item = from < all ? from : from - all;
   if (item < na) run_product<T, Elem>(a, item, 0, lds);
   else if (item < na + nb) run_product<T, Elem>(b, item - na, 0, lds);
   else run_product<T, Elem>(c, item - na - nb, 0, lds);
@@ -768,7 +806,7 @@ struct TileCost {
 inline TileCost tile_cost(int tile, bool gated) {
   if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 12.0, 4.0};
   if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 4.0};
-  return {64, 64, 2, gated ? 0.80 : 0.48, gated ? 0.50 : 0.30, 2.5, 4.0};
+  return {64, 64, 2, gated ? 0.80 : 0.50, gated ? 0.45 : 0.25, 3.0, 4.0};
 }
 constexpr double kBytesPerUs = 4.5e6;  // what products stream, about nine tenths of a large copy's rate
 
@@ -829,7 +867,7 @@ inline Choice choose(const Shape& s, const SplitSpace& ws, int num_cus) {
 }
 
 // One tile for products that share a launch, and the split of each: every
-// slot gets about the same work, so an item should not last longer than that.
+// slot gets about the same work, so no item should last longer than that.
 template <int N>
 int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&split)[N]) {
   int best = TILE_64;
@@ -851,9 +889,9 @@ int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&
       if (!tiles) continue;
       // (a long item shares its CU with short ones that mostly move data)
       const double unit = items <= num_cus ? t.alone : 0.5 * (t.alone + t.unit);
-      // An item may take two fifths of its slot's share, or what it takes for the overheads not to outweigh the work.
-      const double limit = 0.4 * share > 3 * t.item ? 0.4 * share : 3 * t.item;
-      int64_t want = (int64_t)(units * unit / limit + 0.999);
+      // An item longer than its slot's share is cut to three fifths of it, or to where overheads would outweigh the work.
+      const double whole = units * unit + t.item, limit = 0.6 * share > 3 * t.item ? 0.6 * share : 3 * t.item;
+      int64_t want = whole > share ? (int64_t)(units * unit / limit + 0.999) : 1;
       const int64_t room = split_room(s[i], t, ws);
       if (want > room) want = room;
       if (want > units) want = units;
@@ -915,11 +953,11 @@ hipError_t launch_product(const P& a, int batches, hipStream_t stream) {
 }
 
 // Calls f with the tile type of a choice.
-template <bool GATED, class F>
+template <class Epi, class F>
 auto with_tile(int tile, F&& f) {
   if (tile == TILE_256) return f(Tile256{});
   if (tile == TILE_128) return f(Tile128{});
-  if constexpr (GATED) return f(Tile64G{});
+  if constexpr (Epi::kGated) return f(Tile64G{});
   else return f(Tile64{});
 }
 
@@ -928,7 +966,7 @@ template <class Elem, bool RO, bool CO, class Epi>
 hipError_t product(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const Epi& epi, const SplitSpace& ws,
                    int num_cus, hipStream_t stream) {
   const Choice ch = choose({M, N, K, batches, Epi::kGated, Epi::kSymmetric}, ws, num_cus);
-  return with_tile<Epi::kGated>(ch.tile, [&](auto tile) {
+  return with_tile<Epi>(ch.tile, [&](auto tile) {
     using T = decltype(tile);
     return launch_product<T, Elem>(make_problem<T, Problem<RO, CO, Epi>>(r, c, M, N, K, batches, epi, ch.split, ws), batches, stream);
   });

@@ -213,7 +213,7 @@ hipError_t backward_first(const mlp2_train_s* p, int64_t M, const void* dY, cons
   const int64_t H = p->H, F = p->F;
   StoreBackward<ACT> epi{(const uint16_t*)P, p->dP, p->Z, M * F, F, (int)round_up(M, 64)};
   const Choice ch = choose({M, F, H, 1, false, false}, p->split, p->num_cus);
-  return with_tile<false>(ch.tile, [&](auto tile) {
+  return with_tile<StoreBackward<ACT>>(ch.tile, [&](auto tile) {
     using T = decltype(tile);
     using Dz = Problem<false, false, StoreBackward<ACT>>;
     const Dz a = make_problem<T, Dz>(make_side(dY, H, M * H * 2), make_side(W2, H, F * H * 2), M, F, H, 1, epi, ch.split,
@@ -236,7 +236,7 @@ hipError_t backward_second(const mlp2_train_s* p, int64_t M, const void* dY, con
   Side w1 = make_side(W1, F, H * F * 2);
   w1.jump_at = (int)(F / 64);  // without a gate K ends there
   w1.jump = H * F - F;
-  return with_tile<false>(tile, [&](auto t) {
+  return with_tile<StorePlain>(tile, [&](auto t) {
     using T = decltype(t);
     const Dx x = make_problem<T, Dx>(make_side(p->dP, nb * F, M * nb * F * 2), w1, mx, H, nb * F, 1, StorePlain{(uint16_t*)dX, H, 0, INT_MAX},
                                      split[0], p->split);
@@ -246,7 +246,8 @@ hipError_t backward_second(const mlp2_train_s* p, int64_t M, const void* dY, con
     ws = behind<T>(ws, a);
     const Dw b = make_problem<T, Dw>(make_side(p->Z, rows, F * rows * 2), make_side(dY, H, M * H * 2), m2, H, M, 1,
                                      StorePlain{(uint16_t*)dW2, H, 0, INT_MAX}, split[2], ws);
-    k_products<T, Bf16, Dx, Dw, Dw><<<x.items() + a.items() + b.items(), T::THREADS, 0, s>>>(x, a, b);
+    const int first = a.per > x.per ? x.items() : 0;
+    k_products<T, Bf16, Dx, Dw, Dw><<<x.items() + a.items() + b.items(), T::THREADS, 0, s>>>(x, a, b, first);
     return hipGetLastError();
   });
 }
