@@ -616,15 +616,13 @@ __device__ __forceinline__ bool join_parts(Acc<T>& acc, float* part, uint32_t* a
                                              0, kSc1);
   wait_all_mem();
   __syncthreads();
-  uint32_t* last = reinterpret_cast<uint32_t*>(lds);
-  if (tid == 0) {
-    uint32_t* count = arrived + tile * kLine;
-    const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *last = before;
-    if (before == (uint32_t)split - 1) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+  uint32_t* seen = reinterpret_cast<uint32_t*>(lds);
+  uint32_t* count = arrived + tile * kLine;
+  if (tid == 0) *seen = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  if (uniform(*last) != (uint32_t)split - 1) return false;
+  const uint32_t before = uniform(*seen);
+  if (before != (uint32_t)(split - 1)) return false;
+  if (tid == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
 #pragma unroll
   for (int c = 0; c < T::COLP * 2; ++c)
 #pragma unroll
