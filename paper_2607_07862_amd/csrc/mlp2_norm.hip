@@ -81,19 +81,32 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_norm_forward(const Norm
     if (a.w && n > 0) load8(a.w + col, n, w[c]);
     if (a.b && n > 0) load8(a.b + col, n, b[c]);
   }
-  for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += gridDim.x * GROUPS) {
-    const int row = row0 + group;
-    const bool live = row < a.M;
-    const XT* x = (const XT*)a.X + (int64_t)(live ? row : row0) * a.ldx;
-    float v[C][8], s[1] = {0.f};
+  Piece<XT> now[C], next[C];
+  auto request = [&](Piece<XT> (&p)[C], int row) {
+    const XT* x = (const XT*)a.X + (int64_t)(row < a.M ? row : a.M - 1) * a.ldx;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = 8 * (t + NT * c), n = a.H - col;
+      if (n > 0) p[c].load(x + col, n);
+    }
+  };
+  const int step = gridDim.x * GROUPS;
+  request(now, blockIdx.x * GROUPS + group);
+  for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += step) {
+    const int row = row0 + group;
+    const bool live = row < a.M;
+    if (row0 + step < a.M) request(next, row + step);
+    float v[C][8], s[1] = {0.f};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] = 0.f;
-      if (n > 0) load8(x + col, n, v[c]);
+    for (int c = 0; c < C; ++c) {
+      const int n = a.H - 8 * (t + NT * c);
+      now[c].values(v[c]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[0] += v[c][i];
+      for (int i = 0; i < 8; ++i) {
+        if (i >= n) v[c][i] = 0.f;
+        s[0] += v[c][i];
+      }
+      now[c] = next[c];
     }
     group_sum<NT>(s, buf[0]);
     const float mean = s[0] * inv;
