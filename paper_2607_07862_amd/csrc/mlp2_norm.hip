@@ -91,22 +91,19 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_norm_forward(const Norm
     }
   };
   const int step = gridDim.x * GROUPS;
-  request(now, blockIdx.x * GROUPS + group);
+  request(next, blockIdx.x * GROUPS + group);
   for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += step) {
     const int row = row0 + group;
     const bool live = row < a.M;
+#pragma unroll
+    for (int c = 0; c < C; ++c) now[c] = next[c];
     if (row0 + step < a.M) request(next, row + step);
     float v[C][8], s[1] = {0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int n = a.H - 8 * (t + NT * c);
-      now[c].values(v[c]);
+      now[c].values(v[c]);  // zeros past the row
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i >= n) v[c][i] = 0.f;
-        s[0] += v[c][i];
-      }
-      now[c] = next[c];
+      for (int i = 0; i < 8; ++i) s[0] += v[c][i];
     }
     group_sum<NT>(s, buf[0]);
     const float mean = s[0] * inv;
@@ -115,10 +112,13 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_norm_forward(const Norm
     for (int c = 0; c < C; ++c) {
       const int n = a.H - 8 * (t + NT * c);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[c][i] -= mean;
-        s[0] += i < n ? v[c][i] * v[c][i] : 0.f;
+      for (int i = 0; i < 8; ++i) v[c][i] -= mean;
+      if (n < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] = i < n ? v[c][i] : 0.f;
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[0] += v[c][i] * v[c][i];
     }
     group_sum<NT>(s, buf[1]);
     const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
@@ -178,30 +178,42 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
     r.rstd = a.rstd[at];
   };
   constexpr bool AHEAD = C == 1;
+  auto weights = [&](int c, float (&w)[8]) {
+    const int col = 8 * (t + NT * c), n = a.H - col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    if (a.w && n > 0) load8(a.w + col, n, w);
+  };
+  float mine[8];  // the weights, kept where the registers reach, else read again for every row
+  if constexpr (AHEAD) weights(0, mine);
   const int step = gridDim.x * GROUPS;
   Row now, next;
-  if constexpr (AHEAD) request(now, blockIdx.x * GROUPS + group);
+  if constexpr (AHEAD) request(next, blockIdx.x * GROUPS + group);
   int turn = 0;
   for (int row0 = blockIdx.x * GROUPS; row0 < a.M; row0 += step, turn ^= 1) {
     const int row = row0 + group;
     const bool live = row < a.M;
-    if constexpr (!AHEAD) request(now, row);
-    else if (row0 + step < a.M) request(next, row + step);
+    if constexpr (AHEAD) {
+      now = next;
+      if (row0 + step < a.M) request(next, row + step);
+    } else {
+      request(now, row);
+    }
     const float mean = now.mean, rstd = now.rstd;
     float xh[C][8], g[C][8], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = 8 * (t + NT * c), n = live ? a.H - col : 0;
       float w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = 1.f;
-      if (a.w && n > 0) load8(a.w + col, n, w);
+      if constexpr (!AHEAD) weights(c, w);
       now.x[c].values(xh[c]);
-      now.d[c].values(g[c]);
+      now.d[c].values(g[c]);  // zeros past the row: so are all sums there
+      if (!live) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xh[c][i] = g[c][i] = 0.f;
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        xh[c][i] = i < n ? (xh[c][i] - mean) * rstd : 0.f;
-        g[c][i] = i < n ? g[c][i] : 0.f;
+        xh[c][i] = (xh[c][i] - mean) * rstd;
         if constexpr (!IN_LDS) {
           dw[c][i] += g[c][i] * xh[c][i];
           db[c][i] += g[c][i];
@@ -222,23 +234,22 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        g[c][i] *= w[i];
+        g[c][i] *= AHEAD ? mine[i] : w[i];
         s[0] += g[c][i];
         s[1] += g[c][i] * xh[c][i];
       }
     }
     group_sum<NT>(s, buf[turn]);
-    const float m0 = s[0] * inv, m1 = s[1] * inv;
+    const float m0 = -rstd * (s[0] * inv), m1 = -rstd * (s[1] * inv);
     XT* dx = (XT*)a.Y + (int64_t)row * a.ldy;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = 8 * (t + NT * c), n = a.H - col;
       float o[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = rstd * (g[c][i] - m0 - xh[c][i] * m1);
+      for (int i = 0; i < 8; ++i) o[i] = rstd * g[c][i] + (m0 + xh[c][i] * m1);
       if (live && n > 0) store8(dx + col, n, o);
     }
-    if constexpr (AHEAD) now = next;
   }
   if (!a.part) return;
   if constexpr (IN_LDS)
@@ -267,10 +278,11 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
         __syncthreads();
         if (group == 0) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            for (int g = 0; g < GROUPS; ++g) v[i] += sums[g][i * NT + t];
-          }
+          for (int i = 0; i < 8; ++i) v[i] = 0.f;
+#pragma unroll 4
+          for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += sums[g][i * NT + t];
         }
       }
       if (group == 0 && n > 0) store8(to + (int64_t)which * a.H + col, n, v);

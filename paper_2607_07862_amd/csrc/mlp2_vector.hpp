@@ -40,12 +40,12 @@ __device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
   }
 }
 
-// The same 8 elements as they are stored, for loads that run ahead of their use.
+// The same 8 elements as they are stored, for loads that run ahead of their use; zeros until the first load.
 template <class T>
 struct Piece;
 template <>
 struct Piece<uint16_t> {
-  u32x4 q;
+  u32x4 q = {0, 0, 0, 0};
   __device__ __forceinline__ void load(const uint16_t* p, int n) {
     if (n >= 8) {
       q = *reinterpret_cast<const u32x4_any*>(p);
@@ -58,7 +58,7 @@ struct Piece<uint16_t> {
 };
 template <>
 struct Piece<float> {
-  float f[8];
+  float f[8] = {};
   __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, f); }
   __device__ __forceinline__ void values(float (&v)[8]) const {
 #pragma unroll
