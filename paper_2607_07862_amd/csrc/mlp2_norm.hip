@@ -4,13 +4,17 @@
 //   dx = rstd (g - mean(g) - xhat mean(g xhat)),   g = dy w,  xhat = (x - mean) rstd
 //   dw = sum over rows of dy xhat,   db = sum over rows of dy
 //
-// Both directions are bound by memory traffic.  A row is held in registers by
-// a group of 16 to 1024 threads (up to 16 elements a thread), so each input is
-// read once; the variance is taken around the mean in a second pass over the
-// registers.  The groups of a persistent grid walk the rows with the weights
+// Both directions are bound by memory traffic: bf16 8192 x 4096 takes 26 us
+// forward (5.1 TB/s; a large copy reaches 4.9) and 52 us backward (3.9 TB/s, 5 us
+// of it in the second kernel),
+// fp32 to bf16 16384 x 8192 146 (5.5) and 256 us (5.2).  Calls of a few rows are
+// bound by their launch (4 us).  A row is held in registers by a group of 16 to
+// 1024 threads (up to 16 elements a thread), so each input is read once; the
+// variance is taken around the mean in a second pass over the registers.  The groups of a persistent grid walk the rows with the weights
 // (forward) or the running dw and db of their columns (backward) in registers.
-// The backward pass leaves one partial dw and db per work-group, and a second
-// small kernel adds these in a fixed order: no atomics, the same bits each run.
+// The backward pass leaves one partial dw and db per work-group.  Few and short
+// ones are added by the work-group that finishes last, others by a second small
+// kernel; either adds in a fixed order and gives the same bits each run.
 #include <new>
 
 #include "mlp2_host.h"
@@ -60,7 +64,12 @@ struct NormArgs {
   int64_t ldx, ldd, ldy;
   int M, H;
   float eps;
+  float *dw, *db;     // backward: written by a work-group alone, or by the last one to arrive
+  uint32_t* arrived;  // null: another kernel adds the parts
 };
+
+// Floats of a part's dw (and of its db, which follows).
+__host__ __device__ __forceinline__ int part_pitch(int H) { return (H + 7) / 8 * 8; }
 
 // NT threads a row, C pieces of 8 elements a thread: NT * 8 * C >= H.
 template <class XT, class YT, int NT, int C>
@@ -260,40 +269,95 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
         dw[c][i] = kept[4 * c + i / 4][threadIdx.x][i % 4];
         db[c][i] = kept[4 * c + 2 + i / 4][threadIdx.x][i % 4];
       }
-  // The groups' sums of the same columns meet in LDS, one piece after the other.
-  __shared__ float sums[GROUPS][GROUPS > 1 ? NT * 8 : 1];
-  float* to = a.part + (int64_t)blockIdx.x * 2 * a.H;
+  // The groups' sums of the same columns meet in LDS: eight groups a thread, then what is left.
+  if constexpr (GROUPS > 1) {
+    constexpr int COLS = NT * 8, LEFT = GROUPS > 8 ? GROUPS / 8 : 1, EACH = GROUPS / LEFT;
+    __shared__ float sums[2][GROUPS][COLS];
 #pragma unroll
-  for (int which = 0; which < 2; ++which)
+    for (int i = 0; i < 8; ++i) {
+      sums[0][group][i * NT + t] = dw[0][i];
+      sums[1][group][i * NT + t] = db[0][i];
+    }
+    __syncthreads();
+    if constexpr (LEFT > 1) {
+      const int col = threadIdx.x % COLS, first = threadIdx.x / COLS * EACH;
+      float some[2] = {0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = 8 * (t + NT * c), n = a.H - col;
-      float v[8];
+      for (int g = 0; g < EACH; ++g)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = which ? db[c][i] : dw[c][i];
-      if constexpr (GROUPS > 1) {
-        __syncthreads();
+        for (int k = 0; k < 2; ++k) some[k] += sums[k][first + g][col];
+      // (nobody else reads these columns of these groups)
+      sums[0][first][col] = some[0];
+      sums[1][first][col] = some[1];
+      __syncthreads();
+    }
+    if (group == 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[group][i * NT + t] = v[i];
-        __syncthreads();
-        if (group == 0) {
+      for (int i = 0; i < 8; ++i) dw[0][i] = db[0][i] = 0.f;
+      constexpr int STEP = LEFT > 1 ? EACH : 1;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = 0.f;
-#pragma unroll 4
-          for (int g = 0; g < GROUPS; ++g)
+      for (int g = 0; g < GROUPS; g += STEP)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += sums[g][i * NT + t];
+        for (int i = 0; i < 8; ++i) {
+          dw[0][i] += sums[0][g][i * NT + t];
+          db[0][i] += sums[1][g][i * NT + t];
+        }
+    }
+  }
+  constexpr int kSc1 = 16;  // device scope: stores written through, loads past this XCD's L2
+  const int pitch = part_pitch(a.H);
+  const auto parts = __builtin_amdgcn_make_buffer_rsrc(a.part, 0, (int)(gridDim.x * 8u * pitch), 0x00027000);
+  if (group == 0) {
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = 8 * (t + NT * c), n = a.H - col;
+        if (n <= 0) continue;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = which ? db[c][i] : dw[c][i];
+        if (gridDim.x == 1) {
+          float* to = which ? a.db : a.dw;
+          if (to) store8(to + col, n, v);
+        } else {
+          const int at = 4 * ((blockIdx.x * 2 + which) * pitch + col);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}), parts, at, 0, kSc1);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}), parts, at + 16, 0, kSc1);
         }
       }
-      if (group == 0 && n > 0) store8(to + (int64_t)which * a.H + col, n, v);
+  }
+  if (!a.arrived || gridDim.x == 1) return;
+  __shared__ uint32_t seen;
+  wait_all_mem();
+  __syncthreads();
+  if (threadIdx.x == 0) seen = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (uniform(seen) != gridDim.x - 1) return;
+  if (threadIdx.x == 0) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next call expects it
+  for (int col = 4 * threadIdx.x; col < 2 * pitch; col += 4 * kNormBlock) {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int first = 0; first < (int)gridDim.x; first += 8) {
+      u32x4 v[8] = {};  // in flight together
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (first + i < (int)gridDim.x) v[i] = __builtin_amdgcn_raw_buffer_load_b128(parts, 4 * ((first + i) * 2 * pitch + col), 0, kSc1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += __builtin_bit_cast(f32x4, v[i]);
     }
+    const int c = col >= pitch ? col - pitch : col;
+    float* to = col >= pitch ? a.db : a.dw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (to && c + i < a.H) to[c + i] = sum[i];
+  }
 }
 
-// dw and db from the work-groups' partials: 32 columns of [parts][2 H] a work-group, 32 threads a column.
+// dw and db from the work-groups' partials: 32 columns of [parts][2 pitch] a work-group, 32 threads a column.
 __global__ __launch_bounds__(1024) void k_norm_reduce(const float* part, int parts, int H, float* dw, float* db) {
   __shared__ float sums[32][33];
   const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
-  const int64_t width = 2 * (int64_t)H, col = (int64_t)blockIdx.x * 32 + lane;
+  const int64_t pitch = part_pitch(H), width = 2 * pitch, col = (int64_t)blockIdx.x * 32 + lane;
   float s = 0.f;
   if (col < width) {
 #pragma unroll 8
@@ -305,8 +369,9 @@ __global__ __launch_bounds__(1024) void k_norm_reduce(const float* part, int par
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) s += sums[i][lane];
-    float* to = col < H ? dw : db;
-    if (to) to[col < H ? col : col - H] = s;
+    float* to = col < pitch ? dw : db;
+    const int64_t c = col < pitch ? col : col - pitch;
+    if (to && c < H) to[c] = s;
   }
 }
 
@@ -318,8 +383,17 @@ struct mlp2_norm_s {
   int64_t rows = 0, H = 0;
   int x = 0, y = 0, device = -1, num_cus = 0;
   float* part = nullptr;
+  uint32_t* arrived = nullptr;  // work-groups of a backward pass whose part is written
   int max_parts = 0;
 };
+
+// The last work-group adds the parts of at most 32 work-groups and 128 KB: one
+// CU reads these past its L2 in about 3 us, where another launch takes 3.4 us of
+// the host and 4 of the GPU.  bf16, us a call one after the other, by the last
+// work-group and by another kernel: 64 x 1024 (64 KB) 6.5 and 7.6, 8 x 4096 (128
+// KB) 8.5 and 7.8 (10.4 where Python issues them), 256 x 1024 (256 KB) 8.2 and
+// 7.6, 64 x 4096 (1 MB) 16.8 and 7.7.
+constexpr int kJoinParts = 32, kJoinBytes = 128 << 10;
 
 namespace {
 
@@ -403,12 +477,15 @@ mlp2_norm_t mlp2_norm_plan(int64_t max_rows, int64_t H, int x_dtype, int y_dtype
   p->device = device;
   p->num_cus = cus;
   p->max_parts = cus;  // one backward work-group per CU
-  if (hipMalloc((void**)&p->part, (size_t)p->max_parts * 2 * H * sizeof(float)) != hipSuccess) {
+  const size_t bytes = (size_t)p->max_parts * 2 * part_pitch((int)H) * sizeof(float);
+  if (hipMalloc((void**)&p->part, bytes + sizeof(uint32_t)) != hipSuccess || hipMemset((char*)p->part + bytes, 0, sizeof(uint32_t)) != hipSuccess) {
     (void)hipGetLastError();
+    (void)hipFree(p->part);
     delete p;
     record_error(MLP2_ERR_HIP);
     return nullptr;
   }
+  p->arrived = (uint32_t*)((char*)p->part + bytes);
   return p;
 }
 
@@ -456,6 +533,7 @@ int mlp2_norm_backward(mlp2_norm_t p, int64_t M, const void* dY, int64_t lddy, c
   hipStream_t s = (hipStream_t)stream;
   const bool grads = dweight || dbias;
   int parts = 0;
+  bool joined = false;
   if (M > 0) {
     NormArgs a{};
     a.X = X;
@@ -473,11 +551,15 @@ int mlp2_norm_backward(mlp2_norm_t p, int64_t M, const void* dY, int64_t lddy, c
     const int groups = kNormBlock / backward_threads(p->H);
     const int64_t blocks = (M + groups - 1) / groups;
     parts = (int)(blocks < p->max_parts ? blocks : p->max_parts);
+    joined = parts == 1 || (parts <= kJoinParts && parts * 8 * part_pitch(a.H) <= kJoinBytes);
+    a.dw = dweight;
+    a.db = dbias;
+    a.arrived = joined ? p->arrived : nullptr;
     const hipError_t e = launch_norm(p, false, a, parts, s);
     if (e != hipSuccess) return record_error(MLP2_ERR_HIP);
   }
-  if (grads) {
-    k_norm_reduce<<<(unsigned)((2 * p->H + 31) / 32), 1024, 0, s>>>(p->part, parts, (int)p->H, dweight, dbias);
+  if (grads && !joined) {
+    k_norm_reduce<<<(unsigned)((2 * part_pitch((int)p->H) + 31) / 32), 1024, 0, s>>>(p->part, parts, (int)p->H, dweight, dbias);
     if (hipGetLastError() != hipSuccess) return record_error(MLP2_ERR_HIP);
   }
   return MLP2_OK;

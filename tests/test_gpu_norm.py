@@ -125,6 +125,28 @@ def test_no_rows_and_fewer_than_planned(lib):
         check(M, H, BF, BF, plan=plan)
 
 
+@pytest.mark.parametrize("H,rows", [(1000, (8, 9, 128, 129, 2, 264)), (64, (64, 65, 2048, 2049)), (1, (64, 2048, 2112)), (4093, (2, 3, 8, 10)), (16381, (1, 2))])
+def test_weight_gradients_of_one_few_and_many_work_groups(lib, H, rows):
+    """A work-group writes them alone, the last of few adds their parts, another kernel those of many: one plan, in turn."""
+    plan = B.NormPlan(max(rows), H, BF)
+    for M in rows + rows[:1]:
+        check(M, H, BF, BF, seed=M, plan=plan)
+
+
+@pytest.mark.parametrize("M,H", [(128, 1024), (2048, 64), (1024, 1024)])
+def test_weight_gradients_have_the_same_bits_every_time(lib, M, H):
+    g = case(M, H, BF, BF)
+    plan = B.NormPlan(M, H, BF)
+    Y, mean, rstd = torch.empty_like(g["X"]), torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    plan.forward(g["X"], g["w"], g["b"], Y, mean, rstd)
+    runs = []
+    for _ in range(20):
+        dw, db = torch.empty(H, device="cuda"), torch.empty(H, device="cuda")
+        plan.backward(g["dY"], g["X"], g["w"], mean, rstd, Y, dw, db)
+        runs.append(torch.stack((dw, db)))
+    assert all(torch.equal(runs[0], r) for r in runs[1:])
+
+
 def test_a_bad_row_stays_alone(lib):
     M, H = 30, 900
     g = case(M, H, F32, F32)
