@@ -33,7 +33,16 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def short_name(n: str) -> str:
-    """k_mlp2<Tile<BM, BN, WM, WN, NS[, BK[, NT]]>, NB, Tile<...>, HV, PHASE> -> phase and tile shape."""
+    """k_mlp2<Tile<BM, BN, WM, WN, NS[, BK[, NT]]>, NB, Tile<...>, HV, PHASE> -> phase and tile shape; the training
+    products (k_product<PTile<ER, ROWP, EC, COLP, WM, WN, BK, NS>, type, Problem<...>>) -> name, epilogue and tile."""
+    m = re.search(r"(k_products?|k_backward_first)<mlp2::PTile<([\d, ]+)>", n)
+    if m:
+        t = [int(x) for x in m.group(2).split(",")]
+        store = [re.sub(r"<(\d+|true|false)>$", r" \1", x) for x in re.findall(r"mlp2::(Store\w+(?:<\w+>)?)", n.split("(")[0])]
+        return f"{m.group(1)} {' + '.join(store)} (tile {t[0] * t[1]} x {t[2] * t[3]}, stages {t[7]}, waves {t[4] * t[5]})"
+    m = re.search(r"mlp2::(k_(?:norm|ortho)_\w+)(<[^>]*>)?", n)
+    if m:
+        return m.group(1) + (m.group(2) or "")
     m = re.search(r"k_mlp2<mlp2::Tile<([^>]*)>, (\d), mlp2::Tile<([^>]*)>, (\d), (\d)>", n)
     if m:
         t1 = [x.strip() for x in m.group(1).split(",")]
@@ -163,7 +172,7 @@ def counters(args):
         f = _one(os.path.join(d, "**", "*counter_collection.csv"))
         acc = defaultdict(lambda: defaultdict(float))
         for r in csv.DictReader(open(f)):
-            if "k_mlp2" not in r["Kernel_Name"]:
+            if not re.search(r"k_(mlp2|products?|backward_first|norm_\w+|ortho_\w+)\b", r["Kernel_Name"]):
                 continue
             acc[(r["Kernel_Name"], r["Dispatch_Id"])][r["Counter_Name"]] += float(r["Counter_Value"])
         for (k, _), cs in acc.items():
