@@ -5,16 +5,17 @@
 //   dw = sum over rows of dy xhat,   db = sum over rows of dy
 //
 // Both directions are bound by memory traffic: bf16 8192 x 4096 takes 26 us
-// forward (5.1 TB/s; a large copy reaches 4.9) and 52 us backward (3.9 TB/s, 5 us
-// of it in the second kernel),
-// fp32 to bf16 16384 x 8192 146 (5.5) and 256 us (5.2).  Calls of a few rows are
-// bound by their launch (4 us).  A row is held in registers by a group of 16 to
-// 1024 threads (up to 16 elements a thread), so each input is read once; the
-// variance is taken around the mean in a second pass over the registers.  The groups of a persistent grid walk the rows with the weights
-// (forward) or the running dw and db of their columns (backward) in registers.
-// The backward pass leaves one partial dw and db per work-group.  Few and short
-// ones are added by the work-group that finishes last, others by a second small
-// kernel; either adds in a fixed order and gives the same bits each run.
+// forward (5.1 TB/s; a large copy reaches 4.9) and 52 backward (3.9 TB/s, 5 us of
+// it in the second kernel), fp32 to bf16 16384 x 8192 146 (5.5 TB/s) and 256 us
+// (5.2).  Calls of a few rows are bound by their launch, 4 us.  A row is held in
+// registers by a group of 16 to 1024 threads (up to 16 elements a thread), so
+// each input is read once; the variance is taken around the mean in a second
+// pass over the registers.  The groups of a persistent grid walk the rows with
+// the weights (forward) or the running dw and db of their columns (backward) in
+// registers.  The backward pass leaves one partial dw and db per work-group.  Few
+// and short ones are added by the work-group that finishes last, others by a
+// second small kernel; either adds in a fixed order and gives the same bits each
+// run.
 #include <new>
 
 #include "mlp2_host.h"

@@ -6,15 +6,24 @@
 // on the short side: a tall matrix is transposed where it is scaled, and its
 // result on the way out, so that A = X X^T has K contiguous in both operands
 // (the fastest order).  A and B are symmetric: only their tiles on and above the
-// diagonal are computed, and stored twice.  Every product runs on the matrix cores in fp16 with
-// fp32 sums.  fp16 rather than bf16 because the iteration lifts the small
-// singular values by up to a^steps, and with them what rounding leaves there:
-// the values are bounded (the singular values stay below about 1.3), so the
-// range of fp16 is enough once each matrix has its own power-of-two scale, and
-// its three more bits are needed.  Three choices keep a bf16 result's
-// error within 1.05 to 1.5 times that of its own rounding (1.7e-3 of the norm),
-// whatever the spectrum (Gaussian, power-law, low-rank and rank-one matrices
-// against 64 bits; the narrowest matrices are the worst):
+// diagonal are computed, and stored twice.
+//
+// The matrix cores bound it: a step of 14336 x 4096 takes 250 us for A (136 tiles
+// of 256 x 256 on 256 CUs; one part of K each, since three parts, 25 us shorter
+// alone, left the whole run where it was), 90 for B and 450 for X (1.07 PFLOP/s
+// with 470 MB of both halves of X read and written in its epilogue).  Small ones
+// are bound by the fixed costs of three launches a step: 2 x 512 x 2048 takes 9.8,
+// 6.5 and 9.8 us.
+//
+// Every product runs on the matrix cores in fp16 with fp32 sums.  fp16 rather
+// than bf16 because the iteration lifts the small singular values by up to
+// a^steps, and with them what rounding leaves there: the values are bounded (the
+// singular values stay below about 1.3), so the range of fp16 is enough once each
+// matrix has its own power-of-two scale, and its three more bits are needed.
+// Three choices keep a bf16 result's error within 1.05 to 1.5 times that of its
+// own rounding (1.7e-3 of the norm), whatever the spectrum (Gaussian, power-law,
+// low-rank and rank-one matrices against 64 bits; the narrowest matrices are the
+// worst):
 //   * X is held as two fp16 (22 bits); the products read the upper one, and
 //     a X is added from both (but in the last step, after which no error grows
 //     any more).  B X rounds only inside B's columns, so the error
@@ -77,7 +86,7 @@ __device__ __forceinline__ float block_sum(float v, float* buf) {
   return v;
 }
 
-// part[matrix][blockIdx.x]: sums of squares of a slice of the matrix.
+// part[matrix][blockIdx.x]: sums of squares of a slice of the matrix.  Bound by the read: fp32 2 x 4096 x 14336 103 us (4.6 TB/s).
 template <class T>
 __global__ __launch_bounds__(1024) void k_ortho_squares(const T* G, int64_t n, float* part) {
   __shared__ float buf[16];
@@ -95,6 +104,7 @@ __global__ __launch_bounds__(1024) void k_ortho_squares(const T* G, int64_t n, f
 }
 
 // The first X [n][m] (n <= m, padded to 64): G, transposed if it is tall, scaled, zeros in the padding.  One 64 x 64 block a work-group.
+// Bound by memory traffic: fp32 2 x 4096 x 14336 163 us (5.8 TB/s), 14336 x 4096, through LDS, 90 us (5.2).
 template <class T, bool TALL>
 __global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int cols, int n, int m, const float* part, int parts,
                                                      float eps, float scale, uint16_t* hi, uint16_t* lo) {

@@ -278,6 +278,10 @@ using Acc = f32x4[T::COLP][2][T::TM];
 // out once a stage, passes behind the products.  Stage it's ring slot is free
 // once every wave holds its fragments, at the barrier for stage it + 1, and
 // takes the loads of stage it + NS.
+//
+// LDS bounds it: a 64 x 64 x 64 unit reads 32 KB of fragments and takes in 16
+// KB, 384 clocks at 128 bytes each, and measures 0.2 us on a CU of its own; twice
+// the stages gained nothing (the Gram matrices of 2 x 512 x 2048 9.8 -> 10.4 us).
 template <class T, class Elem, bool RO, bool CO, bool JUMP>
 __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
                                              Acc<T>& acc, char* lds) {
@@ -384,7 +388,8 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
 //     slot p (lgkmcnt(0)) and its ring slot is requested again in memory slot
 //     p + 2, after the barrier that ends the trailing waves' product slot p.
 // Here the two sides may have either storage order, and every panel carries
-// its own 64-bit base and range.
+// its own 64-bit base and range.  8192 x 8192 x 8192 in bf16: K contiguous on both
+// sides 731 us (1.50 PFLOP/s), on the row side 749 (1.47), on neither 926 (1.19).
 template <class T, class Elem, bool RO, bool CO, bool JUMP>
 __device__ __forceinline__ void product_pingpong(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
                                                  Acc<T>& acc, char* lds) {
