@@ -632,15 +632,27 @@ __device__ __forceinline__ bool join_parts(Acc<T>& acc, float* part, uint32_t* a
   for (int c = 0; c < T::COLP * 2; ++c)
 #pragma unroll
     for (int tm = 0; tm < T::TM; ++tm) acc[c / 2][c % 2][tm] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int q = 0; q < split; ++q) {
+  // Loads in flight together: those of 8 row blocks with the largest tile, of a whole part or of several with the others
+  // (a part a round trip past the L2 takes about 0.35 us; 27 parts of a 64 x 64 tile 15.2 us).
+  constexpr int AHEAD = BLOCKS >= 16 ? 1 : 32 / BLOCKS, COLS = BLOCKS > 16 ? 1 : T::COLP * 2;
+  for (int q = 0; q < split; q += AHEAD) {
 #pragma unroll
-    for (int c = 0; c < T::COLP * 2; ++c) {
-      u32x4 v[T::TM];  // in flight together
+    for (int c0 = 0; c0 < T::COLP * 2; c0 += COLS) {
+      u32x4 v[AHEAD][COLS][T::TM] = {};
 #pragma unroll
-      for (int tm = 0; tm < T::TM; ++tm)
-        v[tm] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(off[tm] + q * (ITEM * 4) + (c * T::TM + tm) * 1024), 0, kSc1);
+      for (int d = 0; d < AHEAD; ++d)
+        if (q + d < split)
 #pragma unroll
-      for (int tm = 0; tm < T::TM; ++tm) acc[c / 2][c % 2][tm] += __builtin_bit_cast(f32x4, v[tm]);
+          for (int c = 0; c < COLS; ++c)
+#pragma unroll
+            for (int tm = 0; tm < T::TM; ++tm)
+              v[d][c][tm] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(off[tm] + (q + d) * (ITEM * 4) + ((c0 + c) * T::TM + tm) * 1024), 0, kSc1);
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d)
+#pragma unroll
+        for (int c = 0; c < COLS; ++c)
+#pragma unroll
+          for (int tm = 0; tm < T::TM; ++tm) acc[(c0 + c) / 2][(c0 + c) % 2][tm] += __builtin_bit_cast(f32x4, v[d][c][tm]);
     }
   }
   return true;
@@ -800,16 +812,18 @@ struct Shape {
 // What a tile costs a work-group, in microseconds: `unit` for 64 of K with every
 // slot of the chip taken, `alone` with at most one work-group to a CU, `item`
 // once (prologue and epilogue), `join` for meeting the other parts of K beside
-// the traffic of their sums.  Measured with the products of 2048 x 4096 x 14336
-// (every slot taken), 24 x 4096 x 14336 and 64 x 512 x 2048.
+// the traffic of their sums, and `part` for each of them.  Measured with the
+// products of 2048 x 4096 x 14336 (every slot taken), 24 x 4096 x 14336, 64 x 512 x
+// 2048 and the Gram matrices of 4 x 37 x 5081 (64 x 64 tiles, 2, 4, 8, 16 and 27
+// parts: 12.8, 9.6, 8.0, 9.0 and 11.9 us).
 struct TileCost {
   int rows, cols, slots;  // slots: work-groups to a CU
-  double unit, alone, item, join;
+  double unit, alone, item, join, part;
 };
 inline TileCost tile_cost(int tile, bool gated) {
-  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 12.0, 4.0};
-  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 4.0};
-  return {64, 64, 2, gated ? 0.80 : 0.50, gated ? 0.45 : 0.25, 3.0, 4.0};
+  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 12.0, 4.0, 0.0};
+  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 4.0, 0.0};
+  return {64, 64, 2, gated ? 0.80 : 0.50, gated ? 0.45 : 0.25, 3.0, 0.5, gated ? 0.5 : 0.3};
 }
 constexpr double kBytesPerUs = 4.5e6;  // what products stream, about nine tenths of a large copy's rate
 
@@ -834,7 +848,7 @@ inline int64_t split_room(const Shape& s, const TileCost& t, const SplitSpace& w
 // Microseconds for the parts' sums, written and read.
 inline double join_time(const Shape& s, const TileCost& t, int64_t split) {
   const int64_t rows = s.M < t.rows ? round_up(s.M, 16) : t.rows;
-  return split > 1 ? t.join + 8.0 * tiles_of(s, t) * split * rows * t.cols * (s.gated ? 2 : 1) / kBytesPerUs : 0.0;
+  return split > 1 ? t.join + t.part * split + 8.0 * tiles_of(s, t) * split * rows * t.cols * (s.gated ? 2 : 1) / kBytesPerUs : 0.0;
 }
 
 // Time of the tiles' items: whole rounds of the chip's slots, then the rest, but no less than the operands' traffic.
@@ -900,7 +914,7 @@ int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&
       if (want > units) want = units;
       if (want > kMaxSplit) want = kMaxSplit;
       if (want > 1) parts[i] = (int)want;
-      const double one = (double)((units + parts[i] - 1) / parts[i]) * unit + t.item + (parts[i] > 1 ? t.join : 0.0);
+      const double one = (double)((units + parts[i] - 1) / parts[i]) * unit + t.item + (parts[i] > 1 ? t.join + t.part * parts[i] : 0.0);
       if (one > longest) longest = one;
       if (parts[i] > 1) extra += (double)tiles * (parts[i] - 1) * t.item / slots + 0.5 * join_time(s[i], t, parts[i]);
     }
