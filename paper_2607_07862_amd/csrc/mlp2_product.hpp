@@ -23,6 +23,8 @@
 // columns of one row for each pair of 16 x 16 blocks.
 #pragma once
 
+#include <cmath>
+
 #include "mlp2_device.hpp"
 #include "mlp2_host.h"
 
@@ -814,18 +816,24 @@ struct Shape {
 // once (prologue and epilogue), `join` for meeting the other parts of K beside
 // the traffic of their sums, and `part` for each of them.  Measured with the
 // products of 2048 x 4096 x 14336 (every slot taken), 24 x 4096 x 14336, 64 x 512 x
-// 2048 and the Gram matrices of 4 x 37 x 5081 (64 x 64 tiles, 2, 4, 8, 16 and 27
-// parts: 12.8, 9.6, 8.0, 9.0 and 11.9 us).
+// 2048, and by their parts of K: the Gram matrices of 4 x 37 x 5081 (64 x 64 tiles;
+// 2, 4, 8, 16 and 27 parts 12.8, 9.6, 8.0, 9.0 and 11.9 us) and of 1664 x 6656 (128 x
+// 128; 1, 2, 4 and 5 parts 69, 45, 38 and 38), 2063 x 768 with K = 8192 (256 x 256;
+// 1, 2, 3, 4, 6 and 8 parts 131, 81, 65, 60, 62 and 65).
 struct TileCost {
   int rows, cols, slots;  // slots: work-groups to a CU
   double unit, alone, item, join, part;
 };
-inline TileCost tile_cost(int tile, bool gated) {
-  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 12.0, 4.0, 0.0};
-  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 4.0, 0.0};
-  return {64, 64, 2, gated ? 0.80 : 0.50, gated ? 0.45 : 0.25, 3.0, 0.5, gated ? 0.5 : 0.3};
+// `once`: every weight is read by one row of tiles, from memory and not from an
+// L2 (23 rows of 7104 by 2 x 18944, 296 tiles: 153 us, in two parts of K 111).
+inline TileCost tile_cost(int tile, bool gated, bool once) {
+  if (tile == TILE_256) return {256, gated ? 128 : 256, 1, 1.40, 1.20, 12.0, 1.0, 1.5};
+  if (tile == TILE_128) return {128, gated ? 64 : 128, 2, 1.20, 0.65, 4.0, 2.5, 0.8};
+  if (gated) return {64, 64, 2, once ? 1.30 : 0.80, once ? 0.58 : 0.45, 3.0, 0.5, 0.5};
+  return {64, 64, 2, 0.50, 0.25, 3.0, 0.5, 0.3};
 }
-constexpr double kBytesPerUs = 4.5e6;  // what products stream, about nine tenths of a large copy's rate
+constexpr double kBytesPerUs = 6.0e6;   // what parts are written and read at (most stay in the last-level cache)
+constexpr double kStreamPerUs = 5.2e6;  // what a product reads its operands at
 
 struct Choice {
   int tile, split;
@@ -851,15 +859,18 @@ inline double join_time(const Shape& s, const TileCost& t, int64_t split) {
   return split > 1 ? t.join + t.part * split + 8.0 * tiles_of(s, t) * split * rows * t.cols * (s.gated ? 2 : 1) / kBytesPerUs : 0.0;
 }
 
-// Time of the tiles' items: whole rounds of the chip's slots, then the rest, but no less than the operands' traffic.
+// Time of the tiles' items, whole rounds of the chip's slots, then the rest, and
+// of the operands' traffic; where both are alike they hold each other up.  (24
+// rows of 14336 by 14336 x 4096 in 64 tiles, two to six parts of K: 40, 30, 27, 37
+// and 33 us; the estimates 36, 30, 28, 33 and 30.)
 inline double product_time(const Shape& s, const TileCost& t, int64_t split, int num_cus) {
   const int64_t items = tiles_of(s, t) * split, slots = (int64_t)num_cus * t.slots, per = (units_of(s) + split - 1) / split;
   const int64_t rest = items % slots;
   double time = (double)(items / slots) * (per * t.unit + t.item);
   if (rest) time += per * (rest <= num_cus ? t.alone : t.unit) + t.item;
   const double bytes = 2.0 * s.batches * ((double)s.M * s.K + (s.symmetric ? 0.0 : (double)s.N * s.K * (s.gated ? 2 : 1)));
-  if (time < bytes / kBytesPerUs + t.item) time = bytes / kBytesPerUs + t.item;
-  return time + join_time(s, t, split);
+  const double stream = bytes / kStreamPerUs + t.item;
+  return std::cbrt(time * time * time + stream * stream * stream) + join_time(s, t, split);
 }
 
 // The tile and split of one product: the least of the estimates.  (Splitting
@@ -870,7 +881,8 @@ inline Choice choose(const Shape& s, const SplitSpace& ws, int num_cus) {
   Choice best{TILE_64, 1};
   double least = 1e30;
   for (int tile = 0; tile < TILES; ++tile) {
-    const TileCost t = tile_cost(tile, s.gated);
+    TileCost t = tile_cost(tile, s.gated, s.M <= 64);
+    if (s.symmetric && tile == TILE_128) t.unit = 1.0, t.alone = 0.6;  // K is contiguous on both sides
     const int64_t units = units_of(s), room = split_room(s, t, ws), most = units < kMaxSplit ? units : kMaxSplit;
     for (int64_t split = 1; split <= most && split <= room; ++split) {
       const double time = product_time(s, t, split, num_cus);
@@ -892,7 +904,7 @@ int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&
   for (int tile = 0; tile < TILES; ++tile) {
     int parts[N];
     double work = 0.0;
-    const TileCost t = tile_cost(tile, false);
+    const TileCost t = tile_cost(tile, false, false);
     int64_t items = 0;
     for (int i = 0; i < N; ++i) {
       items += tiles_of(s[i], t);
