@@ -22,7 +22,7 @@
 // Many rows are bound by the matrix cores, few by the stream of weights.  SwiGLU,
 // H = 4096, F = 14336, us: 2048 rows forward 390 + 192 (1.23 and 1.25 PFLOP/s),
 // backward 248 + 866 (0.97, with 190 MB of P, dP and transposes moved in its
-// epilogue, and 1.39); 24 rows forward 48 + 31 (4.9 and 3.8 TB/s of weights).
+// epilogue, and 1.39); 24 rows forward 48 + 27 (4.9 and 4.3 TB/s of weights).
 #include <climits>
 #include <new>
 
