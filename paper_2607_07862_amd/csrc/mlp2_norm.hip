@@ -479,7 +479,9 @@ mlp2_norm_t mlp2_norm_plan(int64_t max_rows, int64_t H, int x_dtype, int y_dtype
   p->num_cus = cus;
   p->max_parts = cus;  // one backward work-group per CU
   const size_t bytes = (size_t)p->max_parts * 2 * part_pitch((int)H) * sizeof(float);
-  if (hipMalloc((void**)&p->part, bytes + sizeof(uint32_t)) != hipSuccess || hipMemset((char*)p->part + bytes, 0, sizeof(uint32_t)) != hipSuccess) {
+  if (hipMalloc((void**)&p->part, bytes + sizeof(uint32_t)) != hipSuccess ||
+      hipMemset((char*)p->part + bytes, 0, sizeof(uint32_t)) != hipSuccess ||
+      hipStreamSynchronize(nullptr) != hipSuccess) {  // calls may come on any stream
     (void)hipGetLastError();
     (void)hipFree(p->part);
     delete p;

@@ -358,7 +358,8 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   const int64_t floats = split_floats(p->n, p->m, count), parts = floats * 4, counters = kSplitCounters * kLine * 4;
   const int64_t fixed = 4 * x + 2 * a + part + diag;
   if (hipMalloc((void**)&p->ws, (size_t)(fixed + parts + counters)) != hipSuccess ||
-      hipMemset(p->ws + fixed + parts, 0, (size_t)counters) != hipSuccess) {
+      hipMemset(p->ws + fixed + parts, 0, (size_t)counters) != hipSuccess ||
+      hipStreamSynchronize(nullptr) != hipSuccess) {  // calls may come on any stream
     (void)hipGetLastError();
     (void)hipFree(p->ws);
     delete p;

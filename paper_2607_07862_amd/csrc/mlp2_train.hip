@@ -295,7 +295,8 @@ mlp2_train_t mlp2_train_plan(int64_t max_rows, int64_t H, int64_t F, int act, in
   const int64_t tall = padded > H ? (padded > F ? padded : F) : (H > F ? H : F);
   const int64_t floats = split_floats(tall, wide, 1), parts = floats * 4, counters = kSplitCounters * kLine * 4;
   if (hipMalloc((void**)&p->ws, (size_t)(z + dp + xt + parts + counters)) != hipSuccess ||
-      hipMemset(p->ws + z + dp + xt + parts, 0, (size_t)counters) != hipSuccess) {
+      hipMemset(p->ws + z + dp + xt + parts, 0, (size_t)counters) != hipSuccess ||
+      hipStreamSynchronize(nullptr) != hipSuccess) {  // calls may come on any stream
     (void)hipGetLastError();
     (void)hipFree(p->ws);
     delete p;
