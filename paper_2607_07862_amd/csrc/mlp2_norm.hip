@@ -216,14 +216,20 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
       float w[8];
       if constexpr (!AHEAD) weights(c, w);
       now.x[c].values(xh[c]);
-      now.d[c].values(g[c]);  // zeros past the row: so are all sums there
-      if (!live) {
+      now.d[c].values(g[c]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) xh[c][i] = g[c][i] = 0.f;
+      for (int i = 0; i < 8; ++i) xh[c][i] = (xh[c][i] - mean) * rstd;
+      // Where there is no element xhat is 0, not (0 - mean) rstd: that may be infinite, and its product with a dy of 0 a NaN.
+      const int n = live ? a.H - 8 * (t + NT * c) : 0;
+      if (n < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          xh[c][i] = i < n ? xh[c][i] : 0.f;
+          g[c][i] = i < n ? g[c][i] : 0.f;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        xh[c][i] = (xh[c][i] - mean) * rstd;
         if constexpr (!IN_LDS) {
           dw[c][i] += g[c][i] * xh[c][i];
           db[c][i] += g[c][i];
