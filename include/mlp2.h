@@ -435,7 +435,7 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
  * keep X's singular values below 4 (the usual ones stay below 1.3): beyond
  * that the fp16 intermediates overflow to infinity and the result is NaN.  A
  * zero matrix gives zeros (with eps > 0); a NaN or infinity in G gives NaN.
- * |G|_F^2 is summed in fp32: from |G|_F = 1.8e19 on, a finite G gives zeros. */
+ * |G|_F may lie anywhere in fp32's range or past it. */
 int mlp2_ortho_run(mlp2_ortho_t plan, const void* G, void* O, int steps, const float* coeffs, float eps, void* stream);
 
 /* Free the plan and its workspace (synchronises the device first).  NULL-safe. */

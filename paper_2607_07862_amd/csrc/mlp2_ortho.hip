@@ -76,28 +76,29 @@ __device__ __forceinline__ void store_split(uint16_t* hi, uint16_t* lo, const fl
   *reinterpret_cast<u32x4*>(lo) = pack_f16x8(rest);
 }
 
-__device__ __forceinline__ float block_sum(float v, float* buf) {
+__device__ __forceinline__ double block_sum(double v, double* buf) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
   if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = 0.f;
+  v = 0.;
   for (int w = 0; w < (int)blockDim.x / 64; ++w) v += buf[w];
   return v;
 }
 
-// part[matrix][blockIdx.x]: sums of squares of a slice of the matrix.  Bound by the read: fp32 2 x 4096 x 14336 103 us (4.6 TB/s).
+// part[matrix][blockIdx.x]: sums of squares of a slice of the matrix, in 64 bits, which hold the square of any fp32 (in 32 bits
+// norms from 1.8e19 on and below about 1e-19 were lost).  Bound by the read: fp32 2 x 4096 x 14336 103 us (4.6 TB/s).
 template <class T>
-__global__ __launch_bounds__(1024) void k_ortho_squares(const T* G, int64_t n, float* part) {
-  __shared__ float buf[16];
+__global__ __launch_bounds__(1024) void k_ortho_squares(const T* G, int64_t n, double* part) {
+  __shared__ double buf[16];
   const T* g = G + (int64_t)blockIdx.y * n;
-  float s = 0.f;
+  double s = 0.;
 #pragma unroll 2
   for (int64_t i = ((int64_t)blockIdx.x * 1024 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 8192) {
     float v[8];
     load8(g + i, (int)min(n - i, (int64_t)8), v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += v[e] * v[e];
+    for (int e = 0; e < 8; ++e) s += (double)v[e] * (double)v[e];
   }
   s = block_sum(s, buf);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * kOrthoParts + blockIdx.x] = s;
@@ -106,13 +107,15 @@ __global__ __launch_bounds__(1024) void k_ortho_squares(const T* G, int64_t n, f
 // The first X [n][m] (n <= m, padded to 64): G, transposed if it is tall, scaled, zeros in the padding.  One 64 x 64 block a work-group.
 // Bound by memory traffic: fp32 2 x 4096 x 14336 163 us (5.8 TB/s), 14336 x 4096, through LDS, 90 us (5.2).
 template <class T, bool TALL>
-__global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int cols, int n, int m, const float* part, int parts,
+__global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int cols, int n, int m, const double* part, int parts,
                                                      float eps, float scale, uint16_t* hi, uint16_t* lo) {
-  __shared__ float buf[4];
+  __shared__ double buf[4];
   __shared__ float block[64][65];
-  const float* mine = part + (int64_t)blockIdx.y * kOrthoParts;
-  const float norm = sqrtf(block_sum((int)threadIdx.x < parts ? mine[threadIdx.x] : 0.f, buf));
-  const float by = scale / (norm + eps);
+  const double* mine = part + (int64_t)blockIdx.y * kOrthoParts;
+  // |G| + eps is down * [1, 2): neither it nor its reciprocal need be an fp32 number, so G is scaled by 1 / down and by the rest.
+  const double norm = sqrt(block_sum((int)threadIdx.x < parts ? mine[threadIdx.x] : 0., buf)) + (double)eps;
+  const int down = norm > 0. && norm < INFINITY ? ilogb(norm) : 0;
+  const float by = scale / (float)ldexp(norm, -down);
   const T* g = G + (int64_t)blockIdx.y * rows * cols;
   const int64_t base = (int64_t)blockIdx.y * n * m;
   const int across = m / 64, i0 = blockIdx.x / across * 64, j0 = blockIdx.x % across * 64;  // of X
@@ -134,7 +137,7 @@ __global__ __launch_bounds__(256) void k_ortho_scale(const T* G, int rows, int c
   for (int h = 0; h < 2; ++h) {
     const int r = threadIdx.x / 8 + 32 * h, c = threadIdx.x % 8 * 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[h][e] = (TALL ? block[r][c + e] : v[h][e]) * by;
+    for (int e = 0; e < 8; ++e) v[h][e] = ldexpf(TALL ? block[r][c + e] : v[h][e], -down) * by;
     const int64_t at = base + (int64_t)(i0 + r) * m + j0 + c;
     store_split(hi + at, lo + at, v[h]);
   }
@@ -273,7 +276,8 @@ struct mlp2_ortho_s {
   char* ws = nullptr;
   uint16_t* X[2][2] = {};  // [buffer][upper, lower]: [count][n][m]
   uint16_t *A = nullptr, *B = nullptr;  // [count][n][n]
-  float *part = nullptr, *diag = nullptr;
+  double* part = nullptr;
+  float* diag = nullptr;
   SplitSpace split{};
 };
 
@@ -354,7 +358,7 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   p->num_cus = cus;
   p->scale = std::exp2(std::round(0.5f * std::log2((float)(rows > cols ? rows : cols))));
   const int64_t x = round_up(count * p->n * p->m * 2, 256), a = round_up(count * p->n * p->n * 2, 256);
-  const int64_t part = round_up(count * kOrthoParts * 4, 256), diag = round_up(count * p->n * 4, 256);
+  const int64_t part = round_up(count * kOrthoParts * 8, 256), diag = round_up(count * p->n * 4, 256);
   const int64_t floats = split_floats(p->n, p->m, count), parts = floats * 4, counters = kSplitCounters * kLine * 4;
   const int64_t fixed = 4 * x + 2 * a + part + diag;
   if (hipMalloc((void**)&p->ws, (size_t)(fixed + parts + counters)) != hipSuccess ||
@@ -370,7 +374,7 @@ mlp2_ortho_t mlp2_ortho_plan(int64_t count, int64_t rows, int64_t cols, int dtyp
   for (int i = 0; i < 4; ++i, at += x) p->X[i / 2][i % 2] = (uint16_t*)at;
   p->A = (uint16_t*)at;
   p->B = (uint16_t*)(at + a);
-  p->part = (float*)(at + 2 * a);
+  p->part = (double*)(at + 2 * a);
   p->diag = (float*)(at + 2 * a + part);
   p->split = SplitSpace{(float*)(p->ws + fixed), floats, (uint32_t*)(p->ws + fixed + parts), kSplitCounters};
   return p;
