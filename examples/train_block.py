@@ -51,7 +51,8 @@ class Block:
         for W, w, m, d, o, plan in ((self.W1, self.w1, self.m1, self.d1, self.o1, self.ortho1), (self.W2, self.w2, self.m2, self.d2, self.o2, self.ortho2)):
             m.mul_(momentum).add_(d)
             plan.run(m, o)
-            W.add_(o, alpha=-rate * max(1.0, W.shape[-2] / W.shape[-1]) ** 0.5)
+            fan_in, fan_out = W.shape[-2:]  # rows times W
+            W.add_(o, alpha=-rate * max(1.0, fan_out / fan_in) ** 0.5)
             w.copy_(W)
         self.weight.add_(self.dw, alpha=-rate)
         self.bias.add_(self.db, alpha=-rate)
