@@ -408,7 +408,8 @@ mlp2_norm_t mlp2_norm_plan(int64_t max_rows, int64_t H, int x_dtype, int y_dtype
 
 /* Y = (X - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps), eps >= 0.
  * ldx and ldy (>= H) are the rows' strides in elements; rows may start at any
- * element.  weight (NULL: ones) and bias (NULL: zeros) hold H values; mean and
+ * element, and matrices whose strides are as many bytes may lie in the columns
+ * of one buffer.  weight (NULL: ones) and bias (NULL: zeros) hold H values; mean and
  * rstd receive M values each for the backward pass, or are NULL. */
 int mlp2_norm_forward(mlp2_norm_t plan, int64_t M, const void* X, int64_t ldx, const float* weight, const float* bias, float eps,
                       void* Y, int64_t ldy, float* mean, float* rstd, void* stream);

@@ -537,7 +537,7 @@ class NormPlan(_Owned):
 
     ``x_dtype`` is the type of ``X`` and ``dX``, ``y_dtype`` (default: the same)
     that of ``Y`` and ``dY``; everything else is float32.  Matrices may have any
-    row stride.
+    row stride, and may be columns of one buffer.
     """
 
     _name = "norm"

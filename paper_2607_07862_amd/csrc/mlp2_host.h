@@ -28,14 +28,24 @@ inline bool on_device(int device) {
   return hipGetDevice(&dev) == hipSuccess && dev == device;
 }
 
+// An operand's bytes: `rows` rows of `width` at a distance of `pitch`; one row is a plain range.
 struct Span {
   const void* p;
-  int64_t bytes;
+  int64_t width;
+  int64_t rows = 1, pitch = 0;
+  int64_t bytes() const { return rows > 0 && width > 0 ? (rows - 1) * pitch + width : 0; }
 };
 
+// Whether two operands share a byte.  Rows of the same pitch may lie beside each other (columns of one buffer, rows in turn);
+// of other shapes the whole ranges are compared, gaps between rows included.
 inline bool overlap(const Span& a, const Span& b) {
   const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
+  if (!a.p || !b.p || !a.bytes() || !b.bytes() || x >= y + (uint64_t)b.bytes() || y >= x + (uint64_t)a.bytes()) return false;
+  if (a.rows == 1 || b.rows == 1 || a.pitch != b.pitch) return true;
+  if (x > y) return overlap(b, a);
+  // Row j of b starts `in` bytes into the pitch of row j + k of a.
+  const int64_t k = (int64_t)((y - x) / (uint64_t)a.pitch), in = (int64_t)((y - x) % (uint64_t)a.pitch);
+  return (in < a.width && k < a.rows) || (in + b.width > a.pitch && k + 1 < a.rows);
 }
 
 // Whether any of the outputs overlaps an input or another output.

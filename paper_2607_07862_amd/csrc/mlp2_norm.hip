@@ -447,8 +447,7 @@ hipError_t launch_norm(const mlp2_norm_s* p, bool forward, const NormArgs& a, in
 
 int64_t size_of(int dtype) { return dtype == MLP2_DTYPE_BF16 ? 2 : 4; }
 
-// Bytes from a matrix's first element to its last.
-int64_t extent(int64_t M, int64_t H, int64_t ld, int dtype) { return M > 0 ? ((M - 1) * ld + H) * size_of(dtype) : 0; }
+Span matrix(const void* p, int64_t M, int64_t H, int64_t ld, int dtype) { return {p, H * size_of(dtype), M, ld * size_of(dtype)}; }
 
 bool aligned(const void* p, int64_t a) { return (uintptr_t)p % (uint64_t)a == 0; }
 
@@ -506,8 +505,8 @@ int mlp2_norm_forward(mlp2_norm_t p, int64_t M, const void* X, int64_t ldx, cons
   if (!aligned(X, size_of(p->x)) || !aligned(Y, size_of(p->y)) || !aligned(weight, 4) || !aligned(bias, 4) || !aligned(mean, 4) ||
       !aligned(rstd, 4))
     return record_error(MLP2_ERR_ALIGNMENT);
-  const Span in[] = {{X, extent(M, p->H, ldx, p->x)}, {weight, p->H * 4}, {bias, p->H * 4}};
-  const Span out[] = {{Y, extent(M, p->H, ldy, p->y)}, {mean, M * 4}, {rstd, M * 4}};
+  const Span in[] = {matrix(X, M, p->H, ldx, p->x), {weight, p->H * 4}, {bias, p->H * 4}};
+  const Span out[] = {matrix(Y, M, p->H, ldy, p->y), {mean, M * 4}, {rstd, M * 4}};
   if (outputs_overlap(in, out)) return record_error(MLP2_ERR_INVALID_ARG);
   if (!on_device(p->device)) return record_error(MLP2_ERR_DEVICE);
   NormArgs a{};
@@ -535,8 +534,8 @@ int mlp2_norm_backward(mlp2_norm_t p, int64_t M, const void* dY, int64_t lddy, c
   if (!aligned(dY, size_of(p->y)) || !aligned(X, size_of(p->x)) || !aligned(dX, size_of(p->x)) || !aligned(weight, 4) ||
       !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
     return record_error(MLP2_ERR_ALIGNMENT);
-  const Span in[] = {{dY, extent(M, p->H, lddy, p->y)}, {X, extent(M, p->H, ldx, p->x)}, {weight, p->H * 4}, {mean, M * 4}, {rstd, M * 4}};
-  const Span out[] = {{dX, extent(M, p->H, lddx, p->x)}, {dweight, p->H * 4}, {dbias, p->H * 4}};
+  const Span in[] = {matrix(dY, M, p->H, lddy, p->y), matrix(X, M, p->H, ldx, p->x), {weight, p->H * 4}, {mean, M * 4}, {rstd, M * 4}};
+  const Span out[] = {matrix(dX, M, p->H, lddx, p->x), {dweight, p->H * 4}, {dbias, p->H * 4}};
   if (outputs_overlap(in, out)) return record_error(MLP2_ERR_INVALID_ARG);
   if (!on_device(p->device)) return record_error(MLP2_ERR_DEVICE);
   hipStream_t s = (hipStream_t)stream;
