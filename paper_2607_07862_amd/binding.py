@@ -528,6 +528,8 @@ class TrainPlan(_Owned):
                                (dX, "dX", (M, H)), (dW1, "dW1", (H, F)), (dW2, "dW2", (F, H))):
             if t is not None or not name.startswith(("dX", "dW")):
                 self._check(t, name, *shape)
+        if M == 0 and dX is not None and dW1 is None and dW2 is None:
+            return  # (an empty tensor's pointer is null, which the library takes for a gradient that is not asked for)
         self._done(self.lib.mlp2_train_backward(self.handle, M, _ptr(dY), _ptr(X), _ptr(W1), _ptr(W2), _ptr(P), _ptr(dX),
                                                 _ptr(dW1), _ptr(dW2), self._on(stream)), "backward")
 
