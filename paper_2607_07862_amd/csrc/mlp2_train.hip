@@ -138,13 +138,25 @@ struct Transpose {
   uint16_t* Xt;
   int64_t H;
   int M, rows;
-  __host__ __device__ int items() const { return Xt ? (int)(H / 64) * (rows / 64) : 0; }
-  // Item: one 64 x 64 block, through LDS.
+  __host__ __device__ int blocks() const { return Xt ? (int)(H / 64) * (rows / 64) : 0; }
+  // Blocks of an item: one, but for the largest X, since a launch holds fewer than 2^32 work-items (1048576 rows of 32768).
+  __host__ __device__ int each() const { return blocks() / kMostItems + 1; }
+  __host__ __device__ int items() const { return (blocks() + each() - 1) / each(); }
+  static constexpr int kMostItems = 1 << 21;
   template <int THREADS>
   __device__ __forceinline__ void run(int item, char* lds) const {
+    const int n = each(), end = min((item + 1) * n, blocks());
+    for (int block = item * n; block < end; ++block) {
+      if (block > item * n) __syncthreads();  // the block ahead has left the LDS
+      move<THREADS>(block, lds);
+    }
+  }
+  // One 64 x 64 block, through LDS.
+  template <int THREADS>
+  __device__ __forceinline__ void move(int block, char* lds) const {
     constexpr int PITCH = 64 + 8;  // elements
     uint16_t* t = reinterpret_cast<uint16_t*>(lds);
-    const int across = (int)(H / 64), h0 = item % across * 64, m0 = item / across * 64;
+    const int across = (int)(H / 64), h0 = block % across * 64, m0 = block / across * 64;
     static_assert(512 % THREADS == 0, "whole rounds");
 #pragma unroll
     for (int j = 0; j < 512 / THREADS; ++j) {
