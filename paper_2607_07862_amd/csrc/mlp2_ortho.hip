@@ -292,20 +292,20 @@ hipError_t ortho_step(const mlp2_ortho_s* p, const float* coeff, bool apart, int
   x.batch = n * m;
   sq.batch = n * n;
   const StoreGram gram{p->A, (int)n, (int)n, kOrthoScaleA / (p->scale * p->scale)};
-  hipError_t e = product<Fp16, false, false>(x, x, n, n, m, count, gram, p->split, p->num_cus, s);
+  hipError_t e = product<Fp16, false>(x, x, n, n, m, count, gram, p->split, p->num_cus, s);
   if (e != hipSuccess) return e;
   const StorePoly poly{p->A, p->B, p->diag, (int)n, (int)n, coeff[1] * kOrthoScaleB / kOrthoScaleA,
                        coeff[2] * kOrthoScaleB / (kOrthoScaleA * kOrthoScaleA), apart ? 1 : 0};
-  e = product<Fp16, false, false>(sq, sq, n, n, n, count, poly, p->split, p->num_cus, s);
+  e = product<Fp16, false>(sq, sq, n, n, n, count, poly, p->split, p->num_cus, s);
   if (e != hipSuccess) return e;
   sq.p = p->B;
   const Update update{X[0], last ? nullptr : X[1], p->diag, n, m, coeff[0], 1.f / kOrthoScaleB};
-  if (!last) return product<Fp16, false, true>(sq, x, n, m, n, count, StoreUpdate{update, out[0], left == 1 ? nullptr : out[1]}, p->split, p->num_cus, s);
+  if (!last) return product<Fp16, true>(sq, x, n, m, n, count, StoreUpdate{update, out[0], left == 1 ? nullptr : out[1]}, p->split, p->num_cus, s);
   const int rows = (int)p->rows, cols = (int)p->cols;
   if (p->tall)
-    return product<Fp16, false, true>(sq, x, n, m, n, count, StoreLast<true>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
+    return product<Fp16, true>(sq, x, n, m, n, count, StoreLast<true>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
                                       p->split, p->num_cus, s);
-  return product<Fp16, false, true>(sq, x, n, m, n, count, StoreLast<false>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
+  return product<Fp16, true>(sq, x, n, m, n, count, StoreLast<false>{update, (uint16_t*)O, rows, cols, (int)n, 1.f / p->scale},
                                     p->split, p->num_cus, s);
 }
 

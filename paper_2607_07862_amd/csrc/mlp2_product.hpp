@@ -1,11 +1,11 @@
 // Tile products of the training operators: C[m][n] = sum over k of R(m, k) C(n, k)
-// for operands of either storage order, with a fused epilogue.
+// for column operands of either storage order, with a fused epilogue.
 //
 // The forward kernels of the library multiply activations [M, K] by weights
-// [K, N].  Training needs every other order too: dZ = dY W2^T reads weights
-// whose K is contiguous, dW = X^T dP reads both operands with K as the slow
-// index.  Here each side of the product is staged through LDS in panels of
-// its own order:
+// [K, N].  Training needs other orders too: dZ = dY W2^T reads weights whose K
+// is contiguous, dW = X^T dP has K as the slow index of both operands, of which
+// the row side is transposed beforehand.  Here the column side is staged
+// through LDS in panels of its own order, the row side in inner ones:
 //
 //   inner panel (K contiguous in memory): [rows][k], read
 //     by ds_read_b128 (8 consecutive k per lane);
@@ -58,12 +58,13 @@ struct Side {
 };
 
 // A work-group tile: ROWP row panels of ER rows and COLP column panels of EC
-// columns, WM x WN waves, an NS-deep ring of BK-deep stages.  Every wave owns
+// columns, WM x WN waves, a ring of NS stages, each BK deep.  Every wave owns
 // 32 columns of every column panel (so that the two panels of a gated product,
 // gate and up weights, meet in one lane) and 16 * TM rows.
-template <int ER_, int ROWP_, int EC_, int COLP_, int WM_, int WN_, int BK_, int NS_>
+template <int ER_, int ROWP_, int EC_, int COLP_, int WM_, int WN_, int NS_>
 struct PTile {
-  static constexpr int ER = ER_, ROWP = ROWP_, EC = EC_, COLP = COLP_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
+  static constexpr int ER = ER_, ROWP = ROWP_, EC = EC_, COLP = COLP_, WM = WM_, WN = WN_, NS = NS_;
+  static constexpr int BK = 64;
   static constexpr int NWAVES = WM * WN, THREADS = 64 * NWAVES;
   static constexpr int BM = ER * ROWP, BN = EC * COLP;
   static constexpr int TM = BM / WM / 16;             // 16-row blocks of a wave
@@ -72,7 +73,6 @@ struct PTile {
   static constexpr int STAGE = ROWP * RPANEL + COLP * CPANEL;
   static constexpr int LOADS = STAGE / 1024 / NWAVES;  // 1 KB loads per wave and stage
   static constexpr int LDS = NS * STAGE;
-  static_assert(BK == 32 || BK == 64, "stage depth");
   static_assert(EC == 32 * WN, "a wave owns 32 columns of every column panel");
   static_assert(RPANEL % (1024 * NWAVES) == 0 && CPANEL % (1024 * NWAVES) == 0, "every wave loads whole 1 KB pieces");
   // Wave wm's row block tm: in the quadrant tile its rows lie in both halves, elsewhere together.
@@ -81,10 +81,10 @@ struct PTile {
     return QUAD ? 64 * wm + 16 * (tm & 3) + 128 * (tm >> 2) : wm * (BM / WM) + 16 * tm;
   }
 };
-using Tile64 = PTile<64, 1, 64, 1, 2, 2, 64, 4>;    // 64 x 64
-using Tile64G = PTile<64, 1, 64, 2, 2, 2, 64, 3>;   // 64 x (64 + 64): gated
-using Tile128 = PTile<64, 2, 64, 2, 2, 2, 64, 2>;   // 128 x 128, gated 128 x (64 + 64)
-using Tile256 = PTile<128, 2, 128, 2, 2, 4, 64, 2>;  // 256 x 256, gated 256 x (128 + 128): the ping-pong loop
+using Tile64 = PTile<64, 1, 64, 1, 2, 2, 4>;    // 64 x 64
+using Tile64G = PTile<64, 1, 64, 2, 2, 2, 3>;   // 64 x (64 + 64): gated
+using Tile128 = PTile<64, 2, 64, 2, 2, 2, 2>;   // 128 x 128, gated 128 x (64 + 64)
+using Tile256 = PTile<128, 2, 128, 2, 2, 4, 2>;  // 256 x 256, gated 256 x (128 + 128): the ping-pong loop
 
 // ------------------------------------------------------------------ panel loads
 
@@ -98,13 +98,10 @@ __device__ __forceinline__ void dma16_buffer(u32x4 rsrc, uint32_t voff, uint32_t
   asm volatile("s_nop %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds_addr), "n"(STATES - 1) : "memory");
 }
 
-// The chunk swizzle of a panel's row.  Inner: rows of BK / 8 chunks, so that
-// the 16 rows of one ds_read_b128 group lie in different banks.  Outer: k rows
+// The chunk swizzle of a panel's row.  Inner: rows of 8 chunks, so that the 16
+// rows of one ds_read_b128 group lie in different banks.  Outer: k rows
 // of E / 8 chunks, so that the 4 k rows of one ds_read_b64_tr_b16 group do.
-template <int BK>
-__device__ __forceinline__ int swz_inner(int row) {
-  return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
-}
+__device__ __forceinline__ int swz_inner(int row) { return (row >> 1) & 7; }
 template <int E>
 __device__ __forceinline__ int swz_outer(int k) {
   return E == 128 ? (4 * (k & 3)) ^ (2 * ((k >> 3) & 1)) : (4 * ((k >> 1) & 1)) ^ (2 * ((k >> 3) & 1));
@@ -127,6 +124,7 @@ struct PanelLoad {
   static constexpr int E = COL ? T::EC : T::ER, BK = T::BK, BYTES = COL ? T::CPANEL : T::RPANEL;
   static constexpr int PIECES = BYTES / 1024 / T::NWAVES;
   static_assert(!JUMP || !OUTER, "a second matrix along K is inner");
+  static_assert(!OUTER || COL, "K is contiguous on the row side");
   const char* base;
   uint32_t range, tail;  // of every stage; outer: of the last stage
   uint32_t step;
@@ -166,13 +164,13 @@ struct PanelLoad {
       range = clamp((s.batch ? (batch + 1) * s.batch * 2 : s.bytes) - 2 * rows);
       if constexpr (JUMP) {
         jump = s.jump * 2;
-        left = s.jump_at * (64 / BK) - stage0;
+        left = s.jump_at - stage0;
         if (left <= 0) base += jump;
       }
       constexpr int CPR = BK / 8, RPP = 64 / CPR;  // chunks per row, rows per piece
       const int row = RPP * wave + lane / CPR;
       static_assert(T::NWAVES * RPP % 32 == 0, "so do swizzle and permutation");
-      const int chunk = (lane % CPR) ^ swz_inner<BK>(row);
+      const int chunk = (lane % CPR) ^ swz_inner(row);
       const int i = row & 15;
       const int at = COL ? (row & ~31) + 8 * (i >> 2) + 4 * ((row >> 4) & 1) + (i & 3) : row;
       piece_step = (uint32_t)(T::NWAVES * RPP * s.ld * 2);
@@ -208,36 +206,25 @@ __device__ __forceinline__ u32x4 read_tr(const char* p, int upper) {
 }
 
 // Row side: lane holds row (lane % 16) of a 16-row block, k = 8 (lane / 16) .. + 7 of a 32-deep slice.
-template <class T, bool OUTER>
+template <class T>
 struct RowFrag {
   static constexpr int E = T::ER;
-  uint32_t off[T::KS];  // inner: one per K slice; outer: the first
+  uint32_t off[T::KS];  // one per K slice
   __device__ __forceinline__ RowFrag(int wm) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63;
     const int first = T::row_of(wm, 0), r0 = first % E;
     const uint32_t panel = (uint32_t)(first / E * T::RPANEL);
-    if constexpr (OUTER) {
-      // lane 4 r + c of group g addresses k row 8 g + r, columns 4 c .. + 3 of the block
-      const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), c = lane & 3;
-      off[0] = panel + (uint32_t)(k * (2 * E) + ((((r0 >> 3) + (c >> 1)) ^ swz_outer<E>(k)) << 4) + 8 * (c & 1));
-    } else {
-      const int row = r0 + (lane & 15);
+    const int row = r0 + (lane & 15);
 #pragma unroll
-      for (int ks = 0; ks < T::KS; ++ks)
-        off[ks] = panel + (uint32_t)(row * (2 * T::BK) + (((4 * ks + (lane >> 4)) ^ swz_inner<T::BK>(row)) << 4));
-    }
+    for (int ks = 0; ks < T::KS; ++ks)
+      off[ks] = panel + (uint32_t)(row * (2 * T::BK) + (((4 * ks + (lane >> 4)) ^ swz_inner(row)) << 4));
   }
   // Block tm of K slice ks; `stage` is the address of the stage's row panels.
   __device__ __forceinline__ u32x4 read(const char* stage, int ks, int tm) const {
     const int half = T::QUAD ? tm >> 2 : 0, blk = T::QUAD ? tm & 3 : tm;
-    if constexpr (OUTER) {
-      // Block blk is 2 blk chunks further on; the swizzle touches chunk bits 1 to 3, so the offset is XORed, not added.
-      return read_tr(stage + half * T::RPANEL + (off[0] ^ (uint32_t)(32 * blk)) + ks * 64 * E, 8 * E);
-    } else {
-      return *reinterpret_cast<const u32x4*>(stage + half * T::RPANEL + off[ks] + blk * 32 * T::BK);
-    }
+    return *reinterpret_cast<const u32x4*>(stage + half * T::RPANEL + off[ks] + blk * 32 * T::BK);
   }
 };
 
@@ -258,7 +245,7 @@ struct ColFrag {
       const int row = 32 * wn + (lane & 15);
 #pragma unroll
       for (int ks = 0; ks < T::KS; ++ks)
-        off[ks] = (uint32_t)(row * (2 * T::BK) + (((4 * ks + (lane >> 4)) ^ swz_inner<T::BK>(row)) << 4));
+        off[ks] = (uint32_t)(row * (2 * T::BK) + (((4 * ks + (lane >> 4)) ^ swz_inner(row)) << 4));
     }
   }
   __device__ __forceinline__ u32x4 read(const char* panel, int ks, int i) const {
@@ -284,7 +271,7 @@ using Acc = f32x4[T::COLP][2][T::TM];
 // LDS bounds it: a 64 x 64 x 64 unit reads 32 KB of fragments and takes in 16
 // KB, 384 clocks at 128 bytes each, and measures 0.2 us on a CU of its own; twice
 // the stages gained nothing (the Gram matrices of 2 x 512 x 2048 9.8 -> 10.4 us).
-template <class T, class Elem, bool RO, bool CO, bool JUMP>
+template <class T, class Elem, bool CO, bool JUMP>
 __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
                                              Acc<T>& acc, char* lds) {
   const int wave = uniform((int)threadIdx.x >> 6);
@@ -298,7 +285,7 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
   if (nk <= 0) return;
   const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
   constexpr int C0 = T::ROWP * T::RPANEL;  // the column panels of a stage
-  PanelLoad<T, RO, false, false> r0(rs, batch, m0, 0, st0, nk, 0), r1(rs, batch, m0, T::ROWP - 1, st0, nk, (T::ROWP - 1) * T::RPANEL);
+  PanelLoad<T, false, false, false> r0(rs, batch, m0, 0, st0, nk, 0), r1(rs, batch, m0, T::ROWP - 1, st0, nk, (T::ROWP - 1) * T::RPANEL);
   PanelLoad<T, CO, true, JUMP> c0(cs, batch, n0, 0, st0, nk, C0),
       c1(cs, batch, n0, T::COLP - 1, st0, nk, C0 + (T::COLP - 1) * T::CPANEL);
   uint32_t to = lds_base;  // the ring slot that is requested next
@@ -309,7 +296,7 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
     if constexpr (T::COLP == 2) c1.load(to);
     to = to == lds_base + (T::NS - 1) * T::STAGE ? lds_base : to + T::STAGE;
   };
-  const RowFrag<T, RO> rf(wm);
+  const RowFrag<T> rf(wm);
   const ColFrag<T, CO> cf(wn);
   struct Frags {
     u32x4 x[T::KS][T::TM], w[T::KS][T::COLP][2];
@@ -389,10 +376,11 @@ __device__ __forceinline__ void product_loop(const Side& rs, const Side& cs, int
 //   * Reuse: a panel read in memory slot p is complete in registers at product
 //     slot p (lgkmcnt(0)) and its ring slot is requested again in memory slot
 //     p + 2, after the barrier that ends the trailing waves' product slot p.
-// Here the two sides may have either storage order, and every panel carries
+// Here the column side may have either storage order, and every panel carries
 // its own 64-bit base and range.  8192 x 8192 x 8192 in bf16: K contiguous on both
-// sides 731 us (1.50 PFLOP/s), on the row side 749 (1.47), on neither 926 (1.19).
-template <class T, class Elem, bool RO, bool CO, bool JUMP>
+// sides 731 us (1.50 PFLOP/s), on the row side alone 749 (1.47).  (With outer
+// panels on both sides it took 926 (1.19), so no product has them.)
+template <class T, class Elem, bool CO, bool JUMP>
 __device__ __forceinline__ void product_pingpong(const Side& rs, const Side& cs, int64_t batch, int m0, int n0, int st0, int nk,
                                                  Acc<T>& acc, char* lds) {
   static_assert(T::ER == 128 && T::EC == 128 && T::ROWP == 2 && T::COLP == 2 && T::NWAVES == 8 && T::BK == 64 && T::NS == 2 && T::TM == 8, "256 x 256 tile");
@@ -408,13 +396,13 @@ __device__ __forceinline__ void product_pingpong(const Side& rs, const Side& cs,
   if (nk <= 0) return;
 
   const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-  PanelLoad<T, RO, false, false> pa[2] = {{rs, batch, m0, 0, st0, nk, 0}, {rs, batch, m0, 1, st0, nk, T::RPANEL}};
+  PanelLoad<T, false, false, false> pa[2] = {{rs, batch, m0, 0, st0, nk, 0}, {rs, batch, m0, 1, st0, nk, T::RPANEL}};
   PanelLoad<T, CO, true, JUMP> pb[2] = {{cs, batch, n0, 0, st0, nk, 2 * T::RPANEL},
                                         {cs, batch, n0, 1, st0, nk, 2 * T::RPANEL + T::CPANEL}};
   auto load_a = [&](int half, int st) { pa[half].load(lds_base + (uint32_t)(st & 1) * T::STAGE); };  // a panel's stages come in order
   auto load_b = [&](int half, int st) { pb[half].load(lds_base + (uint32_t)(st & 1) * T::STAGE); };
 
-  const RowFrag<T, RO> rf(wm);
+  const RowFrag<T> rf(wm);
   const ColFrag<T, CO> cf(wn);
   u32x4 xa[2][4], xb[2][4], w0[2][2], w1[2][2];
   auto read_a = [&](u32x4 (&x)[2][4], int half, int st) {
@@ -570,10 +558,10 @@ struct TileWalk {
 
 struct Nothing {};  // an epilogue's Read where it reads nothing
 
-// RO, CO: outer sides; JUMP: the column side runs on in a second matrix.
-template <bool RO_, bool CO_, class Epi_, bool JUMP_ = false>
+// CO: an outer column side; JUMP: the column side runs on in a second matrix.
+template <bool CO_, class Epi_, bool JUMP_ = false>
 struct Problem {
-  static constexpr bool RO = RO_, CO = CO_, JUMP = JUMP_;
+  static constexpr bool CO = CO_, JUMP = JUMP_;
   using Epi = Epi_;
   Side r, c;
   int M, N;          // rows and columns of the result (of each matrix of a gated product)
@@ -683,15 +671,15 @@ __device__ __forceinline__ void run_product(const P& a, int item, int batch, cha
   using Epi = typename P::Epi;
   static_assert(!Epi::kSymmetric || (Epi::kMirror && T::BM == T::BN), "square tiles on the diagonal");
   constexpr int COLS = Epi::kGated ? T::EC : T::BN;  // result columns of a tile
-  constexpr int UNIT = 64 / T::BK;                   // stages of a unit of K
+  static_assert(T::BK == 64, "a stage is a unit of K");
   const int total = a.walk.total(), s = item / total, tile = item - s * total;
   int tm_, tn_;
   a.walk.at(tile, tm_, tn_);
   const int m0 = tm_ * T::BM, n0 = tn_ * COLS;
-  const int st0 = s * a.per * UNIT, nk = min(a.per * UNIT, a.nk * UNIT - st0);
+  const int st0 = s * a.per, nk = min(a.per, a.nk - st0);
   Acc<T> acc;
-  if constexpr (T::QUAD) product_pingpong<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
-  else product_loop<T, Elem, P::RO, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  if constexpr (T::QUAD) product_pingpong<T, Elem, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  else product_loop<T, Elem, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
   int go = 1;
   if (a.split > 1) go = join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, a.M - m0, lds);
   if (uniform(go) == 0) return;  // a scalar branch: barriers follow
@@ -991,13 +979,13 @@ auto with_tile(int tile, F&& f) {
 }
 
 // One product with the tile and split that suit it.
-template <class Elem, bool RO, bool CO, class Epi>
+template <class Elem, bool CO, class Epi>
 hipError_t product(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const Epi& epi, const SplitSpace& ws,
                    int num_cus, hipStream_t stream) {
   const Choice ch = choose({M, N, K, batches, Epi::kGated, Epi::kSymmetric}, ws, num_cus);
   return with_tile<Epi>(ch.tile, [&](auto tile) {
     using T = decltype(tile);
-    return launch_product<T, Elem>(make_problem<T, Problem<RO, CO, Epi>>(r, c, M, N, K, batches, epi, ch.split, ws), batches, stream);
+    return launch_product<T, Elem>(make_problem<T, Problem<CO, Epi>>(r, c, M, N, K, batches, epi, ch.split, ws), batches, stream);
   });
 }
 

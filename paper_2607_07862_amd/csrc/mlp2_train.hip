@@ -222,7 +222,7 @@ hipError_t forward_first(const mlp2_train_s* p, int64_t M, const void* X, const 
   const Side r = make_side(X, H, M * H * 2);
   Side c = make_side(W1, F, p->nb * H * F * 2);
   if (p->nb == 2) c.panel = H * F;
-  return product<Bf16, false, true>(r, c, M, F, H, 1, epi, p->split, p->num_cus, s);
+  return product<Bf16, true>(r, c, M, F, H, 1, epi, p->split, p->num_cus, s);
 }
 
 template <int ACT>
@@ -232,7 +232,7 @@ hipError_t backward_first(const mlp2_train_s* p, int64_t M, const void* dY, cons
   const Choice ch = choose({M, F, H, 1, false, false}, p->split, p->num_cus);
   return with_tile<StoreBackward<ACT>>(ch.tile, [&](auto tile) {
     using T = decltype(tile);
-    using Dz = Problem<false, false, StoreBackward<ACT>>;
+    using Dz = Problem<false, StoreBackward<ACT>>;
     const Dz a = make_problem<T, Dz>(make_side(dY, H, M * H * 2), make_side(W2, H, F * H * 2), M, F, H, 1, epi, ch.split,
                                  p->split);
     k_backward_first<T, Dz><<<a.items() + x.items(), T::THREADS, 0, s>>>(a, x);
@@ -242,8 +242,8 @@ hipError_t backward_first(const mlp2_train_s* p, int64_t M, const void* dY, cons
 
 // dX = sum dP_i W1_i^T, dW1 = X^T dP and dW2 = Z^T dY in one launch.
 hipError_t backward_second(const mlp2_train_s* p, int64_t M, const void* dY, const void* W1, void* dX, void* dW1, void* dW2, hipStream_t s) {
-  using Dx = Problem<false, false, StorePlain, true>;
-  using Dw = Problem<false, true, StorePlain>;
+  using Dx = Problem<false, StorePlain, true>;
+  using Dw = Problem<true, StorePlain>;
   const int64_t H = p->H, F = p->F, nb = p->nb, rows = round_up(M, 64);
   // A gradient that is not asked for has no rows, and so no items.
   const int64_t mx = dX ? M : 0, m1 = dW1 ? H : 0, m2 = dW2 ? F : 0;
@@ -338,7 +338,7 @@ int mlp2_train_forward(mlp2_train_t p, int64_t M, const void* X, const void* W1,
   else e = forward_first<ACT_IDENTITY>(p, M, X, W1, P, s);
   if (e != hipSuccess) return status(e);
   const void* Z = p->act == MLP2_ACT_IDENTITY ? P : p->Z;
-  return status(product<Bf16, false, true>(make_side(Z, F, M * F * 2), make_side(W2, H, F * H * 2), M, H, F, 1,
+  return status(product<Bf16, true>(make_side(Z, F, M * F * 2), make_side(W2, H, F * H * 2), M, H, F, 1,
                                            StorePlain{(uint16_t*)Y, H, 0, INT_MAX}, p->split, p->num_cus, s));
 }
 

@@ -34,12 +34,12 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 def short_name(n: str) -> str:
     """k_mlp2<Tile<BM, BN, WM, WN, NS[, BK[, NT]]>, NB, Tile<...>, HV, PHASE> -> phase and tile shape; the training
-    products (k_product<PTile<ER, ROWP, EC, COLP, WM, WN, BK, NS>, type, Problem<...>>) -> name, epilogue and tile."""
+    products (k_product<PTile<ER, ROWP, EC, COLP, WM, WN, NS>, type, Problem<...>>) -> name, epilogue and tile."""
     m = re.search(r"(k_products?|k_backward_first)<mlp2::PTile<([\d, ]+)>", n)
     if m:
         t = [int(x) for x in m.group(2).split(",")]
         store = [re.sub(r"<(\d+|true|false)>$", r" \1", x) for x in re.findall(r"mlp2::(Store\w+(?:<\w+>)?)", n.split("(")[0])]
-        return f"{m.group(1)} {' + '.join(store)} (tile {t[0] * t[1]} x {t[2] * t[3]}, stages {t[7]}, waves {t[4] * t[5]})"
+        return f"{m.group(1)} {' + '.join(store)} (tile {t[0] * t[1]} x {t[2] * t[3]}, stages {t[6]}, waves {t[4] * t[5]})"
     m = re.search(r"mlp2::(k_(?:norm|ortho)_\w+)(<[^>]*>)?", n)
     if m:
         return m.group(1) + (m.group(2) or "")
