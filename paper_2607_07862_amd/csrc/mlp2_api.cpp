@@ -67,7 +67,6 @@ int fail(int code) {
 
 namespace mlp2 {
 int record_error(int code) { return fail(code); }
-void clear_error() { g_last_error = MLP2_OK; }
 }  // namespace mlp2
 
 namespace {

@@ -11,7 +11,7 @@
 namespace mlp2 {
 
 int record_error(int code);   // sets mlp2_last_error() and returns the code (mlp2_api.cpp)
-void clear_error();
+inline void clear_error() { (void)record_error(MLP2_OK); }
 
 // The current device, if it is one the kernels are built for: MLP2_OK, MLP2_ERR_DEVICE or MLP2_ERR_HIP.
 inline int current_device(int* device, int* num_cus) {

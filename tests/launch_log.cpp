@@ -28,7 +28,6 @@ char* const kMemory = (char*)(1ull << 40);  // addresses that nothing reads
 
 namespace mlp2 {
 int record_error(int code) { return code; }
-void clear_error() {}
 }  // namespace mlp2
 
 extern "C" {
