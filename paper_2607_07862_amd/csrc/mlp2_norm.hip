@@ -172,8 +172,9 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
   struct Row {
     Piece<XT> x[C];
     Piece<YT> d[C];
-    float mean, rstd;
+    float mean = 0.f, rstd = 0.f;  // (0 in threads without columns)
   };
+  constexpr bool AHEAD = C == 1;
   auto request = [&](Row& r, int row) {
     const int64_t at = row < a.M ? row : a.M - 1;
 #pragma unroll
@@ -184,10 +185,11 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
         r.d[c].load((const YT*)a.dY + at * a.ldd + col, n);
       }
     }
-    r.mean = a.mean[at];
-    r.rstd = a.rstd[at];
+    if (!AHEAD || 8 * t < a.H) {
+      r.mean = a.mean[at];
+      r.rstd = a.rstd[at];
+    }
   };
-  constexpr bool AHEAD = C == 1;
   auto weights = [&](int c, float (&w)[8]) {
     const int col = 8 * (t + NT * c), n = a.H - col;
 #pragma unroll
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
     } else {
       request(now, row);
     }
-    const float mean = now.mean, rstd = now.rstd;
+    const float mean = live ? now.mean : 0.f, rstd = live ? now.rstd : 0.f;
     float xh[C][8], g[C][8], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -217,16 +219,17 @@ __global__ __launch_bounds__(kNormBlock) void k_norm_backward(const NormArgs a) 
       if constexpr (!AHEAD) weights(c, w);
       now.x[c].values(xh[c]);
       now.d[c].values(g[c]);
+      // Where there is no element xhat is 0, not (0 - mean) rstd: that may be infinite, and its product with a dy of 0 a NaN.
+      if (!live) {  // the last row again
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xh[c][i] = g[c][i] = 0.f;
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) xh[c][i] = (xh[c][i] - mean) * rstd;
-      // Where there is no element xhat is 0, not (0 - mean) rstd: that may be infinite, and its product with a dy of 0 a NaN.
-      const int n = live ? a.H - 8 * (t + NT * c) : 0;
-      if (n < 8) {
+      const int n = a.H - 8 * (t + NT * c);
+      if (n < 8 && (C > 1 || n > 0)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          xh[c][i] = i < n ? xh[c][i] : 0.f;
-          g[c][i] = i < n ? g[c][i] : 0.f;
-        }
+        for (int i = 0; i < 8; ++i) xh[c][i] = i < n ? xh[c][i] : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
