@@ -4,10 +4,10 @@
 //   dx = rstd (g - mean(g) - xhat mean(g xhat)),   g = dy w,  xhat = (x - mean) rstd
 //   dw = sum over rows of dy xhat,   db = sum over rows of dy
 //
-// Both directions are bound by memory traffic: bf16 8192 x 4096 takes 26 us
-// forward (5.1 TB/s; a large copy reaches 4.9) and 52 backward (3.9 TB/s, 5 us of
-// it in the second kernel), fp32 to bf16 16384 x 8192 146 (5.5 TB/s) and 256 us
-// (5.2).  Calls of a few rows are bound by their launch, 4 us.  A row is held in
+// Both directions are bound by memory traffic: bf16 8192 x 4096 takes 26 to 29 us
+// forward (4.7 to 5.1 TB/s; a large copy reaches 4.9) and 45 backward (4.5 TB/s, 5
+// us of it in the second kernel), fp32 to bf16 16384 x 8192 146 (5.5 TB/s) and 260
+// us (5.2), fp32 to fp32 194 and 312 (5.5 and 5.2).  Calls of a few rows are bound by their launch, 4 us.  A row is held in
 // registers by a group of 16 to 1024 threads (up to 16 elements a thread), so
 // each input is read once; the variance is taken around the mean in a second
 // pass over the registers.  The groups of a persistent grid walk the rows with

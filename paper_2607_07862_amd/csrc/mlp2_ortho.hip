@@ -8,12 +8,12 @@
 // (the fastest order).  A and B are symmetric: only their tiles on and above the
 // diagonal are computed, and stored twice.
 //
-// The matrix cores bound it: a step of 14336 x 4096 takes 250 us for A (136 tiles
+// The matrix cores bound it: a step of 14336 x 4096 takes 250 to 275 us for A (136 tiles
 // of 256 x 256 on 256 CUs; one part of K each, since three parts, 25 us shorter
-// alone, left the whole run where it was), 90 for B and 450 for X (1.07 PFLOP/s
+// alone, left the whole run where it was), 90 to 99 for B and 450 to 476 for X (1.07 PFLOP/s
 // with 470 MB of both halves of X read and written in its epilogue).  Small ones
-// are bound by the fixed costs of three launches a step: 2 x 512 x 2048 takes 8.6,
-// 5.9 and 9.7 us.
+// are bound by the fixed costs of three launches a step: 2 x 512 x 2048 takes 9.2,
+// 6.4 and 9.9 us.
 //
 // Every product runs on the matrix cores in fp16 with fp32 sums.  fp16 rather
 // than bf16 because the iteration lifts the small singular values by up to

@@ -885,6 +885,18 @@ inline Choice choose(const Shape& s, const SplitSpace& ws, int num_cus) {
 
 // One tile for products that share a launch, and the split of each: every
 // slot gets about the same work, so no item should last longer than that.
+// The weights of the terms below (three fifths of a share, three times the fixed
+// cost, half of a join, three tenths of the shorter time) were set by trying,
+// and the operands' stream is left out.  Against every tile with 1 to 32 parts
+// of dX (and 1, 2 and 4 of the weight gradients up to 1000 rows), us for whole
+// backward passes, the choice, the best, and the best of each other tile:
+//   64 x 512 x 2048 SwiGLU      17.4 (64, 3 parts)   15.2 (64, 8 parts)   128: 22.9   256: 36.8
+//   24 x 4096 x 14336 SwiGLU    185 (128, 5)         179 (256, 8)         64: 261     128: 184
+//   128 x 1024 x 4096 GELU      25.0 (64, 3)         24.4 (64, 2)         128: 28.1   256: 40.4
+//   300 x 2048 x 5440 SwiGLU    70-73 (128, 5)       65 (128, 4)          64: 87      256: 77
+//   777 x 2112 x 5440 GELU      108 (256, 3)         100 (128, 1)         64: 126     256: 107
+//   1500 x 2048 x 5632 SwiGLU   222 (256, 3)         218 (256, 4)         64: 315     128: 222
+//   2048 x 4096 x 14336 SwiGLU  1100 (256, 1)        1097 (the same)      64: 2040    128: 1415
 template <int N>
 int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&split)[N]) {
   int best = TILE_64;
