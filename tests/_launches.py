@@ -4,6 +4,7 @@ A launch is a ``Launch``: kernel, the tile's rows and columns (0 where it has no
 """
 from __future__ import annotations
 
+import atexit
 import functools
 import os
 import re
@@ -29,7 +30,9 @@ def program() -> str | None:
     """The built program, or None where there is no compiler."""
     if not os.path.exists(HIPCC) or not shutil.which("c++filt"):
         return None
-    to = os.path.join(tempfile.mkdtemp(prefix="mlp2_launches_"), "launch_log")
+    folder = tempfile.mkdtemp(prefix="mlp2_launches_")
+    atexit.register(shutil.rmtree, folder, ignore_errors=True)
+    to = os.path.join(folder, "launch_log")
     cmd = [HIPCC, "-x", "hip", "--offload-arch=gfx950", "--offload-host-only", "-no-hip-rt", "-std=c++17", "-O1",
            "-I" + os.path.join(ROOT, "paper_2607_07862_amd", "csrc"), "-I" + os.path.join(ROOT, "include"),
            os.path.join(ROOT, "tests", "launch_log.cpp"), "-o", to]
