@@ -65,7 +65,7 @@ extern "C" {
 typedef struct mlp2_plan_s* mlp2_plan_t; /* opaque; created by mlp2_plan, freed by mlp2_destroy */
 
 enum mlp2_act { MLP2_ACT_IDENTITY = 0, MLP2_ACT_GELU_TANH = 1, MLP2_ACT_SWIGLU = 2 };
-enum mlp2_dtype { MLP2_DTYPE_BF16 = 0, MLP2_DTYPE_F32 = 1 /* mlp2_norm_* and mlp2_ortho_* only */ };
+enum mlp2_dtype { MLP2_DTYPE_BF16 = 0, MLP2_DTYPE_F32 = 1 /* not for mlp2_plan, mlp2_chain_plan, mlp2_train_plan */ };
 /* MLP2_MODE_SENTINEL is the pipelined launch with the Lamport-style
  * synchronisation the paper discusses as an alternative (Sec. V-A): GEMM1
  * tiles store the intermediate at device scope with no fence and no ready
@@ -447,6 +447,45 @@ int mlp2_ortho_run(mlp2_ortho_t plan, const void* G, void* O, int steps, const f
 
 /* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
 void mlp2_ortho_destroy(mlp2_ortho_t plan);
+
+/* ---- MXFP4: matrices in 4 bits, and their products.
+ *
+ * A matrix [rows, K] in MXFP4 is two arrays.  `codes` [rows, Kp / 2]: Kp is K
+ * rounded up to a multiple of 128, elements 2 i and 2 i + 1 of a row are the low
+ * and the high half of byte i; bit 3 of a code is the sign, bits 0 .. 2 stand for
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6.  `scales` [Kp / 128, rows, 4]: byte b of group g and
+ * row r scales elements 128 g + 32 b .. + 31 of the row by 2^(byte - 127); 255
+ * stands for NaN.  Elements from K on have code 0 and scale 0.  `count` matrices lie one after
+ * the other in both arrays.  Both are 16-byte aligned. */
+typedef struct mlp2_mx_s* mlp2_mx_t;
+
+/* Quantise `count` matrices X [rows, cols] of `dtype` (bf16 or F32; rows ldx
+ * elements apart, matrices matrix_stride apart; any element's address) into
+ * MXFP4, blocks of 32 along a row (down = 0: matrices [rows, K = cols]) or down
+ * a column (down = 1: X is [K, N] as the library's weights are and becomes
+ * matrices [N = cols, K = rows]).  A block's scale is 2^(floor(log2 max|x|) - 2), at least 2^-127;
+ * codes are the nearest ones, ties to the even code, and 6 for what lies above; a
+ * NaN or an infinity makes its block NaN (codes 0, scale 255).  `values` (or
+ * NULL) receives what codes and scales stand for, bf16 [count, rows, cols] in
+ * X's order; they are bf16 numbers, so nothing is rounded again.
+ * 0 <= count <= 65536, 0 <= rows, cols <= 1<<20 (0: nothing to do), and at most 2^24 pieces of 32 x 128 (down: 512 bytes of columns by
+ * 256 rows).  The current device, no workspace. */
+int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const void* X, int dtype, int64_t ldx, int64_t matrix_stride,
+                     void* codes, void* scales, void* values, void* stream);
+
+/* Plan Y = act(A . W^T) for MXFP4 matrices A [M, K], M <= max_rows, and W [N, K]
+ * (SwiGLU: two, Wg then Wu: Y = silu(A . Wg^T) * (A . Wu^T)): 1 <= max_rows, N, K <=
+ * 1<<18, act in enum mlp2_act, y_dtype bf16 or F32.  Sums and activation are
+ * fp32.  The workspace holds up to 96 MB of partial sums.  NULL on failure
+ * (mlp2_last_error).  A plan's calls are ordered on one stream. */
+mlp2_mx_t mlp2_mx_plan(int64_t max_rows, int64_t N, int64_t K, int act, int y_dtype);
+
+/* Y [M, N], contiguous, at any element's address, fully overwritten.  0 <= M <=
+ * max_rows (0 does nothing).  Y must not overlap an input. */
+int mlp2_mx_product(mlp2_mx_t plan, int64_t M, const void* A, const void* A_scales, const void* W, const void* W_scales, void* Y, void* stream);
+
+/* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
+void mlp2_mx_destroy(mlp2_mx_t plan);
 
 #ifdef __cplusplus
 }

@@ -56,6 +56,10 @@ EXPORTS = (
     "mlp2_ortho_plan",
     "mlp2_ortho_run",
     "mlp2_ortho_destroy",
+    "mlp2_mx_quantize",
+    "mlp2_mx_plan",
+    "mlp2_mx_product",
+    "mlp2_mx_destroy",
 )
 
 
@@ -180,7 +184,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.mlp2_run_noalloc.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_int,
                                      P, P, P, P, P, ctypes.c_int]
     I64, F32 = ctypes.c_int64, ctypes.c_float
-    for name in ("train", "norm", "ortho"):
+    for name in ("train", "norm", "ortho", "mx"):
         getattr(lib, f"mlp2_{name}_plan").restype = P
         getattr(lib, f"mlp2_{name}_destroy").restype = None
         getattr(lib, f"mlp2_{name}_destroy").argtypes = [P]
@@ -197,6 +201,11 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.mlp2_ortho_plan.argtypes = [I64, I64, I64, ctypes.c_int]
     lib.mlp2_ortho_run.restype = ctypes.c_int
     lib.mlp2_ortho_run.argtypes = [P, P, P, ctypes.c_int, ctypes.POINTER(F32), F32, P]
+    lib.mlp2_mx_quantize.restype = ctypes.c_int
+    lib.mlp2_mx_quantize.argtypes = [I64, I64, I64, ctypes.c_int, P, ctypes.c_int, I64, I64, P, P, P, P]
+    lib.mlp2_mx_plan.argtypes = [I64, I64, I64, ctypes.c_int, ctypes.c_int]
+    lib.mlp2_mx_product.restype = ctypes.c_int
+    lib.mlp2_mx_product.argtypes = [P, I64] + [P] * 6
     _lib = lib
     return lib
 
@@ -615,3 +624,101 @@ class OrthoPlan(_Owned):
         arr = (ctypes.c_float * len(flat))(*flat)
         self._done(self.lib.mlp2_ortho_run(self.handle, _ptr(G), _ptr(O), int(steps), arr, float(eps),
                                            self._on(stream)), "run")
+
+
+def _mx_shapes(rows, K, count):
+    groups = -(-K // 128)
+    return (count, rows, 64 * groups), (count, groups, rows, 4)
+
+
+class MxMatrix:
+    """``count`` matrices ``[rows, K]`` in MXFP4, K contiguous, on the current device (uninitialised).
+
+    ``codes`` is uint8 ``[count, rows, Kp / 2]`` and ``scales`` uint8 ``[count, Kp / 128, rows, 4]``, Kp being K rounded up to a
+    multiple of 128 (the format: ``include/mlp2.h``).  ``mx_quantize`` fills them."""
+
+    def __init__(self, rows: int, K: int, count: int = 1):
+        import torch
+
+        self.rows, self.K, self.count = int(rows), int(K), int(count)
+        codes, scales = _mx_shapes(self.rows, self.K, self.count)
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.codes = torch.empty(codes, dtype=torch.uint8, device=self.device)
+        self.scales = torch.empty(scales, dtype=torch.uint8, device=self.device)
+
+    @classmethod
+    def of(cls, codes, scales, K: int) -> "MxMatrix":
+        """The matrices that these two tensors hold (not copied)."""
+        import torch
+
+        if codes.dim() != 3:
+            raise ValueError(f"codes must have three dimensions, has {codes.dim()}")
+        self = cls.__new__(cls)
+        self.rows, self.K, self.count = int(codes.shape[1]), int(K), int(codes.shape[0])
+        self.device, self.codes, self.scales = codes.device, codes, scales
+        if self.device.type != "cuda":
+            raise ValueError("codes must live on a GPU")
+        want = _mx_shapes(self.rows, self.K, self.count)
+        _check_shape(codes, "codes", want[0], torch.uint8, self.device)
+        _check_shape(scales, "scales", want[1], torch.uint8, self.device)
+        return self
+
+
+def _check_mx(m, name, rows, K, count, device):
+    if not isinstance(m, MxMatrix):
+        raise TypeError(f"{name} must be an MxMatrix")
+    if m.device != device:
+        raise ValueError(f"{name} must live on {device}")
+    if (m.rows, m.K, m.count) != (rows, K, count):
+        raise ValueError(f"{name} must hold {count} matrices [{rows}, {K}], holds {m.count} of [{m.rows}, {m.K}]")
+
+
+def mx_quantize(X, out: MxMatrix, values=None, down: bool = False, stream=None) -> None:
+    """Enqueue the quantisation of X, bf16 or float32 ``[rows, cols]`` or ``[count, rows, cols]``, into ``out``.
+
+    Blocks of 32 lie along a row, so that ``out`` holds ``[rows, K = cols]``, or with ``down`` down a column: the library's weights
+    ``[K, N]`` become ``[N, K]``.  X's rows must be contiguous, at any distance.  ``values`` (bf16, X's shape, contiguous) receives
+    what the codes stand for."""
+    import torch
+
+    code = _dtype_code(X.dtype)
+    if X.dim() not in (2, 3):
+        raise ValueError(f"X must have two or three dimensions, has {X.dim()}")
+    if X.device.type != "cuda" or X.device.index != torch.cuda.current_device():
+        raise ValueError("X must live on the current device")
+    rows, cols = int(X.shape[-2]), int(X.shape[-1])
+    count = int(X.shape[0]) if X.dim() == 3 else 1
+    _check_mx(out, "out", cols if down else rows, rows if down else cols, count, X.device)
+    if values is not None:
+        _check_shape(values, "values", tuple(X.shape), torch.bfloat16, X.device)
+    ld = X.stride(-2) if rows > 1 else cols
+    matrix = X.stride(0) if count > 1 else rows * ld
+    if (cols > 1 and X.stride(-1) != 1) or ld < cols or (count > 1 and matrix < (rows - 1) * ld + cols):
+        raise ValueError("X's rows must be contiguous and apart from each other")
+    rc = load().mlp2_mx_quantize(count, rows, cols, int(bool(down)), _ptr(X), code, ld, matrix, _ptr(out.codes), _ptr(out.scales),
+                                 _ptr(values), _stream(stream, X.device))
+    if rc != OK:
+        raise Mlp2Error(rc, "mlp2_mx_quantize")
+
+
+class MxPlan(_Owned):
+    """``Y = act(A @ W.T)`` of MXFP4 matrices A ``[M <= max_rows, K]`` and W ``[N, K]`` (SwiGLU: two of them, gate and up), on the
+    current device; ``y_dtype`` is bfloat16 (default) or float32."""
+
+    _name = "mx"
+
+    def __init__(self, max_rows: int, N: int, K: int, act: int = ACT_IDENTITY, y_dtype=None):
+        import torch
+
+        self.max_rows, self.N, self.K, self.act = int(max_rows), int(N), int(K), int(act)
+        self.y_dtype = torch.bfloat16 if y_dtype is None else y_dtype
+        self._create(self.max_rows, self.N, self.K, self.act, _dtype_code(self.y_dtype))
+
+    def product(self, A: MxMatrix, W: MxMatrix, Y, stream=None) -> None:
+        """Enqueue the product on ``stream`` (default: torch's current stream)."""
+        M = int(Y.shape[0])
+        _check_shape(Y, "Y", (M, self.N), self.y_dtype, self.device)
+        _check_mx(A, "A", M, self.K, 1, self.device)
+        _check_mx(W, "W", self.N, self.K, 2 if self.act == ACT_SWIGLU else 1, self.device)
+        self._done(self.lib.mlp2_mx_product(self.handle, M, _ptr(A.codes), _ptr(A.scales), _ptr(W.codes), _ptr(W.scales), _ptr(Y),
+                                            self._on(stream)), "product")

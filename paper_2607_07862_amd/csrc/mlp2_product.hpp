@@ -666,20 +666,12 @@ constexpr int lds_of() {
 // and above the diagonal are computed; those on it are not mirrored.
 // The transpose goes out for rows below Epi's `rows`: M, or M padded, where
 // zeros go out for the rows past M.
-template <class T, class Elem, class P>
-__device__ __forceinline__ void run_product(const P& a, int item, int batch, char* lds) {
+template <class T, class P>
+__device__ __forceinline__ void finish_product(const P& a, Acc<T>& acc, int batch, int tile, int s, int tm_, int tn_, char* lds) {
   using Epi = typename P::Epi;
   static_assert(!Epi::kSymmetric || (Epi::kMirror && T::BM == T::BN), "square tiles on the diagonal");
   constexpr int COLS = Epi::kGated ? T::EC : T::BN;  // result columns of a tile
-  static_assert(T::BK == 64, "a stage is a unit of K");
-  const int total = a.walk.total(), s = item / total, tile = item - s * total;
-  int tm_, tn_;
-  a.walk.at(tile, tm_, tn_);
-  const int m0 = tm_ * T::BM, n0 = tn_ * COLS;
-  const int st0 = s * a.per, nk = min(a.per, a.nk - st0);
-  Acc<T> acc;
-  if constexpr (T::QUAD) product_pingpong<T, Elem, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
-  else product_loop<T, Elem, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  const int total = a.walk.total(), m0 = tm_ * T::BM, n0 = tn_ * COLS;
   int go = 1;
   if (a.split > 1) go = join_parts<T>(acc, a.part, a.arrived, (int64_t)batch * total + tile, a.split, s, a.M - m0, lds);
   if (uniform(go) == 0) return;  // a scalar branch: barriers follow
@@ -740,6 +732,21 @@ __device__ __forceinline__ void run_product(const P& a, int item, int batch, cha
         a.epi.mirror(batch, n0 + col, m0 + 8 * piece, *reinterpret_cast<const u32x4*>(lds + col * mirror_pitch<T>() + 16 * piece));
     }
   }
+}
+
+template <class T, class Elem, class P>
+__device__ __forceinline__ void run_product(const P& a, int item, int batch, char* lds) {
+  constexpr int COLS = P::Epi::kGated ? T::EC : T::BN;  // result columns of a tile
+  static_assert(T::BK == 64, "a stage is a unit of K");
+  const int total = a.walk.total(), s = item / total, tile = item - s * total;
+  int tm_, tn_;
+  a.walk.at(tile, tm_, tn_);
+  const int m0 = tm_ * T::BM, n0 = tn_ * COLS;
+  const int st0 = s * a.per, nk = min(a.per, a.nk - st0);
+  Acc<T> acc;
+  if constexpr (T::QUAD) product_pingpong<T, Elem, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  else product_loop<T, Elem, P::CO, P::JUMP>(a.r, a.c, batch, m0, n0, st0, nk, acc, lds);
+  finish_product<T>(a, acc, batch, tile, s, tm_, tn_, lds);
 }
 
 template <class T, class Elem, class P>
@@ -941,7 +948,7 @@ int choose_shared(const Shape (&s)[N], const SplitSpace& ws, int num_cus, int (&
 }
 
 template <class T, class P>
-P make_problem(const Side& r, const Side& c, int64_t M, int64_t N, int64_t K, int batches, const typename P::Epi& epi, int parts,
+P make_problem(const decltype(P::r)& r, const decltype(P::c)& c, int64_t M, int64_t N, int64_t K, int batches, const typename P::Epi& epi, int parts,
                const SplitSpace& ws) {
   constexpr int COLS = P::Epi::kGated ? T::EC : T::BN;
   P a{};

@@ -1,0 +1,126 @@
+"""The product of MXFP4 matrices on the GPU against fp64: sizes, odd widths and depths, activations, types, NaN, graphs."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_07862_amd import binding as B
+from tests._mx import NAMES, held, product_and_tol
+from tests._train import assert_within
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def matrix(gen, rows, K, count=1, std=1.0):
+    """Random values of rows of different sizes, quantised on the GPU."""
+    x = torch.randn((count, rows, K), generator=gen) * torch.exp(0.5 * torch.randn((count, rows, 1), generator=gen)) * std
+    mx = B.MxMatrix(rows, K, count)
+    B.mx_quantize(x.cuda(), mx)
+    return mx
+
+
+def check(M, N, K, act, y=BF, plan=None, seed=0, max_rows=None):
+    gen = torch.Generator().manual_seed(seed + M + N + K)
+    nb = 2 if act == B.ACT_SWIGLU else 1
+    A, W = matrix(gen, M, K), matrix(gen, N, K, nb, K**-0.5)
+    Y = torch.full((M, N), float("nan"), dtype=y, device="cuda")
+    plan = plan or B.MxPlan(max_rows or M, N, K, act, y)
+    plan.product(A, W, Y)
+    ref, tol = product_and_tol(held(A), [held(W, i) for i in range(nb)], NAMES[act], y == F32)
+    assert_within(Y, ref, tol, f"Y {M}x{N}x{K} {NAMES[act]}")
+    return plan, A, W, Y
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("y", [BF, F32])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 64), (2, 33, 31), (3, 7, 128), (16, 130, 129), (17, 64, 256), (33, 65, 257), (64, 128, 384), (65, 257, 640),
+                                   (127, 100, 1000), (200, 515, 129), (300, 96, 2049)])
+def test_sizes(lib, M, N, K, act, y):
+    check(M, N, K, act, y)
+
+
+@pytest.mark.parametrize("M,N,K,act", [(1, 4096, 14336, 0), (5, 1000, 8192, 2), (16, 2111, 5441, 1), (700, 1100, 640, 2), (1024, 1536, 384, 0),
+                                       (513, 2049, 1153, 0), (1111, 2048, 256, 2), (4096, 300, 128, 1)])
+def test_larger(lib, M, N, K, act):
+    check(M, N, K, act)
+
+
+def test_fewer_rows_than_planned(lib):
+    plan, *_ = check(300, 192, 320, 0)
+    for M in (1, 16, 17, 64, 65, 299):
+        check(M, 192, 320, 0, plan=plan)
+    plan.product(B.MxMatrix(0, 320), matrix(torch.Generator(), 192, 320), torch.empty((0, 192), dtype=BF, device="cuda"))
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+def test_nan_stays_in_its_row_and_column(lib, M):
+    """A block scaled by NaN makes its row (of A) or column (of W) NaN and nothing else."""
+    gen = torch.Generator().manual_seed(9)
+    N, K = 90, 600
+    A, W = matrix(gen, M, K), matrix(gen, N, K)
+    clean, Y = torch.empty((M, N), device="cuda"), torch.empty((M, N), device="cuda")
+    plan = B.MxPlan(M, N, K, 0, F32)
+    plan.product(A, W, clean)
+    A.scales[0, 4, M // 2, 2] = 255
+    W.scales[0, 0, 17, 3] = 255
+    plan.product(A, W, Y)
+    nan = Y.isnan()
+    assert nan[M // 2].all() and nan[:, 17].all()
+    nan[M // 2], nan[:, 17] = True, True
+    assert torch.equal(Y[~nan], clean[~nan])
+    assert int(nan.sum()) == M + N - 1
+
+
+@pytest.mark.parametrize("M", [3, 150])
+def test_extreme_scales(lib, M):
+    """Scales at both ends: products of the smallest vanish in fp32, products that pass fp32's range are infinite."""
+    gen = torch.Generator().manual_seed(2)
+    A, W = matrix(gen, M, 256), matrix(gen, 64, 256)
+    A.scales.fill_(0), W.scales.fill_(0)
+    Y = torch.empty((M, 64), device="cuda")
+    plan = B.MxPlan(M, 64, 256, 0, F32)
+    plan.product(A, W, Y)
+    assert (Y == 0).all()
+    A.scales.fill_(254), W.scales.fill_(0)  # 2^127 2^-127
+    plan.product(A, W, Y)
+    ref, tol = product_and_tol(held(A), [held(W)], "identity", True)
+    assert_within(Y, ref, tol, "Y")
+
+
+def test_same_bits_every_time(lib):
+    """Parts of K are joined in one order, whichever work-group comes last."""
+    plan, A, W, Y = check(16, 320, 16384, 0, F32)
+    for _ in range(5):
+        again = torch.empty_like(Y)
+        plan.product(A, W, again)
+        assert torch.equal(again, Y)
+
+
+def test_captured(lib):
+    gen = torch.Generator().manual_seed(3)
+    M, N, K = 24, 300, 4096
+    A, W = matrix(gen, M, K), matrix(gen, N, K, 2, K**-0.5)
+    plan = B.MxPlan(M, N, K, B.ACT_SWIGLU)
+    Y, want = (torch.empty((M, N), dtype=BF, device="cuda") for _ in range(2))
+    plan.product(A, W, Y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.product(A, W, Y)
+    for i in range(4):
+        B.mx_quantize(torch.randn((M, K), device="cuda"), A)
+        Y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        plan.product(A, W, want)
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want), i
+
+
+def test_rows_behind_the_last_are_left(lib):
+    gen = torch.Generator().manual_seed(4)
+    for M in (5, 70):
+        A, W = matrix(gen, M, 256), matrix(gen, 77, 256)
+        whole = torch.full((M + 3, 77), 5.0, dtype=BF, device="cuda")
+        B.MxPlan(M, 77, 256, 0).product(A, W, whole[:M])
+        assert (whole[M:] == 5).all() and (whole[:M] != 5).any()
