@@ -65,7 +65,8 @@ extern "C" {
 typedef struct mlp2_plan_s* mlp2_plan_t; /* opaque; created by mlp2_plan, freed by mlp2_destroy */
 
 enum mlp2_act { MLP2_ACT_IDENTITY = 0, MLP2_ACT_GELU_TANH = 1, MLP2_ACT_SWIGLU = 2 };
-enum mlp2_dtype { MLP2_DTYPE_BF16 = 0, MLP2_DTYPE_F32 = 1 /* not for mlp2_plan, mlp2_chain_plan, mlp2_train_plan */ };
+enum mlp2_dtype { MLP2_DTYPE_BF16 = 0, MLP2_DTYPE_F32 = 1 /* not for mlp2_plan, mlp2_chain_plan, mlp2_train_plan */,
+                  MLP2_DTYPE_MXFP4 = 2 /* weights of mlp2_moe_plan only */ };
 /* MLP2_MODE_SENTINEL is the pipelined launch with the Lamport-style
  * synchronisation the paper discusses as an alternative (Sec. V-A): GEMM1
  * tiles store the intermediate at device scope with no fence and no ready
@@ -486,6 +487,36 @@ int mlp2_mx_product(mlp2_mx_t plan, int64_t M, const void* A, const void* A_scal
 
 /* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
 void mlp2_mx_destroy(mlp2_mx_t plan);
+
+/* ---- Mixture of experts for a few tokens (decoding batches): router, the best
+ * k of E experts for each token, their two-layer MLPs and the weighted sum,
+ *
+ *     Y[t] = sum over j < k of gates[t][j] * (act(X[t] . W1[e]) . W2[e]),  e = ids[t][j].
+ *
+ * Plan it for up to max_tokens tokens: H and F multiples of 64 up to 32768, 1 <= k <= E <= 512, k <= 16, max_tokens * k <=
+ * 8192, act in enum mlp2_act; w_dtype: the experts' weights in bf16, W1 [E, H, F] (SwiGLU [E, 2, H, F]: Wg, Wu) and W2 [E, F,
+ * H], or MLP2_DTYPE_MXFP4, W1 as E (SwiGLU: 2 E, Wg and Wu of each in turn) matrices [F, K = H] and W2 as E matrices [H, K = F], codes and
+ * scales as for mlp2_mx_quantize with down = 1.  X and the intermediate are bf16
+ * either way; 4-bit weights are taken as the bf16 numbers they stand for.  All sums are fp32.
+ * A plan's calls are ordered on one stream.  NULL on failure (mlp2_last_error). */
+typedef struct mlp2_moe_s* mlp2_moe_t;
+mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, int64_t k, int act, int w_dtype);
+
+/* Y [T, H] bf16, ids [T, k] int32 and gates [T, k] fp32 from X [T, H] bf16 and the router's weight Wr [H, E] (wr_dtype bf16 or
+ * F32): ids are the k largest logits X . Wr of a token in order, ties to the lowest index, NaN counting as the
+ * largest; gates are the softmax over those k.  The logits are summed in fp64, so the choice is that of the exact ones but for
+ * differences of 1e-15.  W1_scales and W2_scales are NULL for bf16 weights.  0 <= T <= max_tokens (0 does nothing). */
+int mlp2_moe_forward(mlp2_moe_t plan, int64_t T, const void* X, const void* Wr, int wr_dtype, const void* W1, const void* W1_scales,
+                     const void* W2, const void* W2_scales, void* Y, void* ids, void* gates, void* stream);
+
+/* The same with the caller's ids and gates.  A slot whose id is outside [0, E)
+ * is empty (-1 by convention; its gate is not read); a token without experts
+ * gets zeros; an expert may stand in several slots of a token. */
+int mlp2_moe_experts(mlp2_moe_t plan, int64_t T, const void* X, const void* ids, const void* gates, const void* W1, const void* W1_scales,
+                     const void* W2, const void* W2_scales, void* Y, void* stream);
+
+/* Free the plan and its workspace (synchronises the device first).  NULL-safe. */
+void mlp2_moe_destroy(mlp2_moe_t plan);
 
 #ifdef __cplusplus
 }

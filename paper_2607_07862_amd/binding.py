@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(PKG, "libmlp2.so")
 TRACE_LIB_PATH = os.path.join(PKG, "libmlp2_trace.so")
 
 ACT_IDENTITY, ACT_GELU_TANH, ACT_SWIGLU = 0, 1, 2
-DTYPE_BF16, DTYPE_F32 = 0, 1
+DTYPE_BF16, DTYPE_F32, DTYPE_MXFP4 = 0, 1, 2
 MODE_SEQUENTIAL, MODE_TILE_PIPELINED, MODE_WORKQUEUE, MODE_STAGE1, MODE_STAGE2, MODE_SENTINEL = 0, 1, 2, 3, 4, 5
 MODES = {"sequential": MODE_SEQUENTIAL, "tile_pipelined": MODE_TILE_PIPELINED, "workqueue": MODE_WORKQUEUE,
          "stage1": MODE_STAGE1, "stage2": MODE_STAGE2, "sentinel": MODE_SENTINEL}
@@ -60,6 +60,10 @@ EXPORTS = (
     "mlp2_mx_plan",
     "mlp2_mx_product",
     "mlp2_mx_destroy",
+    "mlp2_moe_plan",
+    "mlp2_moe_forward",
+    "mlp2_moe_experts",
+    "mlp2_moe_destroy",
 )
 
 
@@ -184,7 +188,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.mlp2_run_noalloc.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_int,
                                      P, P, P, P, P, ctypes.c_int]
     I64, F32 = ctypes.c_int64, ctypes.c_float
-    for name in ("train", "norm", "ortho", "mx"):
+    for name in ("train", "norm", "ortho", "mx", "moe"):
         getattr(lib, f"mlp2_{name}_plan").restype = P
         getattr(lib, f"mlp2_{name}_destroy").restype = None
         getattr(lib, f"mlp2_{name}_destroy").argtypes = [P]
@@ -206,6 +210,11 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.mlp2_mx_plan.argtypes = [I64, I64, I64, ctypes.c_int, ctypes.c_int]
     lib.mlp2_mx_product.restype = ctypes.c_int
     lib.mlp2_mx_product.argtypes = [P, I64] + [P] * 6
+    lib.mlp2_moe_plan.argtypes = [I64, I64, I64, I64, I64, ctypes.c_int, ctypes.c_int]
+    lib.mlp2_moe_forward.restype = ctypes.c_int
+    lib.mlp2_moe_forward.argtypes = [P, I64, P, P, ctypes.c_int] + [P] * 8
+    lib.mlp2_moe_experts.restype = ctypes.c_int
+    lib.mlp2_moe_experts.argtypes = [P, I64] + [P] * 9
     _lib = lib
     return lib
 
@@ -722,3 +731,53 @@ class MxPlan(_Owned):
         _check_mx(W, "W", self.N, self.K, 2 if self.act == ACT_SWIGLU else 1, self.device)
         self._done(self.lib.mlp2_mx_product(self.handle, M, _ptr(A.codes), _ptr(A.scales), _ptr(W.codes), _ptr(W.scales), _ptr(Y),
                                             self._on(stream)), "product")
+
+
+class MoePlan(_Owned):
+    """A mixture-of-experts layer for up to ``max_tokens`` tokens: the best ``k`` of ``E`` experts of each, two-layer MLPs.
+
+    ``w_dtype``: bfloat16, W1 ``[E, H, F]`` (SwiGLU ``[E, 2, H, F]``) and W2 ``[E, F, H]``, or ``"mxfp4"``, W1 an ``MxMatrix`` of E
+    (SwiGLU 2 E) matrices ``[F, K = H]`` and W2 one of E matrices ``[H, K = F]``, as ``mx_quantize(..., down=True)`` makes them."""
+
+    _name = "moe"
+
+    def __init__(self, max_tokens: int, H: int, F: int, E: int, k: int, act: int = ACT_SWIGLU, w_dtype=None):
+        import torch
+
+        self.max_tokens, self.H, self.F, self.E, self.k, self.act = int(max_tokens), int(H), int(F), int(E), int(k), int(act)
+        self.mx = isinstance(w_dtype, str) and w_dtype == "mxfp4"
+        if not self.mx and w_dtype not in (None, torch.bfloat16):
+            raise TypeError(f'{w_dtype} is not supported: bfloat16 or "mxfp4"')
+        self._i32 = torch.int32
+        self._create(self.max_tokens, self.H, self.F, self.E, self.k, self.act, DTYPE_MXFP4 if self.mx else DTYPE_BF16)
+
+    def _check(self, X, W1, W2, Y, ids, gates):
+        T, H, F, E = int(X.shape[0]), self.H, self.F, self.E
+        gated = self.act == ACT_SWIGLU
+        _check_shape(X, "X", (T, H), self._bf16, self.device)
+        _check_shape(Y, "Y", (T, H), self._bf16, self.device)
+        _check_shape(ids, "ids", (T, self.k), self._i32, self.device)
+        _check_shape(gates, "gates", (T, self.k), self._f32, self.device)
+        if self.mx:
+            _check_mx(W1, "W1", F, H, 2 * E if gated else E, self.device)
+            _check_mx(W2, "W2", H, F, E, self.device)
+            return T, (_ptr(W1.codes), _ptr(W1.scales), _ptr(W2.codes), _ptr(W2.scales))
+        if isinstance(W1, MxMatrix) or isinstance(W2, MxMatrix):
+            raise TypeError("W1 and W2 must be bfloat16 tensors")
+        _check_shape(W1, "W1", (E, 2, H, F) if gated else (E, 1, H, F) if W1.dim() == 4 else (E, H, F), self._bf16, self.device)
+        _check_shape(W2, "W2", (E, F, H), self._bf16, self.device)
+        return T, (_ptr(W1), 0, _ptr(W2), 0)
+
+    def forward(self, X, Wr, W1, W2, Y, ids, gates, stream=None) -> None:
+        """Enqueue the whole layer: ids ``[T, k]`` (int32) and gates ``[T, k]`` (float32) from the router's weight Wr ``[H, E]``
+        (bfloat16 or float32), then Y."""
+        T, w = self._check(X, W1, W2, Y, ids, gates)
+        code = _dtype_code(Wr.dtype)
+        _check_shape(Wr, "Wr", (self.H, self.E), Wr.dtype, self.device)
+        self._done(self.lib.mlp2_moe_forward(self.handle, T, _ptr(X), _ptr(Wr), code, *w, _ptr(Y), _ptr(ids), _ptr(gates),
+                                             self._on(stream)), "forward")
+
+    def experts(self, X, ids, gates, W1, W2, Y, stream=None) -> None:
+        """Enqueue the experts and their weighted sum for the caller's ids (outside ``[0, E)``: an empty slot) and gates."""
+        T, w = self._check(X, W1, W2, Y, ids, gates)
+        self._done(self.lib.mlp2_moe_experts(self.handle, T, _ptr(X), _ptr(ids), _ptr(gates), *w, _ptr(Y), self._on(stream)), "experts")

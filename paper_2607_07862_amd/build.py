@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_NAME = "libmlp2.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
 SOURCES = ["mlp2_kernels.hip", "mlp2_api.cpp", "mlp2_noalloc.hip", "mlp2_train.hip", "mlp2_norm.hip",
-           "mlp2_ortho.hip", "mlp2_mx.hip"]
+           "mlp2_ortho.hip", "mlp2_mx.hip", "mlp2_moe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed fp32 VALU ops are turned off for all device code.  The atomic
