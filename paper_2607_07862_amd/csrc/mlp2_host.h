@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <cstring>
 
@@ -21,6 +22,19 @@ inline int current_device(int* device, int* num_cus) {
   if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0) return MLP2_ERR_DEVICE;
   *num_cus = prop.multiProcessorCount;
   return MLP2_OK;
+}
+
+// The same for calls without a plan: what a device is does not change, and asking the runtime for all its properties takes longer
+// than the smallest calls do.
+inline int usable_device() {
+  static std::atomic<uint64_t> known{0};
+  int device = -1, cus;
+  if (hipGetDevice(&device) != hipSuccess) return MLP2_ERR_DEVICE;
+  const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+  if (known.load(std::memory_order_relaxed) & bit) return MLP2_OK;
+  const int rc = current_device(&device, &cus);
+  if (rc == MLP2_OK) known.fetch_or(bit, std::memory_order_relaxed);
+  return rc;
 }
 
 inline bool on_device(int device) {

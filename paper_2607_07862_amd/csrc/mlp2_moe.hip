@@ -20,19 +20,29 @@ namespace mlp2 {
 
 constexpr int kMostExperts = 512, kMostSlots = 8192, kMostChosen = 16;
 constexpr int kWaves = 4;
+constexpr int kRoutePart = 512;  // the most of K in a part of the router
 
 // ------------------------------------------------------------------ memory that other XCDs write and read in the same launch
 
+// (Buffer accesses with the device-scope bit: stores are written through, loads go past this XCD's L2.  Unlike atomic loads, which the
+// compiler waits for one by one, these are in flight together.)
+constexpr int kSc1 = 16;
+constexpr int kNt = 2;  // streamed: read once
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void store_far(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ double load_far(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void store_far(float* p, float a, float b) {
-  const f32x2 v = {a, b};
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x2 load_far(const float* p) {
-  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
+struct Far {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ explicit Far(const void* p) : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)p, 0, -1, 0x00027000)) {}
+  __device__ __forceinline__ void store16(uint32_t off, f32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rsrc, (int)off, 0, kSc1);
+  }
+  __device__ __forceinline__ f32x4 load16(uint32_t off) const {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)off, 0, kSc1));
+  }
+  __device__ __forceinline__ double load_double(uint32_t off) const {
+    return __builtin_bit_cast(double, __builtin_amdgcn_raw_buffer_load_b64(rsrc, (int)off, 0, kSc1));
+  }
+};
 
 // ------------------------------------------------------------------ router
 
@@ -100,32 +110,47 @@ __device__ __forceinline__ void choose_experts(const double* logits, int E, int 
 }
 
 // Logits of TT tokens over one part of K, in fp64: which experts are chosen hangs on logits next to each other, and fp32 sums would
-// put some of them in another order.  256 threads are `width` experts by 256 / width rows of K.
+// put some of them in another order.  256 threads are `width` experts by 256 / width rows of K.  Latencies bound it: the part's X and
+// the first weights are requested together, the parts' sums are read all at once.
 template <class W, int TT>
 __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
-  __shared__ __align__(16) double lds[256 * TT > TT * kMostExperts ? 256 * TT : TT * kMostExperts];
+  constexpr int MOST = TT * kMostExperts > TT * kRoutePart ? TT * kMostExperts : TT * kRoutePart;
+  __shared__ __align__(16) double lds[256 * TT > MOST ? 256 * TT : MOST];
   __shared__ int seen;
+  constexpr int AHEAD = 8;
   const int tid = threadIdx.x, t0 = blockIdx.x * TT, split = blockIdx.y;
   const int sub = tid / a.width, subs = 256 / a.width, e0 = tid % a.width;
-  const int from = split * a.per, to = min(a.H, from + a.per);
-  const W* Wr = (const W*)a.Wr;
+  const int from = split * a.per, deep = min(a.H - from, a.per);
+  const W* Wr = (const W*)a.Wr + (int64_t)from * a.E;
   const int chunks = (a.E + a.width - 1) / a.width;  // of experts; one but for E > 256
   for (int c = 0; c < chunks; ++c) {
     const int e = c * a.width + e0;
-    double acc[TT] = {};
-    for (int k0 = from; k0 < to; k0 += 64) {
-      // 64 of K of the tokens' rows
-      if (c || k0 > from) __syncthreads();
-      for (int i = tid; i < 64 * TT; i += 256) {
-        const int t = i / 64, kk = i % 64;
-        lds[kk * TT + t] = t0 + t < a.T ? widen(a.X[(int64_t)(t0 + t) * a.H + k0 + kk]) : 0.0;
+    W w[AHEAD];
+    auto request = [&](int k0) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int kk = k0 + i * subs;
+        w[i] = Wr[kk < deep && e < a.E ? (int64_t)kk * a.E + e : 0];
       }
-      __syncthreads();
-      if (e < a.E) {
-        const W* w = Wr + (int64_t)k0 * a.E + e;
-#pragma unroll 8
-        for (int kk = sub; kk < 64; kk += subs) {
-          const double v = widen(w[(int64_t)kk * a.E]);
+    };
+    request(sub);
+    if (c) __syncthreads();
+    for (int i = tid; i < deep * TT; i += 256) {
+      const int t = i / deep, kk = i % deep;
+      lds[kk * TT + t] = t0 + t < a.T ? widen(a.X[(int64_t)(t0 + t) * a.H + from + kk]) : 0.0;
+    }
+    __syncthreads();
+    double acc[TT] = {};
+    for (int k0 = sub; k0 < deep; k0 += AHEAD * subs) {
+      W now[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) now[i] = w[i];
+      request(k0 + AHEAD * subs);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int kk = k0 + i * subs;
+        if (kk < deep) {
+          const double v = widen(now[i]);
 #pragma unroll
           for (int t = 0; t < TT; ++t) acc[t] = __builtin_fma(v, lds[kk * TT + t], acc[t]);
         }
@@ -139,6 +164,7 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
     for (int i = tid; i < TT * a.width; i += 256) {
       const int t = i / a.width, en = c * a.width + i % a.width;
       double sum = 0.0;
+#pragma unroll 8
       for (int s = 0; s < subs; ++s) sum += lds[(s * TT + t) * a.width + i % a.width];
       if (t0 + t < a.T && en < a.E) store_far(a.part + ((int64_t)split * a.T + t0 + t) * a.E + en, sum);
     }
@@ -149,11 +175,20 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
   __syncthreads();
   if (uniform(seen) != a.splits - 1) return;
   if (tid == 0) __hip_atomic_store(a.arrived + blockIdx.x * kLine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  for (int i = tid; i < TT * a.E; i += 256) {
-    const int t = i / a.E;
+  // The parts, 8 at a time; all in the order 0, 1, ... whichever came last.
+  const Far part(a.part);
+  const int here = min(TT, a.T - t0) * a.E;
+  for (int i = tid; i < here; i += 256) {
+    const uint32_t first = (uint32_t)((t0 * a.E + i) * 8), pitch = (uint32_t)(a.T * a.E * 8);
     double sum = 0.0;
-    if (t0 + t < a.T)
-      for (int s = 0; s < a.splits; ++s) sum += load_far(a.part + ((int64_t)s * a.T + t0) * a.E + i);
+    for (int s = 0; s < a.splits; s += 8) {
+      double v[8];
+#pragma unroll
+      for (int d = 0; d < 8; ++d) v[d] = part.load_double(first + min(s + d, a.splits - 1) * pitch);
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+        if (s + d < a.splits) sum += v[d];
+    }
     lds[i] = sum;
   }
   __syncthreads();
@@ -170,11 +205,12 @@ struct Experts {
   const char* W;       // bf16 [E, nb, K, N], or MXFP4 codes of E nb matrices [N, K]
   const char* scales;
   uint16_t* out;       // first: Z; second: Y [T, H]
-  float* part;         // second: [splits, T k, N]
-  uint32_t* arrived;   // second: one counter for each token and block of columns; zero between launches
+  float* part;         // parts of K: first [splits, T k, nb, N], second [splits, T k, N] with the gates applied; below 4 GB
+  uint32_t* arrived;   // zero between launches; first: one counter for each slot and block of columns, second: for each token and block
   int T, E, k, K, N;
-  int blocks;          // of columns
-  int splits, per;     // parts of K, steps of each
+  int blocks;          // of 128 columns
+  int steps;           // of K, of a wave
+  int most;            // parts of K
 };
 
 // Weights as they lie in the rest of the library, [K, N] in bf16.  A lane loads 8 columns of 8 consecutive k; taken by columns,
@@ -183,25 +219,27 @@ struct Experts {
 struct Bf16Weights {
   static constexpr int STEP = 32;  // K of a step
   static constexpr int MOST = 4;   // blocks of 16 rows that one pass over the weights serves
+  static constexpr int RING = 2;   // steps in registers
   template <int MT>
   struct Regs {
     u32x4 w[8], x[MT];
   };
   uint32_t off, row;  // of this lane's first row, and from row to row
-  __device__ __forceinline__ Bf16Weights(const Experts& a, int col, int64_t second) {
-    const int lane = threadIdx.x & 63, c = lane & 15;
-    // columns past the last are read as the last eight
-    const int mine = second ? col + 8 * (c & 7) : col + 8 * c;
+  __device__ __forceinline__ Bf16Weights(const Experts& a, int col) {
+    const int lane = threadIdx.x & 63;
     row = (uint32_t)(2 * a.N);
-    off = (uint32_t)((second && c >= 8 ? second : 0) + 2 * (min(mine, a.N - 8) + (int64_t)(8 * (lane >> 4)) * a.N));
+    // columns past the last are read as the last eight
+    off = (uint32_t)(2 * (min(col + 8 * (lane & 15), a.N - 8) + 8 * (lane >> 4) * a.N));
   }
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return (int64_t)a.K * a.N * 2; }
   template <int MT>
-  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const char*, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step) const {
-    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + (int64_t)step * STEP * a.N * 2), 0, -1, 0x00027000);
-    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, -1, 0x00027000);
+  // Steps from `end` on load zeros, from nowhere.
+  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const char*, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step, int end) const {
+    const int range = step < end ? -1 : 0;
+    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + (int64_t)step * STEP * a.N * 2), 0, range, 0x00027000);
+    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, range, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.w[i] = __builtin_amdgcn_raw_buffer_load_b128(wr, (int)off, (int)(i * row), 0);
+    for (int i = 0; i < 8; ++i) r.w[i] = __builtin_amdgcn_raw_buffer_load_b128(wr, (int)off, (int)(i * row), kNt);
 #pragma unroll
     for (int m = 0; m < MT; ++m) r.x[m] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)xo[m], 0, 0);
   }
@@ -239,32 +277,34 @@ struct Bf16Weights {
 struct MxWeights {
   static constexpr int STEP = 128;
   static constexpr int MOST = 2;
+  static constexpr int RING = 2;
   template <int MT>
   struct Regs {
     u32x4 w[8], x[MT][4];
     uint32_t s[8];
   };
   uint32_t off[8], soff[8];
-  __device__ __forceinline__ MxWeights(const Experts& a, int col, int64_t second) {
+  __device__ __forceinline__ MxWeights(const Experts& a, int col) {
     const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int64_t ld = mx_padded(a.K) / 2, groups = ld / 64;
+    const int64_t ld = mx_padded(a.K) / 2;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int up = second && j >= 4, n = min(col + 16 * (up ? j - 4 : j) + (lane & 15), a.N - 1);
-      off[j] = (uint32_t)(((int64_t)up * a.N + n) * ld + 16 * g);
-      soff[j] = (uint32_t)((up * groups * a.N + n) * 4 + g);
+      const int n = min(col + 16 * j + (lane & 15), a.N - 1);
+      off[j] = (uint32_t)(n * ld + 16 * g);
+      soff[j] = (uint32_t)(n * 4 + g);
     }
   }
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return a.N * (mx_padded(a.K) / 2); }
   template <int MT>
-  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const char* s, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step) const {
-    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + step * 64), 0, -1, 0x00027000);
-    const auto sr = __builtin_amdgcn_make_buffer_rsrc((void*)(s + (int64_t)step * a.N * 4), 0, -1, 0x00027000);
-    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, -1, 0x00027000);
+  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const char* s, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step, int end) const {
+    const int range = step < end ? -1 : 0;
+    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + step * 64), 0, range, 0x00027000);
+    const auto sr = __builtin_amdgcn_make_buffer_rsrc((void*)(s + (int64_t)step * a.N * 4), 0, range, 0x00027000);
+    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, range, 0x00027000);
 #pragma unroll
     for (int j = 0; j < 8; ++j) r.s[j] = __builtin_amdgcn_raw_buffer_load_b8(sr, (int)soff[j], 0, 0);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r.w[j] = __builtin_amdgcn_raw_buffer_load_b128(wr, (int)off[j], 0, 0);
+    for (int j = 0; j < 8; ++j) r.w[j] = __builtin_amdgcn_raw_buffer_load_b128(wr, (int)off[j], 0, kNt);
     // K may end inside the last step (it is a multiple of 64): the lanes past it read the step's first k and are cleared
     const bool past = step * STEP + 32 * (int)((threadIdx.x & 63) >> 4) >= a.K;
 #pragma unroll
@@ -275,7 +315,6 @@ struct MxWeights {
   __device__ static __forceinline__ int x_lane() { return 32 * ((threadIdx.x & 63) >> 4); }
   template <int MT>
   __device__ __forceinline__ void multiply(Regs<MT>& r, f32x4 (&acc)[MT][8], const Experts& a, int step) const {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     if ((step + 1) * STEP > a.K) {
       const bool past = step * STEP + x_lane() >= a.K;
 #pragma unroll
@@ -287,15 +326,14 @@ struct MxWeights {
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      // 2^(s - 127) as a float; 2^-127 is a subnormal one
-      const float scale = __builtin_bit_cast(float, r.s[j] == 0 ? 0x00400000u : r.s[j] == 255 ? 0x7FC00000u : r.s[j] << 23);
+      const float scale = mx_unit(r.s[j]);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         u32x4 f;
-        f[0] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 0));
-        f[1] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 1));
-        f[2] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 2));
-        f[3] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 3));
+        f[0] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 0));
+        f[1] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 1));
+        f[2] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 2));
+        f[3] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 3));
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[m][j] = Bf16::mfma(f, r.x[m][q], acc[m][j]);
       }
@@ -312,224 +350,361 @@ constexpr int kPitch = 128 + 4;  // floats of a row of sums in LDS
 struct MoeShared {
   float sums[kWaves][16][kPitch];
   int count[kMostExperts];  // slots of an expert
-  int start[kMostExperts];  // its first item
-  int rows[64];             // slots of the item
-  int total, expert, found;
-  int done[64];             // second: tokens of the item that are complete
+  int start[kMostExperts];  // its first unit (an expert's chunk of rows and a block of columns)
+  int rows[kWaves][64];     // slots of the item, a copy for each wave
+  int total, last;
+  int found, done[64];      // second: tokens of the item that are complete
+  uint32_t valid[64];       // and their slots that have an expert
 };
 
-// Items of every expert: start[] and their total, from the counts.
-__device__ __forceinline__ void place_items(MoeShared& s, const Experts& a, int tile) {
-  const int tid = threadIdx.x;
-  for (int e = tid; e < a.E; e += 256) s.count[e] = 0;
-  __syncthreads();
-  for (int i = tid; i < a.T * a.k; i += 256) {
-    const int e = a.ids[i];
-    if (e >= 0 && e < a.E) atomicAdd(&s.count[e], 1);
-  }
-  __syncthreads();
-  if (tid < 64) {
-    int before = 0;
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
-      const int e = e0 + tid, n = e < a.E ? (s.count[e] + tile - 1) / tile * a.blocks * a.splits : 0;
-      int sum = n;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int v = __shfl_up(sum, d);
-        if (tid >= d) sum += v;
+// An item of work: up to `tile` slots of an expert, a block of columns, a part of K.
+struct Item {
+  int expert, block, split, first, rows;
+};
+
+// Items, from ids.  Up to 64 slots every wave keeps them in a register and goes through the experts that it finds there; beyond,
+// the work-group counts the slots of every expert in LDS.  Either way a wave finds its item and rows without a barrier.
+template <int TILE>
+struct Items {
+  int id;       // few slots: this lane's
+  bool few;
+  int units, splits, per;  // per: steps of a part
+  __device__ __forceinline__ static int chunks(int slots) { return (slots + TILE - 1) / TILE; }
+  __device__ __forceinline__ Items(MoeShared& s, const Experts& a) {
+    const int tid = threadIdx.x, lane = tid & 63, slots = a.T * a.k;
+    few = slots <= 64;
+    id = -1;
+    units = 0;
+    if (few) {
+      if (lane < slots) id = a.ids[lane];
+      if (id >= a.E) id = -1;
+      for (uint64_t left = __ballot(id >= 0); left;) {
+        const uint64_t same = __ballot(id == __builtin_amdgcn_readlane(id, __builtin_ctzll(left)));
+        units += chunks(__builtin_popcountll(same)) * a.blocks;
+        left &= ~same;
       }
-      if (e < a.E) s.start[e] = before + sum - n;
-      before += __shfl(sum, 63);
+    } else {
+      for (int e = tid; e < a.E; e += 256) s.count[e] = 0;
+      __syncthreads();
+      for (int i = tid; i < slots; i += 256) {
+        const int e = a.ids[i];
+        if (e >= 0 && e < a.E) atomicAdd(&s.count[e], 1);
+      }
+      __syncthreads();
+      if (tid < 64) {
+        int before = 0;
+        for (int e0 = 0; e0 < a.E; e0 += 64) {
+          const int e = e0 + tid, n = e < a.E ? chunks(s.count[e]) * a.blocks : 0;
+          int sum = n;
+#pragma unroll
+          for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(sum, d);
+            if (tid >= d) sum += v;
+          }
+          if (e < a.E) s.start[e] = before + sum - n;
+          before += __shfl(sum, 63);
+        }
+        if (tid == 0) s.total = before;
+      }
+      __syncthreads();
+      units = uniform(s.total);
     }
-    if (tid == 0) s.total = before;
+    // Parts of K: as many as make the work-groups' shares alike, each item costing about two steps more than it streams.  (A CU takes in
+    // at most 40 to 50 GB/s, whatever its loads in flight, so the last round of a few items is as long as a whole one.)
+    int least = 0x7FFFFFFF;
+    splits = 1;
+    const int grid = gridDim.x;
+    for (int n = 1; n <= a.most; ++n) {
+      const int rounds = (units * n + grid - 1) / grid, steps = (a.steps + n - 1) / n, cost = rounds * (steps + 2 * kWaves) + (n > 1 ? kWaves : 0);
+      if (cost < least) {
+        least = cost;
+        splits = n;
+      }
+    }
+    splits = uniform(splits);
+    per = (a.steps + splits - 1) / splits;
+    splits = (a.steps + per - 1) / per;
   }
-  __syncthreads();
-}
+  __device__ __forceinline__ int total() const { return units * splits; }
 
-// The item's expert, and the slots of its chunk of rows: their number, and the slots in s.rows.
-__device__ __forceinline__ int find_rows(MoeShared& s, const Experts& a, int item, int tile, int& expert, int& block, int& split) {
-  const int tid = threadIdx.x;
-  __syncthreads();  // the last item's rows are no longer read
-  for (int e = tid; e < a.E; e += 256) {
-    const int n = (s.count[e] + tile - 1) / tile * a.blocks * a.splits;
-    if (item >= s.start[e] && item < s.start[e] + n) s.expert = e;
-  }
-  __syncthreads();
-  expert = uniform(s.expert);
-  const int in = item - uniform(s.start[expert]);
-  // consecutive items: the blocks of columns, then the parts of K, then the next rows
-  block = in % a.blocks;
-  split = in / a.blocks % a.splits;
-  const int first = in / (a.blocks * a.splits) * tile, rows = min(tile, uniform(s.count[expert]) - first);
-  if (tid < 64) {
-    int before = 0;
-    for (int i0 = 0; i0 < a.T * a.k; i0 += 64) {
-      const int i = i0 + tid;
-      const bool here = i < a.T * a.k && a.ids[i] == expert;
+  // Item `n`; its slots go to s.rows[wave].
+  __device__ __forceinline__ Item find(MoeShared& s, const Experts& a, int n) const {
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), slots = a.T * a.k;
+    // consecutive items: the blocks of columns, then the next rows, then the next expert, then the next part of K
+    Item it;
+    it.split = n / units;
+    int in = n - it.split * units, count = 0;
+    it.expert = 0;
+    if (few) {
+      for (uint64_t left = __ballot(id >= 0); left;) {
+        const int e = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const uint64_t same = __ballot(id == e);
+        it.expert = e;
+        count = __builtin_popcountll(same);
+        const int here = chunks(count) * a.blocks;
+        if (in < here) break;
+        in -= here;
+        left &= ~same;
+      }
+    } else {
+      for (int e0 = 0; e0 < a.E; e0 += 64) {
+        const int e = e0 + lane;
+        const bool here = e < a.E && in >= s.start[e] && in < s.start[e] + chunks(s.count[e]) * a.blocks;
+        const uint64_t m = __ballot(here);
+        if (m) {
+          it.expert = e0 + __builtin_ctzll(m);
+          break;
+        }
+      }
+      it.expert = uniform(it.expert);
+      in -= uniform(s.start[it.expert]);
+      count = uniform(s.count[it.expert]);
+    }
+    it.block = in % a.blocks;
+    it.first = in / a.blocks * TILE;
+    it.rows = min(TILE, count - it.first);
+    int before = -it.first;
+    for (int i0 = 0; i0 < slots; i0 += 64) {
+      const int i = i0 + lane;
+      const bool here = few ? id == it.expert : i < slots && a.ids[i] == it.expert;
       const uint64_t all = __ballot(here);
-      const int at = before + __builtin_popcountll(all & ((1ull << tid) - 1)) - first;
-      if (here && at >= 0 && at < rows) s.rows[at] = i;
+      const int at = before + __builtin_popcountll(all & ((1ull << lane) - 1));
+      if (here && at >= 0 && at < it.rows) s.rows[wave][at] = i;
       before += __builtin_popcountll(all);
+      if (before >= it.rows) break;
     }
+    return it;
   }
-  __syncthreads();
-  return rows;
-}
+};
 
-// Sums over this wave's steps of the split, for 16 MT rows.
+// Sums over this wave's steps of the item's part of K: steps first, first + stride, ... before end.
 template <class Weights, int MT, bool SECOND>
-__device__ __forceinline__ void stream_weights(const MoeShared& s, const Experts& a, const Weights& w, int expert, int nb, int rows, int split,
+__device__ __forceinline__ void stream_weights(const int* rows, int n, const Experts& a, const Weights& w, int64_t matrix, int step, int stride, int end,
                                                f32x4 (&acc)[MT][8]) {
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
   uint32_t xo[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int r = 16 * m + (lane & 15), slot = s.rows[r < rows ? r : 0];
+    const int r = 16 * m + (lane & 15), slot = rows[r < n ? r : 0];
     xo[m] = (uint32_t)(((int64_t)(SECOND ? slot : slot / a.k) * a.K + Weights::x_lane()) * 2);
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const int64_t matrix = Weights::matrix(a);
-  const char* base = a.W + (int64_t)expert * nb * matrix;
-  const char* sbase = a.scales + (int64_t)expert * nb * (matrix / 16);
-  const int all = (a.K + Weights::STEP - 1) / Weights::STEP, end = min(all, (split + 1) * a.per);
-  typename Weights::template Regs<MT> p, q;
-  int step = split * a.per + wave;
-  if (step >= end) return;
-  w.template load<MT>(p, base, sbase, a.X, xo, a, step);
-  for (;;) {
-    const int next = step + kWaves;
-    if (next < end) w.template load<MT>(q, base, sbase, a.X, xo, a, next);
-    w.template multiply<MT>(p, acc, a, step);
-    if (next >= end) break;
-    step = next + kWaves;
-    if (step < end) w.template load<MT>(p, base, sbase, a.X, xo, a, step);
-    w.template multiply<MT>(q, acc, a, next);
-    if (step >= end) break;
-  }
-}
-
-// Z = act(X W1) of the item's rows.
-template <class Weights, int ACT, int MT>
-__device__ __forceinline__ void run_first(MoeShared& s, const Experts& a, int expert, int block, int rows) {
-  constexpr bool GATED = ACT == ACT_SWIGLU;
-  constexpr int COLS = GATED ? 64 : 128;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = block * COLS;
-  const Weights w(a, col0, GATED ? Weights::matrix(a) : 0);
-  f32x4 acc[MT][8];
-  stream_weights<Weights, MT, false>(s, a, w, expert, GATED ? 2 : 1, rows, 0, acc);
+  const char* base = a.W + matrix * Weights::matrix(a);
+  const char* sbase = a.scales + matrix * (Weights::matrix(a) / 16);
+  // A ring of steps in registers: while one is multiplied the others are in flight.  What is requested behind the last step arrives
+  // as zeros, so that every request is unconditional and the waits count the same loads on every path.
+  constexpr int D = Weights::RING;
+  typename Weights::template Regs<MT> ring[D];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    if (16 * m >= rows) break;
-    if (m) __syncthreads();
-    Weights::put(s.sums[wave][lane & 15], acc[m]);
-    __syncthreads();
-    const int r = tid / 16, c = 8 * (tid % 16);
-    if (c < COLS && 16 * m + r < rows && col0 + c < a.N) {
-      float v[8] = {}, u[8] = {};
+  for (int d = 0; d < D - 1; ++d) w.template load<MT>(ring[d], base, sbase, a.X, xo, a, step + d * stride, end);
+  for (; step < end; step += D * stride) {
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] += s.sums[i][r][c + e];
-          if (GATED) u[e] += s.sums[i][r][64 + c + e];
-        }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = GATED ? silu(v[e]) * u[e] : ACT == ACT_GELU_TANH ? gelu_tanh(v[e]) : v[e];
-      *reinterpret_cast<u32x4*>(a.out + (int64_t)s.rows[16 * m + r] * a.N + col0 + c) = pack_bf16x8(v);
+    for (int d = 0; d < D; ++d) {
+      w.template load<MT>(ring[(d + D - 1) % D], base, sbase, a.X, xo, a, step + (d + D - 1) * stride, end);
+      __builtin_amdgcn_sched_barrier(0);
+      w.template multiply<MT>(ring[d], acc, a, step + d * stride);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
 
-// The item's part of Z W2, to memory; then, for every token of which this was the last part, Y.
-template <class Weights, int MT>
-__device__ __forceinline__ void run_second(MoeShared& s, const Experts& a, int expert, int block, int split, int rows) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = block * 128;
-  const Weights w(a, col0, 0);
+template <int ACT>
+__device__ __forceinline__ u32x4 activate(const float (&v)[8], const float (&u)[8]) {
+  float z[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = ACT == ACT_SWIGLU ? silu(v[e]) * u[e] : ACT == ACT_GELU_TANH ? gelu_tanh(v[e]) : v[e];
+  return pack_bf16x8(z);
+}
+
+// Z = act(X W1) of the item's rows.  With a gate two waves stream the columns' first matrix and two the second.
+template <class Weights, int ACT, int MT, int TILE>
+__device__ __forceinline__ void run_first(MoeShared& s, const Experts& a, const Items<TILE>& items, const Item& it) {
+  constexpr bool GATED = ACT == ACT_SWIGLU;
+  constexpr int NB = GATED ? 2 : 1, SHARE = kWaves / NB;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = it.block * 128;
+  const int* rows = s.rows[wave];
+  const Weights w(a, col0);
   f32x4 acc[MT][8];
-  stream_weights<Weights, MT, true>(s, a, w, expert, 1, rows, split, acc);
+  const int from = it.split * items.per, end = min(a.steps, from + items.per);
+  stream_weights<Weights, MT, false>(rows, it.rows, a, w, (int64_t)it.expert * NB + wave / SHARE, from + wave % SHARE, SHARE, end, acc);
+  const int r = tid / 16, c = 8 * (tid % 16);
+  const bool inside = col0 + c < a.N;
   const int64_t slots = (int64_t)a.T * a.k;
+  const Far part(a.part);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    if (16 * m >= rows) break;
-    if (m) __syncthreads();
+    if (16 * m >= it.rows) break;
+    __syncthreads();
+    Weights::put(s.sums[wave][lane & 15], acc[m]);
+    __syncthreads();
+    if (16 * m + r < it.rows && inside) {
+      float v[8] = {}, u[8] = {};
+#pragma unroll
+      for (int i = 0; i < SHARE; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] += s.sums[i][r][c + e];
+          if (GATED) u[e] += s.sums[SHARE + i][r][c + e];
+        }
+      const int slot = rows[16 * m + r];
+      if (items.splits == 1) {
+        *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col0 + c) = activate<ACT>(v, u);
+      } else {
+        const uint32_t to = (uint32_t)((it.split * slots + slot) * NB * a.N + col0 + c) * 4;
+        part.store16(to, f32x4{v[0], v[1], v[2], v[3]});
+        part.store16(to + 16, f32x4{v[4], v[5], v[6], v[7]});
+        if (GATED) {
+          part.store16(to + 4 * a.N, f32x4{u[0], u[1], u[2], u[3]});
+          part.store16(to + 4 * a.N + 16, f32x4{u[4], u[5], u[6], u[7]});
+        }
+      }
+    }
+  }
+  if (items.splits == 1) return;
+  // The part that arrives last adds all of them, in the order 0, 1, ...
+  wait_all_mem();
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t* count = a.arrived + (int64_t)rows[0] * a.blocks + it.block;
+    const bool last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(items.splits - 1);
+    if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
+    s.last = last;
+  }
+  __syncthreads();
+  if (!uniform(s.last)) return;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    if (16 * m + r >= it.rows || !inside) continue;
+    const int slot = rows[16 * m + r];
+    const uint32_t first = (uint32_t)(slot * (int64_t)NB * a.N + col0 + c) * 4, pitch = (uint32_t)(slots * NB * a.N * 4);
+    float v[8] = {}, u[8] = {};
+    for (int q = 0; q < items.splits; q += 4) {
+      f32x4 x[4][2 * NB];
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i) x[d][i] = part.load16(first + min(q + d, items.splits - 1) * pitch + (i / 2) * 4 * a.N + 16 * (i % 2));
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] += q + d < items.splits ? x[d][e / 4][e % 4] : 0.f;
+          if (GATED) u[e] += q + d < items.splits ? x[d][2 * NB - 2 + e / 4][e % 4] : 0.f;
+        }
+    }
+    *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col0 + c) = activate<ACT>(v, u);
+  }
+}
+
+// The item's part of Z W2, to memory; then, for every token of which this was the last part, Y.
+template <class Weights, int MT, int TILE>
+__device__ __forceinline__ void run_second(MoeShared& s, const Experts& a, const Items<TILE>& items, const Item& it) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = it.block * 128;
+  const int* rows = s.rows[wave];
+  const Weights w(a, col0);
+  f32x4 acc[MT][8];
+  const int from = it.split * items.per, end = min(a.steps, from + items.per);
+  stream_weights<Weights, MT, true>(rows, it.rows, a, w, it.expert, from + wave, kWaves, end, acc);
+  const int64_t slots = (int64_t)a.T * a.k;
+  const Far part(a.part);
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    if (16 * m >= it.rows) break;
+    __syncthreads();
     Weights::put(s.sums[wave][lane & 15], acc[m]);
     __syncthreads();
     const int r = tid / 16, c = 8 * (tid % 16);
-    if (16 * m + r < rows && col0 + c < a.N) {
+    if (16 * m + r < it.rows && col0 + c < a.N) {
       float v[8] = {};
 #pragma unroll
       for (int i = 0; i < kWaves; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += s.sums[i][r][c + e];
-      float* to = a.part + ((int64_t)split * slots + s.rows[16 * m + r]) * a.N + col0 + c;
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) store_far(to + e, v[e], v[e + 1]);
+      const int slot = rows[16 * m + r];
+      const float gate = a.gates[slot];
+      const uint32_t to = (uint32_t)((it.split * slots + slot) * a.N + col0 + c) * 4;
+      part.store16(to, f32x4{gate * v[0], gate * v[1], gate * v[2], gate * v[3]});
+      part.store16(to + 16, f32x4{gate * v[4], gate * v[5], gate * v[6], gate * v[7]});
     }
+  }
+  // Every slot's part counts for its token; the part that completes the count finds all of them in memory.
+  int t = 0;
+  uint32_t valid = 0;  // the token's slots that have an expert
+  if (tid < it.rows) {
+    t = rows[tid] / a.k;
+    int e[kMostChosen];
+#pragma unroll
+    for (int j = 0; j < kMostChosen; ++j) e[j] = a.ids[t * a.k + min(j, a.k - 1)];
+#pragma unroll
+    for (int j = 0; j < kMostChosen; ++j) valid |= j < a.k && e[j] >= 0 && e[j] < a.E ? 1u << j : 0u;
   }
   wait_all_mem();
   if (tid == 0) s.found = 0;
   __syncthreads();
-  // Every slot's part counts for its token; the part that completes the count finds all of them in memory.
-  if (tid < rows) {
-    const int t = s.rows[tid] / a.k;
-    int valid = 0;
-    for (int j = 0; j < a.k; ++j) {
-      const int e = a.ids[t * a.k + j];
-      valid += e >= 0 && e < a.E;
-    }
-    uint32_t* count = a.arrived + (int64_t)t * a.blocks + block;
-    if (__hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(valid * a.splits - 1)) {
+  if (tid < it.rows) {
+    uint32_t* count = a.arrived + (int64_t)t * a.blocks + it.block;
+    if (__hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(__builtin_popcount(valid) * items.splits - 1)) {
       __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
-      s.done[atomicAdd(&s.found, 1)] = t;
+      const int at = atomicAdd(&s.found, 1);
+      s.done[at] = t;
+      s.valid[at] = valid;
     }
   }
   __syncthreads();
   const int found = uniform(s.found), c = col0 + 4 * (tid % 32);
   if (c < a.N)
     for (int i = tid / 32; i < found; i += 8) {
-      const int t = s.done[i];
+      const int token = s.done[i];
+      const uint32_t mask = s.valid[i], pitch = (uint32_t)(slots * a.N * 4);
+      // terms: slots in order, a slot's parts of K in order; eight in flight
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
-      for (int j = 0; j < a.k; ++j) {
-        const int e = a.ids[t * a.k + j];
-        if (e < 0 || e >= a.E) continue;
-        const float gate = a.gates[t * a.k + j];
-        const float* p = a.part + ((int64_t)t * a.k + j) * a.N + c;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int q = 0; q < a.splits; ++q) {
-          const f32x2 lo = load_far(p + q * slots * a.N), hi = load_far(p + q * slots * a.N + 2);
-          sum[0] += lo[0], sum[1] += lo[1], sum[2] += hi[0], sum[3] += hi[1];
+      const int terms = a.k * items.splits;
+      for (int n = 0; n < terms; n += 8) {
+        f32x4 v[8];
+        bool there[8];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const int term = min(n + d, terms - 1), j = term / items.splits, q = term - j * items.splits;
+          there[d] = n + d < terms && (mask >> j & 1);
+          v[d] = part.load16(there[d] ? (uint32_t)((token * a.k + j) * a.N + c) * 4 + q * pitch : 0u);
         }
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) y[i4] = __builtin_fmaf(gate, sum[i4], y[i4]);
+        for (int d = 0; d < 8; ++d)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) y[i4] += there[d] ? v[d][i4] : 0.f;
       }
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       bf16x4 b;
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) b[i4] = (__bf16)y[i4];
-      *reinterpret_cast<bf16x4*>(a.out + (int64_t)t * a.N + c) = b;
+      *reinterpret_cast<bf16x4*>(a.out + (int64_t)token * a.N + c) = b;
     }
 }
 
 // MOST: the most blocks of 16 rows that an item has.
 template <class Weights, int ACT, int MOST>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_moe_first(const Experts a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MOST == 1 ? 3 : 2))) void k_moe_first(const Experts a) {
   __shared__ MoeShared s;
-  place_items(s, a, 16 * MOST);
-  const int total = uniform(s.total);
-  for (int item = blockIdx.x; item < total; item += gridDim.x) {
-    int expert, block, split;
-    const int rows = find_rows(s, a, item, 16 * MOST, expert, block, split);
-    if (MOST == 1 || rows <= 16) run_first<Weights, ACT, 1>(s, a, expert, block, rows);
-    else if (MOST > 2 && rows <= 32) run_first<Weights, ACT, 2>(s, a, expert, block, rows);
-    else run_first<Weights, ACT, MOST>(s, a, expert, block, rows);
+  const Items<16 * MOST> items(s, a);
+  for (int n = blockIdx.x; n < items.total(); n += gridDim.x) {
+    const Item it = items.find(s, a, n);
+    if (MOST == 1 || it.rows <= 16) run_first<Weights, ACT, 1>(s, a, items, it);
+    else if (MOST > 2 && it.rows <= 32) run_first<Weights, ACT, 2>(s, a, items, it);
+    else run_first<Weights, ACT, MOST>(s, a, items, it);
   }
 }
 
 template <class Weights, int MOST>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_moe_second(const Experts a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MOST == 1 ? 3 : 2))) void k_moe_second(const Experts a) {
   __shared__ MoeShared s;
-  place_items(s, a, 16 * MOST);
+  const Items<16 * MOST> items(s, a);
+  for (int n = blockIdx.x; n < items.total(); n += gridDim.x) {
+    const Item it = items.find(s, a, n);
+    if (MOST == 1 || it.rows <= 16) run_second<Weights, 1>(s, a, items, it);
+    else if (MOST > 2 && it.rows <= 32) run_second<Weights, 2>(s, a, items, it);
+    else run_second<Weights, MOST>(s, a, items, it);
+  }
   // rows of tokens without an expert
   for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
     int valid = 0;
@@ -539,14 +714,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
     if (valid == 0)
       for (int c = 8 * threadIdx.x; c < a.N; c += 8 * 256) *reinterpret_cast<u32x4*>(a.out + (int64_t)t * a.N + c) = u32x4{0, 0, 0, 0};
-  }
-  const int total = uniform(s.total);
-  for (int item = blockIdx.x; item < total; item += gridDim.x) {
-    int expert, block, split;
-    const int rows = find_rows(s, a, item, 16 * MOST, expert, block, split);
-    if (MOST == 1 || rows <= 16) run_second<Weights, 1>(s, a, expert, block, split, rows);
-    else if (MOST > 2 && rows <= 32) run_second<Weights, 2>(s, a, expert, block, split, rows);
-    else run_second<Weights, MOST>(s, a, expert, block, split, rows);
   }
 }
 
@@ -562,8 +729,7 @@ struct mlp2_moe_s {
   float* part = nullptr;
   int64_t part_floats = 0;
   double* logits = nullptr;
-  int64_t logit_parts = 1;
-  uint32_t *arrived = nullptr, *routed = nullptr;
+  uint32_t *arrived = nullptr, *joined = nullptr, *routed = nullptr;
 };
 
 namespace {
@@ -571,20 +737,21 @@ namespace {
 int status(hipError_t e) { return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP); }
 
 constexpr int kRouteTokens = 8;
+constexpr int kMostParts = 16;  // of K
+// K of a part of the router: 16 parts, of 64 to 512 each (more than 16 only for H > 8192).
+int route_part(int64_t H) {
+  const int64_t per = round_up((H + 15) / 16, 64);
+  return (int)(per > kRoutePart ? kRoutePart : per);
+}
 
 template <class W>
 hipError_t route(const mlp2_moe_s* p, int64_t T, const void* X, const void* Wr, int32_t* ids, float* gates, hipStream_t s) {
   Route a{(const uint16_t*)X, Wr, p->logits, p->routed, ids, gates, (int)T, (int)p->H, p->E, p->k, 1, 0, 1};
   while (a.width < p->E && a.width < 256) a.width *= 2;
   const int tokens = T == 1 ? 1 : kRouteTokens;
-  const int64_t groups = (T + tokens - 1) / tokens, units = p->H / 64;
-  int64_t splits = p->num_cus / groups;
-  if (splits > p->logit_parts) splits = p->logit_parts;
-  if (splits > units) splits = units;
-  if (splits < 1) splits = 1;
-  const int64_t per = (units + splits - 1) / splits;
-  a.per = (int)per * 64;
-  a.splits = (int)((units + per - 1) / per);
+  const int64_t groups = (T + tokens - 1) / tokens;
+  a.per = route_part(p->H);
+  a.splits = (int)((p->H + a.per - 1) / a.per);
   const dim3 grid((unsigned)groups, (unsigned)a.splits);
   if (tokens == 1) k_moe_route<W, 1><<<grid, 256, 0, s>>>(a);
   else k_moe_route<W, kRouteTokens><<<grid, 256, 0, s>>>(a);
@@ -601,48 +768,42 @@ template <class Weights>
 hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t* ids, const float* gates, const void* W1, const void* W1s, const void* W2,
                    const void* W2s, void* Y, hipStream_t s) {
   const int64_t slots = T * p->k, active = slots < p->E ? slots : p->E;  // experts that have a slot, at most
-  auto grid_of = [&](const Experts& a) {
-    const int64_t tile = T <= 16 ? 16 : 16 * Weights::MOST, most = (active + slots / tile) * a.blocks * a.splits, slots_of_chip = 4ll * p->num_cus;
-    return (unsigned)(most < slots_of_chip ? most : slots_of_chip);
+  const int64_t resident = (T <= 16 ? 3ll : 2ll) * p->num_cus;            // work-groups that the chip holds at once (by their registers)
+  auto fill = [&](Experts& a, int64_t K, int64_t N, int64_t width) {      // width: floats of a slot's part
+    const int64_t tile = T <= 16 ? 16 : 16 * Weights::MOST, room = p->part_floats / (slots * width);
+    a.K = (int)K;
+    a.N = (int)N;
+    a.blocks = (int)((N + 127) / 128);
+    a.steps = (int)((K + Weights::STEP - 1) / Weights::STEP);
+    a.most = (int)(room < 1 ? 1 : room > kMostParts ? kMostParts : room);
+    if (a.most > a.steps / kWaves) a.most = a.steps / kWaves < 1 ? 1 : a.steps / kWaves;
+    const int64_t most = (active + slots / tile) * a.blocks * a.most;
+    return (unsigned)(most < resident ? most : resident);
   };
   Experts a{};
   a.X = (const uint16_t*)X;
   a.ids = ids;
   a.gates = gates;
-  a.W = (const char*)W1;
-  a.scales = (const char*)W1s;
-  a.out = p->Z;
   a.T = (int)T;
   a.E = p->E;
   a.k = p->k;
-  a.K = (int)p->H;
-  a.N = (int)p->F;
-  a.blocks = (int)(p->nb == 2 ? p->F / 64 : (p->F + 127) / 128);
-  a.splits = 1;
-  a.per = (int)((p->H + Weights::STEP - 1) / Weights::STEP);
-  const unsigned g1 = grid_of(a);
+  a.part = p->part;
+  Experts b = a;
+  a.W = (const char*)W1;
+  a.scales = (const char*)W1s;
+  a.out = p->Z;
+  a.arrived = p->joined;
+  const unsigned g1 = fill(a, p->H, p->F, p->nb * p->F);
   if (p->act == MLP2_ACT_SWIGLU) first<Weights, ACT_SWIGLU>(a, g1, s);
   else if (p->act == MLP2_ACT_GELU_TANH) first<Weights, ACT_GELU_TANH>(a, g1, s);
   else first<Weights, ACT_IDENTITY>(a, g1, s);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  Experts b = a;
   b.X = p->Z;
   b.W = (const char*)W2;
   b.scales = (const char*)W2s;
   b.out = (uint16_t*)Y;
-  b.part = p->part;
   b.arrived = p->arrived;
-  b.K = (int)p->F;
-  b.N = (int)p->H;
-  b.blocks = (int)((p->H + 127) / 128);
-  const int64_t steps = (p->F + Weights::STEP - 1) / Weights::STEP, room = p->part_floats / (slots * p->H);
-  int64_t splits = (4ll * p->num_cus + active * b.blocks - 1) / (active * b.blocks);
-  if (splits > room) splits = room;
-  if (splits > steps / 8) splits = steps / 8;
-  if (splits < 1) splits = 1;
-  b.per = (int)((steps + splits - 1) / splits);
-  b.splits = (int)((steps + b.per - 1) / b.per);
-  const unsigned g2 = grid_of(b);
+  const unsigned g2 = fill(b, p->F, p->H, p->H);
   if (T <= 16) k_moe_second<Weights, 1><<<g2, 256, 0, s>>>(b);
   else k_moe_second<Weights, Weights::MOST><<<g2, 256, 0, s>>>(b);
   return hipGetLastError();
@@ -706,20 +867,13 @@ mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, in
   p->device = device;
   p->num_cus = cus;
   const int64_t slots = max_tokens * k, groups = (max_tokens + kRouteTokens - 1) / kRouteTokens;
-  // room for 16 parts of K of the second product while they are small; one always fits
-  const int64_t one = slots * H, few = (int64_t)8 << 20;
-  p->part_floats = 16 * one < few ? 16 * one : one > few ? one : few;
-  p->logit_parts = cus / groups > 32 ? 32 : cus / groups > 1 ? cus / groups : 1;
+  // room for 16 parts of K of either product while they are small; one part of the second always fits
+  const int64_t wide = p->nb * F > H ? p->nb * F : H, all = kMostParts * slots * wide, few = (int64_t)16 << 20, one = slots * H;
+  p->part_floats = all < few ? all : one > few ? one : few;
   const int64_t z = round_up(slots * F * 2, 256), part = round_up(p->part_floats * 4, 256);
-  // (a call with fewer tokens may split K further, never into more than 32 parts: those of a call with one token are few)
-  int64_t logits = max_tokens * p->logit_parts * E * 8;
-  for (int64_t g = 1; g <= groups; ++g) {
-    const int64_t parts = cus / g > 32 ? 32 : cus / g > 1 ? cus / g : 1, t = g * kRouteTokens < max_tokens ? g * kRouteTokens : max_tokens;
-    if (parts * t * E * 8 > logits) logits = parts * t * E * 8;
-  }
-  p->logit_parts = 32;
-  logits = round_up(logits, 256);
-  const int64_t counters = (max_tokens * ((H + 127) / 128) + groups * kLine) * 4;
+  const int64_t logits = round_up(max_tokens * ((H + route_part(H) - 1) / route_part(H)) * E * 8, 256);
+  const int64_t tokens_blocks = max_tokens * ((H + 127) / 128), slots_blocks = slots * ((F + 127) / 128);
+  const int64_t counters = (tokens_blocks + slots_blocks + groups * kLine) * 4;
   if (hipMalloc((void**)&p->ws, (size_t)(z + part + logits + counters)) != hipSuccess ||
       hipMemset(p->ws + z + part + logits, 0, (size_t)counters) != hipSuccess ||
       hipStreamSynchronize(nullptr) != hipSuccess) {  // calls may come on any stream
@@ -734,6 +888,7 @@ mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, in
   p->logits = (double*)(p->ws + z + part);
   p->routed = (uint32_t*)(p->ws + z + part + logits);
   p->arrived = p->routed + groups * kLine;
+  p->joined = p->arrived + tokens_blocks;
   return p;
 }
 

@@ -94,6 +94,30 @@ __global__ __launch_bounds__(256) void k_mx_quantise_rows(const Quantise a) {
   }
 }
 
+// The values of codes 2 b and 2 b + 1 of a word, in bf16.
+__device__ __forceinline__ uint32_t mx_pair(uint32_t word, float unit, int b) {
+  if (b == 0) return __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 0));
+  if (b == 1) return __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 1));
+  if (b == 2) return __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 2));
+  return __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, unit, 3));
+}
+// The first n of C 16-bit values to any element's address.
+template <int C>
+__device__ __forceinline__ void store_words(uint16_t* p, int n, const uint32_t (&w)[C / 2]) {
+  if (n >= C) {
+    if constexpr (C == 8) {
+      *reinterpret_cast<u32x4_any*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+    } else {
+      typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+      *reinterpret_cast<u32x2_any*>(p) = u32x2_any{w[0], w[1]};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (i < n) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+  }
+}
+
 // Blocks down columns: X [K, N] becomes N rows of K.  A lane takes 32 of K by 16 bytes of columns, so that a block's largest element
 // is found without another lane; 8 lanes lie beside each other, 8 below, and a store of codes covers 128 bytes of 8 rows.
 template <class X>
@@ -130,35 +154,46 @@ __global__ __launch_bounds__(256) void k_mx_quantise_down(const Quantise a) {
     const uint32_t word = raw[i][C == 8 ? c / 2 : c];
     return __builtin_bit_cast(float, C == 8 ? c & 1 ? word & 0xFFFF0000u : word << 16 : word);
   };
-  uint16_t* values = a.values ? a.values + ((int64_t)m * a.rows + k0) * a.cols + col : nullptr;
+  u32x4 q[C];
+  float unit[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     uint32_t largest = 0;
 #pragma unroll
     for (int i = 0; i < kMxBlock; ++i) largest = max(largest, magnitude(value(i, c)));
     const uint32_t s = mx_scale(largest);
-    u32x4 q;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = value(8 * j + e, c);
-      q[j] = mx_codes(v, s);
+      q[c][j] = mx_codes(v, s);
     }
+    unit[c] = mx_unit(s);
     if (c < left) {
       const int64_t row = (int64_t)m * a.cols + col + c;
-      *reinterpret_cast<u32x4*>(a.codes + row * (kp / 2) + block * 16) = q;
+      *reinterpret_cast<u32x4*>(a.codes + row * (kp / 2) + block * 16) = q[c];
       a.scales[(((int64_t)m * (kp / kMxGroup) + block / 4) * a.cols + col + c) * 4 + block % 4] = (uint8_t)s;
-      if (values) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 v = mx_values(q[j], s);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (8 * j + e < deep) values[(int64_t)(8 * j + e) * a.cols + c] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
-        }
-      }
     }
+  }
+  if (!a.values) return;
+  // Two rows of X at a time: a conversion gives two neighbours of a column, a byte permute two columns of a row.
+  uint16_t* values = a.values + ((int64_t)m * a.rows + k0) * a.cols + col;
+#pragma unroll
+  for (int i = 0; i < kMxBlock; i += 2) {
+    uint32_t v[C], lo[C / 2], hi[C / 2];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint32_t word = q[c][i / 8];
+      v[c] = mx_pair(word, unit[c], i / 2 % 4);
+    }
+#pragma unroll
+    for (int c = 0; c < C; c += 2) {
+      lo[c / 2] = __builtin_amdgcn_perm(v[c + 1], v[c], 0x05040100u);
+      hi[c / 2] = __builtin_amdgcn_perm(v[c + 1], v[c], 0x07060302u);
+    }
+    if (i < deep) store_words<C>(values + (int64_t)i * a.cols, left, lo);
+    if (i + 1 < deep) store_words<C>(values + (int64_t)(i + 1) * a.cols, left, hi);
   }
 }
 
@@ -245,8 +280,7 @@ int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const 
                                                            : Span{X, ((count - 1) * matrix_stride + (rows - 1) * ldx + cols) * size};
   const Span in[] = {x}, outs[] = {{codes, count * out * kp / 2}, {scales, count * out * kp / kMxBlock}, {values, values ? count * rows * cols * 2 : 0}};
   if (outputs_overlap(in, outs)) return record_error(MLP2_ERR_INVALID_ARG);
-  int device, cus;
-  if (const int rc = current_device(&device, &cus)) return record_error(rc);
+  if (const int rc = usable_device()) return record_error(rc);
   Quantise a{X, ldx, matrix_stride, (uint8_t*)codes, (uint8_t*)scales, (uint16_t*)values, (int)rows, (int)cols, 0, 0};
   if (down) {
     a.across = (int)((cols * size + 511) / 512);

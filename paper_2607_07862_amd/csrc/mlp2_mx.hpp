@@ -29,6 +29,12 @@ constexpr int kMxBlock = 32;   // elements that share a scale
 constexpr int kMxGroup = 128;  // elements whose scales share a word
 __host__ __device__ constexpr int64_t mx_padded(int64_t k) { return (k + kMxGroup - 1) / kMxGroup * kMxGroup; }
 
+typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+// A scale as the float that the conversion instructions take (2^-127 is a subnormal one).
+__device__ __forceinline__ float mx_unit(uint32_t s) {
+  return __builtin_bit_cast(float, s == 0 ? 0x00400000u : s == 255 ? 0x7FC00000u : s << 23);
+}
+
 constexpr int kFp4 = 4;  // the operand format of the scaled matrix instruction
 
 // c += W X for 16 columns (w) by 16 rows (x) and 128 of K; the scales of this lane's 32 are bytes BW of sw and BX of sx.
