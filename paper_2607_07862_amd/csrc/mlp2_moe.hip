@@ -12,6 +12,7 @@
 // itself, from ids (at most 8192 words), and finds the items of work from that: an item is an expert with at least one slot, up to
 // 16 MT of its rows, a block of columns and a part of K.
 #include <new>
+#include <type_traits>
 
 #include "mlp2_host.h"
 #include "mlp2_mx.hpp"
@@ -44,6 +45,11 @@ struct Far {
   }
 };
 
+// dma16_buffer for what is read once.
+__device__ __forceinline__ void dma16_stream(u32x4 rsrc, uint32_t voff, uint32_t lds_addr) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen nt lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds_addr) : "memory");
+}
+
 // ------------------------------------------------------------------ router
 
 struct Route {
@@ -60,6 +66,27 @@ struct Route {
 __device__ __forceinline__ double widen(uint16_t v) { return (double)__builtin_bit_cast(float, (uint32_t)v << 16); }
 __device__ __forceinline__ double widen(float v) { return (double)v; }
 
+// The largest of a wave's values, in a scalar register: inside rows of 16 lanes by data-parallel moves, then across the four rows.
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+  const u32x2 w = __builtin_bit_cast(u32x2, v);
+  const u32x2 m = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, 0xF, 0xF, true), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, 0xF, 0xF, true)};
+  return __builtin_bit_cast(double, m);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const u32x2 w = __builtin_bit_cast(u32x2, v);
+  const u32x2 m = {(uint32_t)__builtin_amdgcn_readlane((int)w[0], lane), (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane)};
+  return __builtin_bit_cast(double, m);
+}
+__device__ __forceinline__ double largest_of(double a, double b) { return a > b ? a : b; }
+__device__ __forceinline__ double wave_largest(double v) {
+  v = largest_of(v, moved<0xB1>(v));   // quad_perm 1 0 3 2
+  v = largest_of(v, moved<0x4E>(v));   // quad_perm 2 3 0 1
+  v = largest_of(v, moved<0x141>(v));  // row_half_mirror
+  v = largest_of(v, moved<0x140>(v));  // row_mirror
+  return largest_of(largest_of(lane_value(v, 0), lane_value(v, 16)), largest_of(lane_value(v, 32), lane_value(v, 48)));
+}
+
 // The k largest of a token's logits (in LDS; ties: the lowest index; NaN counts as the largest) and the softmax over them, by one wave.
 __device__ __forceinline__ void choose_experts(const double* logits, int E, int k, int32_t* ids, float* gates) {
   const int lane = threadIdx.x & 63;
@@ -71,33 +98,27 @@ __device__ __forceinline__ void choose_experts(const double* logits, int E, int 
     v[i] = e < E ? logits[e] : 0.0;
     if (v[i] != v[i]) v[i] = __builtin_huge_val();
   }
-  uint32_t gone = 0;  // of this lane's experts, those that are chosen already
+  uint32_t gone = 0;  // of this lane's experts, those that are chosen already or do not exist
+#pragma unroll
+  for (int i = 0; i < PER; ++i) gone |= lane + 64 * i >= E ? 1u << i : 0u;
   int mine = 0;
   for (int j = 0; j < k; ++j) {
     double best = -__builtin_huge_val();
-    int at = kMostExperts;
+    int at = kMostExperts;  // this lane's best expert
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = lane + 64 * i;
-      if (e < E && !(gone >> i & 1) && (v[i] > best || at == kMostExperts)) {
+    for (int i = 0; i < PER; ++i)
+      if (!(gone >> i & 1) && (v[i] > best || at == kMostExperts)) {
         best = v[i];
-        at = e;
+        at = lane + 64 * i;
       }
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const double other = __shfl_xor(best, d);
-      const int other_at = __shfl_xor(at, d);
-      if (other > best || (other == best && other_at < at)) {
-        best = other;
-        at = other_at;
-      }
-    }
-    if ((at & 63) == lane) gone |= 1u << (at >> 6);
-    if (lane == j) mine = at;
+    const double top = wave_largest(best);
+    int chosen = kMostExperts;
+    for (uint64_t m = __ballot(best == top && at < kMostExperts); m; m &= m - 1) chosen = min(chosen, __builtin_amdgcn_readlane(at, __builtin_ctzll(m)));
+    if ((chosen & 63) == lane) gone |= 1u << (chosen >> 6);
+    if (lane == j) mine = chosen;
   }
   // lane j: the j-th expert; the exponentials' sum is at least 1
-  const double top = logits[__shfl(mine, 0)];
+  const double top = logits[uniform(__builtin_amdgcn_readlane(mine, 0))];
   float e = 0.f;
   if (lane < k) e = __builtin_amdgcn_exp2f((float)((logits[mine] - top) * 1.4426950408889634));
   float sum = e;
@@ -117,7 +138,7 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
   constexpr int MOST = TT * kMostExperts > TT * kRoutePart ? TT * kMostExperts : TT * kRoutePart;
   __shared__ __align__(16) double lds[256 * TT > MOST ? 256 * TT : MOST];
   __shared__ int seen;
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = 16;
   const int tid = threadIdx.x, t0 = blockIdx.x * TT, split = blockIdx.y;
   const int sub = tid / a.width, subs = 256 / a.width, e0 = tid % a.width;
   const int from = split * a.per, deep = min(a.H - from, a.per);
@@ -208,18 +229,30 @@ struct Experts {
   float* part;         // parts of K: first [splits, T k, nb, N], second [splits, T k, N] with the gates applied; below 4 GB
   uint32_t* arrived;   // zero between launches; first: one counter for each slot and block of columns, second: for each token and block
   int T, E, k, K, N;
-  int blocks;          // of 128 columns
-  int steps;           // of K, of a wave
+  int blocks;          // of columns
+  int steps;           // of K
+  int item;            // what an item costs beside its steps, in steps
   int most;            // parts of K
+};
+
+// An item of work: up to `tile` slots of an expert, a block of columns, a part of K.
+struct Item {
+  int expert, block, split, first, rows;
+  int* slots;  // `rows` of them
 };
 
 // Weights as they lie in the rest of the library, [K, N] in bf16.  A lane loads 8 columns of 8 consecutive k; taken by columns,
 // with one byte permute for each pair, those are the 8 operands (16 columns, 8 k a lane) of eight instructions, the columns of
 // instruction j being j, 8 + j, 16 + j, ...
 struct Bf16Weights {
-  static constexpr int STEP = 32;  // K of a step
+  static constexpr int STEP = 32;  // K of a step (of one wave)
+  static constexpr int ITEM = 8;   // what an item costs beside its steps
   static constexpr int MOST = 4;   // blocks of 16 rows that one pass over the weights serves
+  static constexpr int WAVES = kWaves;
   static constexpr int RING = 2;   // steps in registers
+  static constexpr int cols(bool) { return 128; }     // result columns of an item
+  static constexpr int UP_WAVE = 2, UP_COL = 0;       // where the second matrix's sums are
+  static constexpr int resident(int most) { return most == 1 ? 3 : 2; }  // work-groups of a CU, by their registers
   template <int MT>
   struct Regs {
     u32x4 w[8], x[MT];
@@ -234,7 +267,7 @@ struct Bf16Weights {
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return (int64_t)a.K * a.N * 2; }
   template <int MT>
   // Steps from `end` on load zeros, from nowhere.
-  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const char*, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step, int end) const {
+  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step, int end) const {
     const int range = step < end ? -1 : 0;
     const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + (int64_t)step * STEP * a.N * 2), 0, range, 0x00027000);
     const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, range, 0x00027000);
@@ -243,9 +276,8 @@ struct Bf16Weights {
 #pragma unroll
     for (int m = 0; m < MT; ++m) r.x[m] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)xo[m], 0, 0);
   }
-  __device__ static __forceinline__ int x_lane() { return 8 * ((threadIdx.x & 63) >> 4); }  // this lane's first k
   template <int MT>
-  __device__ __forceinline__ void multiply(const Regs<MT>& r, f32x4 (&acc)[MT][8], const Experts&, int) const {
+  __device__ __forceinline__ void multiply(const Regs<MT>& r, f32x4 (&acc)[MT][8]) const {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       u32x4 f;
@@ -253,6 +285,38 @@ struct Bf16Weights {
       for (int d = 0; d < 4; ++d) f[d] = __builtin_amdgcn_perm(r.w[2 * d + 1][j / 2], r.w[2 * d][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
       for (int m = 0; m < MT; ++m) acc[m][j] = Bf16::mfma(f, r.x[m], acc[m][j]);
+    }
+  }
+  // Sums over this wave's steps of from .. end - 1: every fourth, with a gate every second one of the wave's matrix.
+  template <int MT, bool GATED, bool SECOND>
+  __device__ static __forceinline__ void stream(const Item& it, const Experts& a, int from, int end, f32x4 (&acc)[MT][8]) {
+    constexpr int SHARE = GATED ? 2 : kWaves;
+    const Bf16Weights w(a, 128 * it.block);
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    uint32_t xo[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int r = 16 * m + (lane & 15), slot = it.slots[r < it.rows ? r : 0];
+      xo[m] = (uint32_t)(((int64_t)(SECOND ? slot : slot / a.k) * a.K + 8 * (lane >> 4)) * 2);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const char* base = a.W + ((int64_t)it.expert * (GATED ? 2 : 1) + wave / SHARE) * matrix(a);
+    // A ring of steps in registers: while one is multiplied the others are in flight.  What is requested behind the last step arrives
+    // as zeros, so that every request is unconditional and the waits count the same loads on every path.  (Four steps in place of two
+    // streamed no faster.)
+    Regs<MT> ring[RING];
+    int step = from + wave % SHARE;
+#pragma unroll
+    for (int d = 0; d < RING - 1; ++d) w.load<MT>(ring[d], base, a.X, xo, a, step + d * SHARE, end);
+    for (; step < end; step += RING * SHARE) {
+#pragma unroll
+      for (int d = 0; d < RING; ++d) {
+        w.load<MT>(ring[(d + RING - 1) % RING], base, a.X, xo, a, step + (d + RING - 1) * SHARE, end);
+        __builtin_amdgcn_sched_barrier(0);
+        w.multiply<MT>(ring[d], acc);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
   // Where the four sums of instruction j lie: columns 8 (4 g + i) + j.
@@ -272,94 +336,142 @@ struct Bf16Weights {
   }
 };
 
-// MXFP4 weights [N, K]: a lane loads the codes of 32 k of one row, 16 rows an instruction group, and turns them into bf16 operands
-// (exactly: two significant bits and a power of two), four instructions to a load.
+// MXFP4 weights [N, K], K contiguous.  A memory line is 256 k of one row, the matrix instruction's operand 8 k of 16 rows: loads
+// straight into registers would take a row's line in 64-byte pieces, and stream at 4 TB/s (pieces of a whole line: 6.9).  So the weights
+// go through LDS, and X with them: a stage is 128 rows (with a gate 64 of either matrix) by 256 k of codes, two words of scales a row
+// and 512 bytes of each X row, brought by direct-to-LDS loads of whole lines into a ring of stages.  Every wave multiplies an eighth of
+// the stage's k, all rows and columns, so that each byte leaves LDS once.  A lane turns 8 codes of a row into a bf16 operand (exactly:
+// two significant bits and a power of two).  Two waves to a SIMD: with one, which had twice the k, reads, conversions and products waited for
+// each other (3.8 TB/s).
 struct MxWeights {
-  static constexpr int STEP = 128;
+  static constexpr int WAVES = 8;
+  static constexpr int STEP = 256;  // (of all waves)
+  static constexpr int ITEM = 2;
   static constexpr int MOST = 2;
-  static constexpr int RING = 2;
-  template <int MT>
-  struct Regs {
-    u32x4 w[8], x[MT][4];
-    uint32_t s[8];
-  };
-  uint32_t off[8], soff[8];
-  __device__ __forceinline__ MxWeights(const Experts& a, int col) {
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int64_t ld = mx_padded(a.K) / 2;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int n = min(col + 16 * j + (lane & 15), a.N - 1);
-      off[j] = (uint32_t)(n * ld + 16 * g);
-      soff[j] = (uint32_t)(n * 4 + g);
-    }
-  }
+  static constexpr int resident(int) { return 1; }
+  static constexpr int cols(bool gated) { return gated ? 64 : 128; }   // result columns of an item
+  static constexpr int UP_WAVE = 0, UP_COL = 64;                       // where the second matrix's sums are
+  static constexpr int CODES = 16384, X0 = CODES + 1024;
+  static constexpr int stage(int mt) { return X0 + 8192 * mt; }
+  static constexpr int depth(int mt) { return mt == 1 ? 4 : 3; }       // stages of the ring
+  static constexpr int loads(int mt) { return 2 + 1 + mt; }            // of a wave and stage
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return a.N * (mx_padded(a.K) / 2); }
-  template <int MT>
-  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const char* s, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step, int end) const {
-    const int range = step < end ? -1 : 0;
-    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + step * 64), 0, range, 0x00027000);
-    const auto sr = __builtin_amdgcn_make_buffer_rsrc((void*)(s + (int64_t)step * a.N * 4), 0, range, 0x00027000);
-    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, range, 0x00027000);
+
+  // The stages of an item, one by one.
+  template <int MT, bool GATED, bool SECOND>
+  struct Requests {
+    const char *base, *sbase;
+    int step, rest, last, length, groups;  // the next step, how many are left, the part's last one and length
+    uint32_t wo[2], so, xo[MT];
+    __device__ __forceinline__ void begin(const Item& it, const Experts& a, int from, int to) {
+      const int lane = thread_here() & 63, wave = uniform((int)threadIdx.x >> 6), col = it.block * cols(GATED);
+      const int64_t ld = mx_padded(a.K) / 2;
+      groups = (int)(ld / 64);
+      // Blocks start at different steps of their part and come round: rows lie a multiple of 2 KB apart, so that a step's lines are all in
+      // one of an L2's channels, and work-groups that went through the steps together would all ask the same one.
+      length = to - from;
+      rest = length;
+      last = to - 1;
+      step = from + it.block % length;
+      const int64_t first = (int64_t)it.expert * (GATED ? 2 : 1) * matrix(a);
+      base = a.W + first;
+      sbase = a.scales + first / 16;
+      // Row r of the stage's 128 in its matrices (past the last column: the last).
+      auto row_of = [&](int r) { return GATED ? (r >= 64 ? a.N : 0) + min(col + (r & 63), a.N - 1) : min(col + r, a.N - 1); };
+      // codes: lane l brings 16 bytes of row l / 8 of eight
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r.s[j] = __builtin_amdgcn_raw_buffer_load_b8(sr, (int)soff[j], 0, 0);
+      for (int i = 0; i < 2; ++i) wo[i] = (uint32_t)(row_of(16 * wave + 8 * i + (lane >> 3)) * ld + 16 * chunk(lane, i));
+      // scales: a word of 64 rows, of the stage's first or second 128 k (two waves bring the same)
+      const int sr = row_of(64 * (wave & 1) + lane);
+      so = (uint32_t)(((GATED && sr >= a.N ? (int64_t)(groups - 1) * a.N : 0) + (int64_t)(wave >> 1 & 1) * a.N + sr) * 4);
+      // X: lane l brings 16 bytes of row l / 32 of two
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r.w[j] = __builtin_amdgcn_raw_buffer_load_b128(wr, (int)off[j], 0, kNt);
-    // K may end inside the last step (it is a multiple of 64): the lanes past it read the step's first k and are cleared
-    const bool past = step * STEP + 32 * (int)((threadIdx.x & 63) >> 4) >= a.K;
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) r.x[m][q] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)(xo[m] + 16 * q - (past ? 64 * ((threadIdx.x & 63) >> 4) : 0)), 0, 0);
-  }
-  __device__ static __forceinline__ int x_lane() { return 32 * ((threadIdx.x & 63) >> 4); }
-  template <int MT>
-  __device__ __forceinline__ void multiply(Regs<MT>& r, f32x4 (&acc)[MT][8], const Experts& a, int step) const {
-    if ((step + 1) * STEP > a.K) {
-      const bool past = step * STEP + x_lane() >= a.K;
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int d = 0; d < 4; ++d) r.x[m][q][d] = past ? 0u : r.x[m][q][d];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float scale = mx_unit(r.s[j]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        u32x4 f;
-        f[0] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 0));
-        f[1] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 1));
-        f[2] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 2));
-        f[3] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.w[j][q], scale, 3));
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[m][j] = Bf16::mfma(f, r.x[m][q], acc[m][j]);
+      for (int i = 0; i < MT; ++i) {
+        const int r = 2 * (wave + 8 * i) + (lane >> 5), slot = it.slots[r < it.rows ? r : 0];
+        xo[i] = (uint32_t)((int64_t)(SECOND ? slot : slot / a.k) * a.K * 2 + 16 * x_chunk(lane, wave));
       }
     }
+    // Chunk c of row r of the codes lies at c ^ (r / 2 % 8), chunk c of row r of X at c ^ (r % 16).
+    __device__ static __forceinline__ int chunk(int lane, int i) { return (lane & 7) ^ ((lane >> 4) & 3) ^ (4 * (i & 1)); }
+    __device__ static __forceinline__ int x_chunk(int lane, int wave) { return (lane & 31) ^ (2 * wave + (lane >> 5)); }
+    __device__ __forceinline__ void issue(const Experts& a, uint32_t to) {
+      const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+      const uint32_t range = rest > 0 ? 0x7FFFFFFFu : 0u;
+      const uint64_t b = (uint64_t)(base + (int64_t)step * 128), sb = (uint64_t)(sbase + (int64_t)step * a.N * 8), xb = (uint64_t)(a.X + (int64_t)step * STEP);
+      const u32x4 wr = {uniform((uint32_t)b), uniform((uint32_t)(b >> 32)), range, 0x00027000u};
+      // the last step may have 128 k only: zeros for the others' codes and scales, from past the range
+      const bool half = 2 * step + 1 >= groups;
+      const u32x4 sr = {uniform((uint32_t)sb), uniform((uint32_t)(sb >> 32)), half && (wave >> 1 & 1) ? 0u : range, 0x00027000u};
+      const u32x4 xr = {uniform((uint32_t)xb), uniform((uint32_t)(xb >> 32)), range, 0x00027000u};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) dma16_stream(wr, half && chunk(lane, i) >= 4 ? 0x80000000u : wo[i], uniform(to + 2048u * wave + 1024 * i));
+      dma4_buffer(sr, so, uniform(to + CODES + 256u * (wave & 3)));
+      const int deep = (a.K - step * STEP) / 8;  // chunks of X that exist
+#pragma unroll
+      for (int i = 0; i < MT; ++i) dma16_buffer<5>(xr, x_chunk(lane, wave) >= deep ? 0x80000000u : xo[i], uniform(to + X0 + 1024u * (wave + 8 * i)));
+      step = step == last ? step + 1 - length : step + 1;
+      --rest;
+    }
+  };
+
+  // One stage: this wave's 32 k of it, which are one block of every row; the first HERE blocks of rows.  Everything that the stage
+  // holds for this lane is read before the first product.
+  template <int MT, int HERE>
+  __device__ static __forceinline__ void multiply(const char* stage, f32x4 (&acc)[MT][8]) {
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
+    const char* codes = stage + 128 * i16 + 16 * (wave ^ (i16 >> 1)) + 4 * g;
+    const char* scales = stage + CODES + 512 * (wave >> 2) + 4 * i16 + (wave & 3);
+    u32x4 x[HERE];
+    uint32_t c[8], sc[8];
+#pragma unroll
+    for (int m = 0; m < HERE; ++m) x[m] = *reinterpret_cast<const u32x4*>(stage + X0 + 512 * i16 + 8192 * m + 16 * ((4 * wave + g) ^ i16));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      c[j] = *reinterpret_cast<const uint32_t*>(codes + 2048 * j);
+      sc[j] = *reinterpret_cast<const uint8_t*>(scales + 64 * j);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float scale = mx_unit(sc[j]);
+      u32x4 f;
+      f[0] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 0));
+      f[1] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 1));
+      f[2] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 2));
+      f[3] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 3));
+#pragma unroll
+      for (int m = 0; m < HERE; ++m) acc[m][j] = Bf16::mfma(f, x[m], acc[m][j]);
+    }
   }
+  // Where the four sums of instruction group j lie: columns 16 j + 4 g + i.
   __device__ static __forceinline__ void put(float* to, const f32x4 (&c)[8]) {
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + 16 * j + 4 * g) = c[j];
   }
+  __device__ static __forceinline__ void add(const float* from, f32x4 (&c)[8]) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] += *reinterpret_cast<const f32x4*>(from + 16 * j + 4 * g);
+  }
 };
 
 constexpr int kPitch = 128 + 4;  // floats of a row of sums in LDS
+template <class Weights, int RING>
 struct MoeShared {
-  float sums[kWaves][16][kPitch];
+  static constexpr int kWave = Weights::WAVES, kThreads = 64 * kWave;
+  // (4-bit weights) the ring of stages, and the slots' experts: reading those from memory would wait for every stage in flight
+  static constexpr bool kIds = RING > 0;
+  alignas(1024) char ring[RING ? RING : 16];
+  int16_t ids[kIds ? kMostSlots : 1];
+  float sum[kWaves][16][kPitch];
+  __device__ __forceinline__ float* sums(int wave, int row) { return sum[wave][row]; }
   int count[kMostExperts];  // slots of an expert
   int start[kMostExperts];  // its first unit (an expert's chunk of rows and a block of columns)
-  int rows[kWaves][64];     // slots of the item, a copy for each wave
+  int rows[2][kWave][64];  // slots of an item and of the next one, a copy for each wave
   int total, last;
   int found, done[64];      // second: tokens of the item that are complete
   uint32_t valid[64];       // and their slots that have an expert
-};
-
-// An item of work: up to `tile` slots of an expert, a block of columns, a part of K.
-struct Item {
-  int expert, block, split, first, rows;
 };
 
 // Items, from ids.  Up to 64 slots every wave keeps them in a register and goes through the experts that it finds there; beyond,
@@ -370,7 +482,8 @@ struct Items {
   bool few;
   int units, splits, per;  // per: steps of a part
   __device__ __forceinline__ static int chunks(int slots) { return (slots + TILE - 1) / TILE; }
-  __device__ __forceinline__ Items(MoeShared& s, const Experts& a) {
+  template <class Shared>
+  __device__ __forceinline__ Items(Shared& s, const Experts& a) {
     const int tid = threadIdx.x, lane = tid & 63, slots = a.T * a.k;
     few = slots <= 64;
     id = -1;
@@ -384,11 +497,13 @@ struct Items {
         left &= ~same;
       }
     } else {
-      for (int e = tid; e < a.E; e += 256) s.count[e] = 0;
+      for (int e = tid; e < a.E; e += Shared::kThreads) s.count[e] = 0;
       __syncthreads();
-      for (int i = tid; i < slots; i += 256) {
+      for (int i = tid; i < slots; i += Shared::kThreads) {
         const int e = a.ids[i];
-        if (e >= 0 && e < a.E) atomicAdd(&s.count[e], 1);
+        const bool here = e >= 0 && e < a.E;
+        if (here) atomicAdd(&s.count[e], 1);
+        if constexpr (Shared::kIds) s.ids[i] = (int16_t)(here ? e : -1);
       }
       __syncthreads();
       if (tid < 64) {
@@ -409,13 +524,13 @@ struct Items {
       __syncthreads();
       units = uniform(s.total);
     }
-    // Parts of K: as many as make the work-groups' shares alike, each item costing about two steps more than it streams.  (A CU takes in
+    // Parts of K: as many as make the work-groups' shares alike, each item costing about as much as a.item steps more than it streams.  (A CU takes in
     // at most 40 to 50 GB/s, whatever its loads in flight, so the last round of a few items is as long as a whole one.)
     int least = 0x7FFFFFFF;
     splits = 1;
     const int grid = gridDim.x;
     for (int n = 1; n <= a.most; ++n) {
-      const int rounds = (units * n + grid - 1) / grid, steps = (a.steps + n - 1) / n, cost = rounds * (steps + 2 * kWaves) + (n > 1 ? kWaves : 0);
+      const int rounds = (units * n + grid - 1) / grid, steps = (a.steps + n - 1) / n, cost = rounds * (steps + a.item) + (n > 1 ? a.item / 2 : 0);
       if (cost < least) {
         least = cost;
         splits = n;
@@ -426,12 +541,16 @@ struct Items {
     splits = (a.steps + per - 1) / per;
   }
   __device__ __forceinline__ int total() const { return units * splits; }
+  __device__ __forceinline__ int from(const Item& it) const { return it.split * per; }
+  __device__ __forceinline__ int end(const Experts& a, const Item& it) const { return min(a.steps, (it.split + 1) * per); }
 
-  // Item `n`; its slots go to s.rows[wave].
-  __device__ __forceinline__ Item find(MoeShared& s, const Experts& a, int n) const {
+  // Item `n`; its slots go to this wave's s.rows[copy].
+  template <class Shared>
+  __device__ __forceinline__ Item find(Shared& s, const Experts& a, int n, int copy) const {
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), slots = a.T * a.k;
     // consecutive items: the blocks of columns, then the next rows, then the next expert, then the next part of K
     Item it;
+    it.slots = s.rows[copy][wave];
     it.split = n / units;
     int in = n - it.split * units, count = 0;
     it.expert = 0;
@@ -466,10 +585,12 @@ struct Items {
     int before = -it.first;
     for (int i0 = 0; i0 < slots; i0 += 64) {
       const int i = i0 + lane;
-      const bool here = few ? id == it.expert : i < slots && a.ids[i] == it.expert;
+      bool here;
+      if constexpr (Shared::kIds) here = few ? id == it.expert : i < slots && s.ids[min(i, slots - 1)] == it.expert;
+      else here = few ? id == it.expert : i < slots && a.ids[i] == it.expert;
       const uint64_t all = __ballot(here);
       const int at = before + __builtin_popcountll(all & ((1ull << lane) - 1));
-      if (here && at >= 0 && at < it.rows) s.rows[wave][at] = i;
+      if (here && at >= 0 && at < it.rows) it.slots[at] = i;
       before += __builtin_popcountll(all);
       if (before >= it.rows) break;
     }
@@ -477,36 +598,22 @@ struct Items {
   }
 };
 
-// Sums over this wave's steps of the item's part of K: steps first, first + stride, ... before end.
-template <class Weights, int MT, bool SECOND>
-__device__ __forceinline__ void stream_weights(const int* rows, int n, const Experts& a, const Weights& w, int64_t matrix, int step, int stride, int end,
-                                               f32x4 (&acc)[MT][8]) {
-  const int lane = threadIdx.x & 63;
-  uint32_t xo[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int r = 16 * m + (lane & 15), slot = rows[r < n ? r : 0];
-    xo[m] = (uint32_t)(((int64_t)(SECOND ? slot : slot / a.k) * a.K + Weights::x_lane()) * 2);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  const char* base = a.W + matrix * Weights::matrix(a);
-  const char* sbase = a.scales + matrix * (Weights::matrix(a) / 16);
-  // A ring of steps in registers: while one is multiplied the others are in flight.  What is requested behind the last step arrives
-  // as zeros, so that every request is unconditional and the waits count the same loads on every path.
-  constexpr int D = Weights::RING;
-  typename Weights::template Regs<MT> ring[D];
-#pragma unroll
-  for (int d = 0; d < D - 1; ++d) w.template load<MT>(ring[d], base, sbase, a.X, xo, a, step + d * stride, end);
-  for (; step < end; step += D * stride) {
-#pragma unroll
-    for (int d = 0; d < D; ++d) {
-      w.template load<MT>(ring[(d + D - 1) % D], base, sbase, a.X, xo, a, step + (d + D - 1) * stride, end);
-      __builtin_amdgcn_sched_barrier(0);
-      w.template multiply<MT>(ring[d], acc, a, step + d * stride);
-      __builtin_amdgcn_sched_barrier(0);
+// The waves' sums of one block of rows, in LDS: four copies; of eight waves the upper ones' are added to the lower ones' first.
+template <class Weights, class Shared>
+__device__ __forceinline__ void meet(Shared& s, f32x4 (&c)[8]) {
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  __syncthreads();  // the sums before these have been read
+  if constexpr (Weights::WAVES == 2 * kWaves) {
+    if (wave >= kWaves) Weights::put(s.sums(wave - kWaves, lane & 15), c);
+    __syncthreads();
+    if (wave < kWaves) {
+      Weights::add(s.sums(wave, lane & 15), c);
+      Weights::put(s.sums(wave, lane & 15), c);
     }
+  } else {
+    Weights::put(s.sums(wave, lane & 15), c);
   }
+  __syncthreads();
 }
 
 template <int ACT>
@@ -517,35 +624,30 @@ __device__ __forceinline__ u32x4 activate(const float (&v)[8], const float (&u)[
   return pack_bf16x8(z);
 }
 
-// Z = act(X W1) of the item's rows.  With a gate two waves stream the columns' first matrix and two the second.
-template <class Weights, int ACT, int MT, int TILE>
-__device__ __forceinline__ void run_first(MoeShared& s, const Experts& a, const Items<TILE>& items, const Item& it) {
+// Z = act(X W1) of the item's rows from the waves' sums.  (With a gate the bf16 weights' waves 0 and 1 hold the first matrix's sums, 2 and
+// 3 the second's; the 4-bit ones' hold 64 columns of either.)
+template <class Weights, int ACT, int MT, int TILE, class Shared>
+__device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, f32x4 (&acc)[MT][8]) {
   constexpr bool GATED = ACT == ACT_SWIGLU;
-  constexpr int NB = GATED ? 2 : 1, SHARE = kWaves / NB;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = it.block * 128;
-  const int* rows = s.rows[wave];
-  const Weights w(a, col0);
-  f32x4 acc[MT][8];
-  const int from = it.split * items.per, end = min(a.steps, from + items.per);
-  stream_weights<Weights, MT, false>(rows, it.rows, a, w, (int64_t)it.expert * NB + wave / SHARE, from + wave % SHARE, SHARE, end, acc);
+  constexpr int NB = GATED ? 2 : 1, COLS = Weights::cols(GATED), SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : kWaves;
+  const int tid = threadIdx.x, col0 = it.block * COLS;
+  const int* rows = it.slots;
   const int r = tid / 16, c = 8 * (tid % 16);
-  const bool inside = col0 + c < a.N;
+  const bool inside = tid < 256 && c < COLS && col0 + c < a.N;
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     if (16 * m >= it.rows) break;
-    __syncthreads();
-    Weights::put(s.sums[wave][lane & 15], acc[m]);
-    __syncthreads();
+    meet<Weights>(s, acc[m]);
     if (16 * m + r < it.rows && inside) {
       float v[8] = {}, u[8] = {};
 #pragma unroll
       for (int i = 0; i < SHARE; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          v[e] += s.sums[i][r][c + e];
-          if (GATED) u[e] += s.sums[SHARE + i][r][c + e];
+          v[e] += s.sums(i, r)[c + e];
+          if (GATED) u[e] += s.sums(Weights::UP_WAVE + i, r)[Weights::UP_COL + c + e];
         }
       const int slot = rows[16 * m + r];
       if (items.splits == 1) {
@@ -598,29 +700,23 @@ __device__ __forceinline__ void run_first(MoeShared& s, const Experts& a, const 
 }
 
 // The item's part of Z W2, to memory; then, for every token of which this was the last part, Y.
-template <class Weights, int MT, int TILE>
-__device__ __forceinline__ void run_second(MoeShared& s, const Experts& a, const Items<TILE>& items, const Item& it) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col0 = it.block * 128;
-  const int* rows = s.rows[wave];
-  const Weights w(a, col0);
-  f32x4 acc[MT][8];
-  const int from = it.split * items.per, end = min(a.steps, from + items.per);
-  stream_weights<Weights, MT, true>(rows, it.rows, a, w, it.expert, from + wave, kWaves, end, acc);
+template <class Weights, int MT, int TILE, class Shared>
+__device__ __forceinline__ void finish_second(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, f32x4 (&acc)[MT][8]) {
+  const int tid = threadIdx.x, col0 = it.block * 128;
+  const int* rows = it.slots;
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     if (16 * m >= it.rows) break;
-    __syncthreads();
-    Weights::put(s.sums[wave][lane & 15], acc[m]);
-    __syncthreads();
+    meet<Weights>(s, acc[m]);
     const int r = tid / 16, c = 8 * (tid % 16);
-    if (16 * m + r < it.rows && col0 + c < a.N) {
+    if (tid < 256 && 16 * m + r < it.rows && col0 + c < a.N) {
       float v[8] = {};
 #pragma unroll
       for (int i = 0; i < kWaves; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += s.sums[i][r][c + e];
+        for (int e = 0; e < 8; ++e) v[e] += s.sums(i, r)[c + e];
       const int slot = rows[16 * m + r];
       const float gate = a.gates[slot];
       const uint32_t to = (uint32_t)((it.split * slots + slot) * a.N + col0 + c) * 4;
@@ -654,23 +750,24 @@ __device__ __forceinline__ void run_second(MoeShared& s, const Experts& a, const
   __syncthreads();
   const int found = uniform(s.found), c = col0 + 4 * (tid % 32);
   if (c < a.N)
-    for (int i = tid / 32; i < found; i += 8) {
+    for (int i = tid / 32; i < found; i += Shared::kThreads / 32) {
       const int token = s.done[i];
       const uint32_t mask = s.valid[i], pitch = (uint32_t)(slots * a.N * 4);
-      // terms: slots in order, a slot's parts of K in order; eight in flight
+      // terms: slots in order, a slot's parts of K in order; sixteen in flight
+      constexpr int AHEAD = 16;
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
       const int terms = a.k * items.splits;
-      for (int n = 0; n < terms; n += 8) {
-        f32x4 v[8];
-        bool there[8];
+      for (int n = 0; n < terms; n += AHEAD) {
+        f32x4 v[AHEAD];
+        bool there[AHEAD];
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {
+        for (int d = 0; d < AHEAD; ++d) {
           const int term = min(n + d, terms - 1), j = term / items.splits, q = term - j * items.splits;
           there[d] = n + d < terms && (mask >> j & 1);
           v[d] = part.load16(there[d] ? (uint32_t)((token * a.k + j) * a.N + c) * 4 + q * pitch : 0u);
         }
 #pragma unroll
-        for (int d = 0; d < 8; ++d)
+        for (int d = 0; d < AHEAD; ++d)
 #pragma unroll
           for (int i4 = 0; i4 < 4; ++i4) y[i4] += there[d] ? v[d][i4] : 0.f;
       }
@@ -682,30 +779,8 @@ __device__ __forceinline__ void run_second(MoeShared& s, const Experts& a, const
     }
 }
 
-// MOST: the most blocks of 16 rows that an item has.
-template <class Weights, int ACT, int MOST>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MOST == 1 ? 3 : 2))) void k_moe_first(const Experts a) {
-  __shared__ MoeShared s;
-  const Items<16 * MOST> items(s, a);
-  for (int n = blockIdx.x; n < items.total(); n += gridDim.x) {
-    const Item it = items.find(s, a, n);
-    if (MOST == 1 || it.rows <= 16) run_first<Weights, ACT, 1>(s, a, items, it);
-    else if (MOST > 2 && it.rows <= 32) run_first<Weights, ACT, 2>(s, a, items, it);
-    else run_first<Weights, ACT, MOST>(s, a, items, it);
-  }
-}
-
-template <class Weights, int MOST>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MOST == 1 ? 3 : 2))) void k_moe_second(const Experts a) {
-  __shared__ MoeShared s;
-  const Items<16 * MOST> items(s, a);
-  for (int n = blockIdx.x; n < items.total(); n += gridDim.x) {
-    const Item it = items.find(s, a, n);
-    if (MOST == 1 || it.rows <= 16) run_second<Weights, 1>(s, a, items, it);
-    else if (MOST > 2 && it.rows <= 32) run_second<Weights, 2>(s, a, items, it);
-    else run_second<Weights, MOST>(s, a, items, it);
-  }
-  // rows of tokens without an expert
+// Zeros for the tokens without an expert.
+__device__ __forceinline__ void clear_idle(const Experts& a) {
   for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
     int valid = 0;
     for (int j = 0; j < a.k; ++j) {
@@ -713,8 +788,92 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MOST == 1 ?
       valid += e >= 0 && e < a.E;
     }
     if (valid == 0)
-      for (int c = 8 * threadIdx.x; c < a.N; c += 8 * 256) *reinterpret_cast<u32x4*>(a.out + (int64_t)t * a.N + c) = u32x4{0, 0, 0, 0};
+      for (int c = 8 * threadIdx.x; c < a.N; c += 8 * blockDim.x) *reinterpret_cast<u32x4*>(a.out + (int64_t)t * a.N + c) = u32x4{0, 0, 0, 0};
   }
+}
+
+// Items of bf16 weights, one after the other.  MOST: the most blocks of 16 rows that an item has; SECOND: of the second product.
+template <int ACT, int MOST, bool SECOND>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Bf16Weights::resident(MOST)))) void k_moe_bf16(const Experts a) {
+  __shared__ MoeShared<Bf16Weights, 0> s;
+  const Items<16 * MOST> items(s, a);
+  for (int n = blockIdx.x; n < items.total(); n += gridDim.x) {
+    const Item it = items.find(s, a, n, 0);
+    auto run = [&](auto mt) {
+      constexpr int MT = decltype(mt)::value;
+      f32x4 acc[MT][8];
+      Bf16Weights::stream<MT, ACT == ACT_SWIGLU && !SECOND, SECOND>(it, a, items.from(it), items.end(a, it), acc);
+      if constexpr (SECOND) finish_second<Bf16Weights, MT>(s, a, items, it, acc);
+      else finish_first<Bf16Weights, ACT, MT>(s, a, items, it, acc);
+    };
+    if (MOST == 1 || it.rows <= 16) run(int_constant<1>());
+    else if (MOST > 2 && it.rows <= 32) run(int_constant<2>());
+    else run(int_constant<MOST>());
+  }
+  if constexpr (SECOND) clear_idle(a);
+}
+
+// Items of 4-bit weights.  A work-group has most of a CU's LDS to itself, so nothing else would stream while it ends an item: its
+// requests run on into the next item's stages.  An item with fewer stages than are in flight is filled up with empty ones, so that
+// requests are never more than one item ahead.
+template <int ACT, int MT, bool SECOND>
+__global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
+  using W = MxWeights;
+  constexpr int NS = W::depth(MT), STAGE = W::stage(MT);
+  constexpr bool GATED = ACT == ACT_SWIGLU && !SECOND;
+  __shared__ MoeShared<W, STAGE * NS> s;
+  const Items<16 * MT> items(s, a);
+  const int total = items.total();
+  if ((int)blockIdx.x < total) {
+    int ahead = blockIdx.x, copy = 0, left;  // the item that is being requested; its stages left
+    Item next = items.find(s, a, ahead, copy);
+    W::Requests<MT, GATED, SECOND> ask;
+    auto begin = [&]() {
+      ask.begin(next, a, items.from(next), items.end(a, next));
+      left = max(NS - 1, ask.length);
+    };
+    begin();
+    uint32_t to = 0, at = 0;  // places of the ring: of the next request, of the next products
+    auto request = [&]() {
+      if (left == 0 && ahead + (int)gridDim.x < total) {
+        ahead += gridDim.x;
+        copy ^= 1;
+        next = items.find(s, a, ahead, copy);
+        begin();
+      }
+      ask.issue(a, (uint32_t)(uintptr_t)s.ring + to * STAGE);  // behind the last item: zeros, from nowhere
+      left = max(left - 1, 0);
+      to = to == NS - 1 ? 0 : to + 1;
+    };
+    Item it = next;
+    for (int i = 0; i < NS - 1; ++i) request();
+    for (int n = blockIdx.x; n < total; n += gridDim.x) {
+      f32x4 acc[MT][8];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int steps = items.end(a, it) - items.from(it), stages = max(NS - 1, steps);
+      for (int i = 0; i < stages; ++i) {
+        wait_vm<(NS - 2) * W::loads(MT)>();
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave holds what it read of the stage before
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        request();  // into the place of the stage before
+        if (i < steps) {
+          const char* stage = s.ring + at * STAGE;
+          if (MT == 1 || it.rows > 16) W::multiply<MT, MT>(stage, acc);
+          else W::multiply<MT, 1>(stage, acc);
+        }
+        at = at == NS - 1 ? 0 : at + 1;
+      }
+      if constexpr (SECOND) finish_second<W, MT>(s, a, items, it, acc);
+      else finish_first<W, ACT, MT>(s, a, items, it, acc);
+      it = next;  // (the last item's requests stay with it)
+    }
+    wait_vm<0>();  // no load is left that writes LDS
+  }
+  if constexpr (SECOND) clear_idle(a);
 }
 
 }  // namespace mlp2
@@ -738,9 +897,9 @@ int status(hipError_t e) { return e == hipSuccess ? MLP2_OK : record_error(MLP2_
 
 constexpr int kRouteTokens = 8;
 constexpr int kMostParts = 16;  // of K
-// K of a part of the router: 16 parts, of 64 to 512 each (more than 16 only for H > 8192).
+// K of a part of the router: 32 parts, of 64 to 512 each (more than 32 only for H > 16384).
 int route_part(int64_t H) {
-  const int64_t per = round_up((H + 15) / 16, 64);
+  const int64_t per = round_up((H + 31) / 32, 64);
   return (int)(per > kRoutePart ? kRoutePart : per);
 }
 
@@ -748,35 +907,50 @@ template <class W>
 hipError_t route(const mlp2_moe_s* p, int64_t T, const void* X, const void* Wr, int32_t* ids, float* gates, hipStream_t s) {
   Route a{(const uint16_t*)X, Wr, p->logits, p->routed, ids, gates, (int)T, (int)p->H, p->E, p->k, 1, 0, 1};
   while (a.width < p->E && a.width < 256) a.width *= 2;
-  const int tokens = T == 1 ? 1 : kRouteTokens;
+  // Tokens of a group share the reads of Wr, and are chosen for by four waves: four of them, eight where there are many.
+  const int tokens = T == 1 ? 1 : T <= 64 ? kRouteTokens / 2 : kRouteTokens;
   const int64_t groups = (T + tokens - 1) / tokens;
   a.per = route_part(p->H);
   a.splits = (int)((p->H + a.per - 1) / a.per);
   const dim3 grid((unsigned)groups, (unsigned)a.splits);
   if (tokens == 1) k_moe_route<W, 1><<<grid, 256, 0, s>>>(a);
+  else if (tokens < kRouteTokens) k_moe_route<W, kRouteTokens / 2><<<grid, 256, 0, s>>>(a);
   else k_moe_route<W, kRouteTokens><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <class Weights, int ACT>
-void first(const Experts& a, unsigned grid, hipStream_t s) {
-  if (a.T <= 16) k_moe_first<Weights, ACT, 1><<<grid, 256, 0, s>>>(a);
-  else k_moe_first<Weights, ACT, Weights::MOST><<<grid, 256, 0, s>>>(a);
+// Whether items hold up to 16 rows of an expert only: with few slots an expert, more rows than that are rare (they make a second item,
+// which streams the weights again), and the smaller kernel leaves more work-groups to a CU.
+bool narrow(int64_t slots, int E) { return slots <= 16 || slots <= 6ll * E; }
+
+template <class Weights, int ACT, bool SECOND>
+void launch(const Experts& a, unsigned grid, hipStream_t s) {
+  const bool few = narrow((int64_t)a.T * a.k, a.E);
+  if constexpr (std::is_same_v<Weights, Bf16Weights>) {
+    if (few) k_moe_bf16<ACT, 1, SECOND><<<grid, 256, 0, s>>>(a);
+    else k_moe_bf16<ACT, Weights::MOST, SECOND><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (few) k_moe_mx<ACT, 1, SECOND><<<grid, 512, 0, s>>>(a);
+    else k_moe_mx<ACT, Weights::MOST, SECOND><<<grid, 512, 0, s>>>(a);
+  }
 }
 
 template <class Weights>
 hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t* ids, const float* gates, const void* W1, const void* W1s, const void* W2,
                    const void* W2s, void* Y, hipStream_t s) {
   const int64_t slots = T * p->k, active = slots < p->E ? slots : p->E;  // experts that have a slot, at most
-  const int64_t resident = (T <= 16 ? 3ll : 2ll) * p->num_cus;            // work-groups that the chip holds at once (by their registers)
-  auto fill = [&](Experts& a, int64_t K, int64_t N, int64_t width) {      // width: floats of a slot's part
-    const int64_t tile = T <= 16 ? 16 : 16 * Weights::MOST, room = p->part_floats / (slots * width);
+  const int most_blocks = narrow(slots, p->E) ? 1 : Weights::MOST;
+  const int64_t resident = (int64_t)Weights::resident(most_blocks) * p->num_cus;  // work-groups that the chip holds at once
+  auto fill = [&](Experts& a, int64_t K, int64_t N, int64_t width, bool gated) {  // width: floats of a slot's part
+    const int64_t tile = 16 * most_blocks, room = p->part_floats / (slots * width);
     a.K = (int)K;
     a.N = (int)N;
-    a.blocks = (int)((N + 127) / 128);
+    a.blocks = (int)((N + Weights::cols(gated) - 1) / Weights::cols(gated));
+    a.item = Weights::ITEM;
     a.steps = (int)((K + Weights::STEP - 1) / Weights::STEP);
     a.most = (int)(room < 1 ? 1 : room > kMostParts ? kMostParts : room);
-    if (a.most > a.steps / kWaves) a.most = a.steps / kWaves < 1 ? 1 : a.steps / kWaves;
+    const int fewest = Weights::ITEM / 2;  // steps of a part
+    if (a.most > a.steps / fewest) a.most = a.steps / fewest < 1 ? 1 : a.steps / fewest;
     const int64_t most = (active + slots / tile) * a.blocks * a.most;
     return (unsigned)(most < resident ? most : resident);
   };
@@ -793,19 +967,18 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
   a.scales = (const char*)W1s;
   a.out = p->Z;
   a.arrived = p->joined;
-  const unsigned g1 = fill(a, p->H, p->F, p->nb * p->F);
-  if (p->act == MLP2_ACT_SWIGLU) first<Weights, ACT_SWIGLU>(a, g1, s);
-  else if (p->act == MLP2_ACT_GELU_TANH) first<Weights, ACT_GELU_TANH>(a, g1, s);
-  else first<Weights, ACT_IDENTITY>(a, g1, s);
+  const unsigned g1 = fill(a, p->H, p->F, p->nb * p->F, p->nb == 2);
+  if (p->act == MLP2_ACT_SWIGLU) launch<Weights, ACT_SWIGLU, false>(a, g1, s);
+  else if (p->act == MLP2_ACT_GELU_TANH) launch<Weights, ACT_GELU_TANH, false>(a, g1, s);
+  else launch<Weights, ACT_IDENTITY, false>(a, g1, s);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   b.X = p->Z;
   b.W = (const char*)W2;
   b.scales = (const char*)W2s;
   b.out = (uint16_t*)Y;
   b.arrived = p->arrived;
-  const unsigned g2 = fill(b, p->F, p->H, p->H);
-  if (T <= 16) k_moe_second<Weights, 1><<<g2, 256, 0, s>>>(b);
-  else k_moe_second<Weights, Weights::MOST><<<g2, 256, 0, s>>>(b);
+  const unsigned g2 = fill(b, p->F, p->H, p->H, false);
+  launch<Weights, ACT_IDENTITY, true>(b, g2, s);
   return hipGetLastError();
 }
 
@@ -866,13 +1039,13 @@ mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, in
   p->nb = act == MLP2_ACT_SWIGLU ? 2 : 1;
   p->device = device;
   p->num_cus = cus;
-  const int64_t slots = max_tokens * k, groups = (max_tokens + kRouteTokens - 1) / kRouteTokens;
+  const int64_t slots = max_tokens * k, groups = (max_tokens + kRouteTokens - 1) / kRouteTokens + 16;  // up to 64 tokens: of four
   // room for 16 parts of K of either product while they are small; one part of the second always fits
   const int64_t wide = p->nb * F > H ? p->nb * F : H, all = kMostParts * slots * wide, few = (int64_t)16 << 20, one = slots * H;
   p->part_floats = all < few ? all : one > few ? one : few;
   const int64_t z = round_up(slots * F * 2, 256), part = round_up(p->part_floats * 4, 256);
   const int64_t logits = round_up(max_tokens * ((H + route_part(H) - 1) / route_part(H)) * E * 8, 256);
-  const int64_t tokens_blocks = max_tokens * ((H + 127) / 128), slots_blocks = slots * ((F + 127) / 128);
+  const int64_t tokens_blocks = max_tokens * ((H + 127) / 128), slots_blocks = slots * (F / 64);
   const int64_t counters = (tokens_blocks + slots_blocks + groups * kLine) * 4;
   if (hipMalloc((void**)&p->ws, (size_t)(z + part + logits + counters)) != hipSuccess ||
       hipMemset(p->ws + z + part + logits, 0, (size_t)counters) != hipSuccess ||

@@ -30,9 +30,9 @@ constexpr int kMxGroup = 128;  // elements whose scales share a word
 __host__ __device__ constexpr int64_t mx_padded(int64_t k) { return (k + kMxGroup - 1) / kMxGroup * kMxGroup; }
 
 typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
-// A scale as the float that the conversion instructions take (2^-127 is a subnormal one).
+// A scale as the float that the conversion instructions take: they use its exponent field alone, 0 standing for 2^-127 and 255 for NaN.
 __device__ __forceinline__ float mx_unit(uint32_t s) {
-  return __builtin_bit_cast(float, s == 0 ? 0x00400000u : s == 255 ? 0x7FC00000u : s << 23);
+  return __builtin_bit_cast(float, s << 23);
 }
 
 constexpr int kFp4 = 4;  // the operand format of the scaled matrix instruction
