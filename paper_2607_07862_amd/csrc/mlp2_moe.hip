@@ -226,7 +226,7 @@ struct Experts {
   const char* W;       // bf16 [E, nb, K, N], or MXFP4 codes of E nb matrices [N, K]
   const char* scales;
   uint16_t* out;       // first: Z; second: Y [T, H]
-  float* part;         // parts of K: first [splits, T k, nb, N], second [splits, T k, N] with the gates applied; below 4 GB
+  float* part;         // parts of K: first [splits, T k, nb, N], second [splits, T k, N]; below 4 GB
   uint32_t* arrived;   // zero between launches; first: one counter for each slot and block of columns, second: for each token and block
   int T, E, k, K, N;
   int blocks;          // of columns
@@ -252,6 +252,7 @@ struct Bf16Weights {
   static constexpr int RING = 2;   // steps in registers
   static constexpr int cols(bool) { return 128; }     // result columns of an item
   static constexpr int UP_WAVE = 2, UP_COL = 0;       // where the second matrix's sums are
+  static constexpr int J = 8;                         // instruction groups of a wave: 16 columns each
   static constexpr int resident(int most) { return most == 1 ? 3 : 2; }  // work-groups of a CU, by their registers
   template <int MT>
   struct Regs {
@@ -320,8 +321,10 @@ struct Bf16Weights {
     }
   }
   // Where the four sums of instruction j lie: columns 8 (4 g + i) + j.
-  __device__ static __forceinline__ void put(float* to, const f32x4 (&c)[8]) {
-    const int g = (threadIdx.x & 63) >> 4;
+  template <class Sums>
+  __device__ static __forceinline__ void put(Sums& sum, const f32x4 (&c)[8]) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    float* to = sum[uniform((int)threadIdx.x >> 6)][lane & 15];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 lo, hi;
@@ -339,10 +342,9 @@ struct Bf16Weights {
 // MXFP4 weights [N, K], K contiguous.  A memory line is 256 k of one row, the matrix instruction's operand 8 k of 16 rows: loads
 // straight into registers would take a row's line in 64-byte pieces, and stream at 4 TB/s (pieces of a whole line: 6.9).  So the weights
 // go through LDS, and X with them: a stage is 128 rows (with a gate 64 of either matrix) by 256 k of codes, two words of scales a row
-// and 512 bytes of each X row, brought by direct-to-LDS loads of whole lines into a ring of stages.  Every wave multiplies an eighth of
-// the stage's k, all rows and columns, so that each byte leaves LDS once.  A lane turns 8 codes of a row into a bf16 operand (exactly:
-// two significant bits and a power of two).  Two waves to a SIMD: with one, which had twice the k, reads, conversions and products waited for
-// each other (3.8 TB/s).
+// and 512 bytes of each X row, brought by direct-to-LDS loads of whole lines into a ring of stages.  Every wave multiplies a quarter
+// of the stage's k with half of its rows.  A lane turns 16 codes of a row into two bf16 operands (exactly: two significant bits and a power of
+// two).  Two waves to a SIMD: with one, reads, conversions and products waited for each other (3.8 TB/s).
 struct MxWeights {
   static constexpr int WAVES = 8;
   static constexpr int STEP = 256;  // (of all waves)
@@ -351,6 +353,7 @@ struct MxWeights {
   static constexpr int resident(int) { return 1; }
   static constexpr int cols(bool gated) { return gated ? 64 : 128; }   // result columns of an item
   static constexpr int UP_WAVE = 0, UP_COL = 64;                       // where the second matrix's sums are
+  static constexpr int J = 4;                                          // instruction groups of a wave: 16 columns each
   static constexpr int CODES = 16384, X0 = CODES + 1024;
   static constexpr int stage(int mt) { return X0 + 8192 * mt; }
   static constexpr int depth(int mt) { return mt == 1 ? 4 : 3; }       // stages of the ring
@@ -414,64 +417,64 @@ struct MxWeights {
     }
   };
 
-  // One stage: this wave's 32 k of it, which are one block of every row; the first HERE blocks of rows.  Everything that the stage
-  // holds for this lane is read before the first product.
+  // One stage: a quarter of its k, one half of its rows; the first HERE blocks of X's rows.  Lane group g has 16 k of every row, two
+  // operands; everything that the stage holds for this lane is read before the first product.
   template <int MT, int HERE>
-  __device__ static __forceinline__ void multiply(const char* stage, f32x4 (&acc)[MT][8]) {
-    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
-    const char* codes = stage + 128 * i16 + 16 * (wave ^ (i16 >> 1)) + 4 * g;
-    const char* scales = stage + CODES + 512 * (wave >> 2) + 4 * i16 + (wave & 3);
-    u32x4 x[HERE];
-    uint32_t c[8], sc[8];
+  __device__ static __forceinline__ void multiply(const char* stage, f32x4 (&acc)[MT][J]) {
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15, k = wave % 4, upper = wave / 4;
+    const char* codes = stage + 8192 * upper + 128 * i16 + 16 * ((2 * k + (g >> 1)) ^ (i16 >> 1)) + 8 * (g & 1);
+    const char* scales = stage + CODES + 512 * (k >> 1) + 256 * upper + 4 * i16 + 2 * (k & 1) + (g >> 1);
+    const char* xs = stage + X0 + 512 * i16;
+    u32x4 x[HERE][2];
+    u32x2 c[J];
+    uint32_t sc[J];
 #pragma unroll
-    for (int m = 0; m < HERE; ++m) x[m] = *reinterpret_cast<const u32x4*>(stage + X0 + 512 * i16 + 8192 * m + 16 * ((4 * wave + g) ^ i16));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      c[j] = *reinterpret_cast<const uint32_t*>(codes + 2048 * j);
+    for (int j = 0; j < J; ++j) {
+      c[j] = *reinterpret_cast<const u32x2*>(codes + 2048 * j);
       sc[j] = *reinterpret_cast<const uint8_t*>(scales + 64 * j);
     }
+#pragma unroll
+    for (int m = 0; m < HERE; ++m)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) x[m][p] = *reinterpret_cast<const u32x4*>(xs + 8192 * m + 16 * ((8 * k + 2 * g + p) ^ i16));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float scale = mx_unit(sc[j]);
-      u32x4 f;
-      f[0] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 0));
-      f[1] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 1));
-      f[2] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 2));
-      f[3] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], scale, 3));
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int m = 0; m < HERE; ++m) acc[m][j] = Bf16::mfma(f, x[m], acc[m][j]);
-    }
+      for (int j = 0; j < J; ++j) {
+        const float scale = mx_unit(sc[j]);
+        u32x4 f;
+        f[0] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j][p], scale, 0));
+        f[1] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j][p], scale, 1));
+        f[2] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j][p], scale, 2));
+        f[3] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j][p], scale, 3));
+#pragma unroll
+        for (int m = 0; m < HERE; ++m) acc[m][j] = Bf16::mfma(f, x[m][p], acc[m][j]);
+      }
   }
-  // Where the four sums of instruction group j lie: columns 16 j + 4 g + i.
-  __device__ static __forceinline__ void put(float* to, const f32x4 (&c)[8]) {
-    const int g = (threadIdx.x & 63) >> 4;
+  // Where the four sums of instruction group j lie: columns 16 j + 4 g + i of the wave's half.
+  template <class Sums>
+  __device__ static __forceinline__ void put(Sums& sum, const f32x4 (&c)[J]) {
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    float* to = sum[wave % 4][lane & 15] + 64 * (wave / 4) + 4 * (lane >> 4);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + 16 * j + 4 * g) = c[j];
-  }
-  __device__ static __forceinline__ void add(const float* from, f32x4 (&c)[8]) {
-    const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] += *reinterpret_cast<const f32x4*>(from + 16 * j + 4 * g);
+    for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4*>(to + 16 * j) = c[j];
   }
 };
 
-constexpr int kPitch = 128 + 4;  // floats of a row of sums in LDS
+constexpr int kIdsInLds = 2048;
 template <class Weights, int RING>
 struct MoeShared {
   static constexpr int kWave = Weights::WAVES, kThreads = 64 * kWave;
   // (4-bit weights) the ring of stages, and the slots' experts: reading those from memory would wait for every stage in flight
   static constexpr bool kIds = RING > 0;
   alignas(1024) char ring[RING ? RING : 16];
-  int16_t ids[kIds ? kMostSlots : 1];
-  float sum[kWaves][16][kPitch];
-  __device__ __forceinline__ float* sums(int wave, int row) { return sum[wave][row]; }
+  int16_t ids[kIds ? kIdsInLds : 1];
+  float sum[kWaves][16][128 + 4];  // the waves' sums; behind the last item, tokens that are complete
   int count[kMostExperts];  // slots of an expert
   int start[kMostExperts];  // its first unit (an expert's chunk of rows and a block of columns)
   int rows[2][kWave][64];  // slots of an item and of the next one, a copy for each wave
-  int total, last;
-  int found, done[64];      // second: tokens of the item that are complete
-  uint32_t valid[64];       // and their slots that have an expert
+  int total, found;
 };
 
 // Items, from ids.  Up to 64 slots every wave keeps them in a register and goes through the experts that it finds there; beyond,
@@ -503,7 +506,7 @@ struct Items {
         const int e = a.ids[i];
         const bool here = e >= 0 && e < a.E;
         if (here) atomicAdd(&s.count[e], 1);
-        if constexpr (Shared::kIds) s.ids[i] = (int16_t)(here ? e : -1);
+        if (Shared::kIds && slots <= kIdsInLds) s.ids[i] = (int16_t)(here ? e : -1);
       }
       __syncthreads();
       if (tid < 64) {
@@ -585,9 +588,8 @@ struct Items {
     int before = -it.first;
     for (int i0 = 0; i0 < slots; i0 += 64) {
       const int i = i0 + lane;
-      bool here;
-      if constexpr (Shared::kIds) here = few ? id == it.expert : i < slots && s.ids[min(i, slots - 1)] == it.expert;
-      else here = few ? id == it.expert : i < slots && a.ids[i] == it.expert;
+      bool here = few ? id == it.expert : i < slots;
+      if (!few && here) here = Shared::kIds && slots <= kIdsInLds ? s.ids[i] == it.expert : a.ids[i] == it.expert;
       const uint64_t all = __ballot(here);
       const int at = before + __builtin_popcountll(all & ((1ull << lane) - 1));
       if (here && at >= 0 && at < it.rows) it.slots[at] = i;
@@ -598,22 +600,25 @@ struct Items {
   }
 };
 
-// The waves' sums of one block of rows, in LDS: four copies; of eight waves the upper ones' are added to the lower ones' first.
-template <class Weights, class Shared>
-__device__ __forceinline__ void meet(Shared& s, f32x4 (&c)[8]) {
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+// The waves' sums of one block of rows meet in LDS, four copies of them.  Thread 16 r + c / 8 (of the first 256) gets eight columns of row r:
+// v those from column c on, and with a gate u those of the second matrix.
+template <class Weights, bool GATED, class Shared>
+__device__ __forceinline__ void collect(Shared& s, const f32x4 (&acc)[Weights::J], float (&v)[8], float (&u)[8]) {
+  constexpr int SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : kWaves;
+  const int tid = threadIdx.x, r = tid / 16, c = 8 * (tid % 16);
   __syncthreads();  // the sums before these have been read
-  if constexpr (Weights::WAVES == 2 * kWaves) {
-    if (wave >= kWaves) Weights::put(s.sums(wave - kWaves, lane & 15), c);
-    __syncthreads();
-    if (wave < kWaves) {
-      Weights::add(s.sums(wave, lane & 15), c);
-      Weights::put(s.sums(wave, lane & 15), c);
-    }
-  } else {
-    Weights::put(s.sums(wave, lane & 15), c);
-  }
+  Weights::put(s.sum, acc);
   __syncthreads();
+  if (tid >= 256 || c >= Weights::cols(GATED)) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = u[e] = 0.f;
+#pragma unroll
+  for (int i = 0; i < SHARE; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] += s.sum[i][r][c + e];
+      if (GATED) u[e] += s.sum[Weights::UP_WAVE + i][r][Weights::UP_COL + c + e];
+    }
 }
 
 template <int ACT>
@@ -624,159 +629,172 @@ __device__ __forceinline__ u32x4 activate(const float (&v)[8], const float (&u)[
   return pack_bf16x8(z);
 }
 
-// Z = act(X W1) of the item's rows from the waves' sums.  (With a gate the bf16 weights' waves 0 and 1 hold the first matrix's sums, 2 and
-// 3 the second's; the 4-bit ones' hold 64 columns of either.)
+// Z = act(X W1) of the item's rows, or a part of X W1, from the waves' sums.
 template <class Weights, int ACT, int MT, int TILE, class Shared>
-__device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, f32x4 (&acc)[MT][8]) {
+__device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
   constexpr bool GATED = ACT == ACT_SWIGLU;
-  constexpr int NB = GATED ? 2 : 1, COLS = Weights::cols(GATED), SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : kWaves;
-  const int tid = threadIdx.x, col0 = it.block * COLS;
-  const int* rows = it.slots;
-  const int r = tid / 16, c = 8 * (tid % 16);
-  const bool inside = tid < 256 && c < COLS && col0 + c < a.N;
+  constexpr int NB = GATED ? 2 : 1, COLS = Weights::cols(GATED);
+  const int tid = threadIdx.x, r = tid / 16, c = 8 * (tid % 16), col = it.block * COLS + c;
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     if (16 * m >= it.rows) break;
-    meet<Weights>(s, acc[m]);
-    if (16 * m + r < it.rows && inside) {
-      float v[8] = {}, u[8] = {};
-#pragma unroll
-      for (int i = 0; i < SHARE; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] += s.sums(i, r)[c + e];
-          if (GATED) u[e] += s.sums(Weights::UP_WAVE + i, r)[Weights::UP_COL + c + e];
-        }
-      const int slot = rows[16 * m + r];
-      if (items.splits == 1) {
-        *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col0 + c) = activate<ACT>(v, u);
-      } else {
-        const uint32_t to = (uint32_t)((it.split * slots + slot) * NB * a.N + col0 + c) * 4;
-        part.store16(to, f32x4{v[0], v[1], v[2], v[3]});
-        part.store16(to + 16, f32x4{v[4], v[5], v[6], v[7]});
-        if (GATED) {
-          part.store16(to + 4 * a.N, f32x4{u[0], u[1], u[2], u[3]});
-          part.store16(to + 4 * a.N + 16, f32x4{u[4], u[5], u[6], u[7]});
-        }
+    float v[8], u[8];
+    collect<Weights, GATED>(s, acc[m], v, u);
+    if (tid >= 256 || c >= COLS || col >= a.N || 16 * m + r >= it.rows) continue;
+    const int slot = it.slots[16 * m + r];
+    if (items.splits == 1) {
+      *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col) = activate<ACT>(v, u);
+    } else {
+      const uint32_t to = (uint32_t)((it.split * slots + slot) * NB * a.N + col) * 4;
+      part.store16(to, f32x4{v[0], v[1], v[2], v[3]});
+      part.store16(to + 16, f32x4{v[4], v[5], v[6], v[7]});
+      if (GATED) {
+        part.store16(to + 4 * a.N, f32x4{u[0], u[1], u[2], u[3]});
+        part.store16(to + 4 * a.N + 16, f32x4{u[4], u[5], u[6], u[7]});
       }
     }
-  }
-  if (items.splits == 1) return;
-  // The part that arrives last adds all of them, in the order 0, 1, ...
-  wait_all_mem();
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t* count = a.arrived + (int64_t)rows[0] * a.blocks + it.block;
-    const bool last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(items.splits - 1);
-    if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
-    s.last = last;
-  }
-  __syncthreads();
-  if (!uniform(s.last)) return;
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    if (16 * m + r >= it.rows || !inside) continue;
-    const int slot = rows[16 * m + r];
-    const uint32_t first = (uint32_t)(slot * (int64_t)NB * a.N + col0 + c) * 4, pitch = (uint32_t)(slots * NB * a.N * 4);
-    float v[8] = {}, u[8] = {};
-    for (int q = 0; q < items.splits; q += 4) {
-      f32x4 x[4][2 * NB];
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 2 * NB; ++i) x[d][i] = part.load16(first + min(q + d, items.splits - 1) * pitch + (i / 2) * 4 * a.N + 16 * (i % 2));
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] += q + d < items.splits ? x[d][e / 4][e % 4] : 0.f;
-          if (GATED) u[e] += q + d < items.splits ? x[d][2 * NB - 2 + e / 4][e % 4] : 0.f;
-        }
-    }
-    *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col0 + c) = activate<ACT>(v, u);
   }
 }
 
-// The item's part of Z W2, to memory; then, for every token of which this was the last part, Y.
-template <class Weights, int MT, int TILE, class Shared>
-__device__ __forceinline__ void finish_second(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, f32x4 (&acc)[MT][8]) {
-  const int tid = threadIdx.x, col0 = it.block * 128;
-  const int* rows = it.slots;
+// Z of the items whose parts of K are all in memory.  A work-group's own parts are, once every wave has waited for its stores; then each
+// wave counts the arrivals of some of its items, and where it was the last one adds all parts, in the order 0, 1, ...  So no item waits
+// for its stores, and the counts' latencies pass side by side.
+template <class Weights, int ACT, int TILE, class Shared>
+__device__ __forceinline__ void join_first(Shared& s, const Experts& a, const Items<TILE>& items) {
+  if (items.splits == 1) return;
+  constexpr int NB = ACT == ACT_SWIGLU ? 2 : 1, COLS = Weights::cols(ACT == ACT_SWIGLU), LANES = COLS / 8;
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), total = items.total();
+  const int64_t slots = (int64_t)a.T * a.k;
+  const Far part(a.part);
+  wait_all_mem();
+  __syncthreads();
+  for (int n = blockIdx.x + wave * gridDim.x; n < total; n += gridDim.x * Shared::kWave) {
+    const Item it = items.find(s, a, n, 0);
+    uint32_t* count = a.arrived + (int64_t)it.slots[0] * a.blocks + it.block;
+    int last = 0;
+    if (lane == 0) {
+      last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(items.splits - 1);
+      if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
+    }
+    if (!uniform(last)) continue;
+    const int col = it.block * COLS + 8 * (lane % LANES);
+    if (col >= a.N) continue;
+    for (int r = lane / LANES; r < it.rows; r += 64 / LANES) {
+      const int slot = it.slots[r];
+      const uint32_t first = (uint32_t)(slot * (int64_t)NB * a.N + col) * 4, pitch = (uint32_t)(slots * NB * a.N * 4);
+      float v[8] = {}, u[8] = {};
+      for (int q = 0; q < items.splits; q += 4) {
+        f32x4 x[4][2 * NB];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 2 * NB; ++i) x[d][i] = part.load16(first + min(q + d, items.splits - 1) * pitch + (i / 2) * 4 * a.N + 16 * (i % 2));
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[e] += q + d < items.splits ? x[d][e / 4][e % 4] : 0.f;
+            if (NB == 2) u[e] += q + d < items.splits ? x[d][2 * NB - 2 + e / 4][e % 4] : 0.f;
+          }
+      }
+      *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col) = activate<ACT>(v, u);
+    }
+  }
+}
+
+// The item's part of Z W2, to memory.
+template <class Weights, int MT, class Shared>
+__device__ __forceinline__ void finish_second(Shared& s, const Experts& a, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
+  const int tid = threadIdx.x, r = tid / 16, col = it.block * 128 + 8 * (tid % 16);
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     if (16 * m >= it.rows) break;
-    meet<Weights>(s, acc[m]);
-    const int r = tid / 16, c = 8 * (tid % 16);
-    if (tid < 256 && 16 * m + r < it.rows && col0 + c < a.N) {
-      float v[8] = {};
+    float v[8], u[8];
+    collect<Weights, false>(s, acc[m], v, u);
+    if (tid >= 256 || col >= a.N || 16 * m + r >= it.rows) continue;
+    const uint32_t to = (uint32_t)((it.split * slots + it.slots[16 * m + r]) * a.N + col) * 4;
+    part.store16(to, f32x4{v[0], v[1], v[2], v[3]});
+    part.store16(to + 16, f32x4{v[4], v[5], v[6], v[7]});
+  }
+}
+
+// Y of one token's block of columns from its slots' parts, by 32 lanes: slots in order, a slot's parts of K in order; sixteen loads in
+// flight.
+__device__ __forceinline__ void sum_token(const Experts& a, int splits, int token, uint32_t valid, int block) {
+  constexpr int AHEAD = 16;
+  const int col = block * 128 + 4 * (threadIdx.x & 31), terms = a.k * splits;
+  if (col >= a.N) return;
+  const Far part(a.part);
+  const uint32_t pitch = (uint32_t)((int64_t)a.T * a.k * a.N * 4);
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < terms; t += AHEAD) {
+    f32x4 v[AHEAD];
+    float gate[AHEAD];
+    bool there[AHEAD];
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += s.sums(i, r)[c + e];
-      const int slot = rows[16 * m + r];
-      const float gate = a.gates[slot];
-      const uint32_t to = (uint32_t)((it.split * slots + slot) * a.N + col0 + c) * 4;
-      part.store16(to, f32x4{gate * v[0], gate * v[1], gate * v[2], gate * v[3]});
-      part.store16(to + 16, f32x4{gate * v[4], gate * v[5], gate * v[6], gate * v[7]});
+    for (int d = 0; d < AHEAD; ++d) {
+      const int term = min(t + d, terms - 1), j = term / splits, q = term - j * splits;
+      there[d] = t + d < terms && (valid >> j & 1);
+      gate[d] = a.gates[token * a.k + j];
+      v[d] = part.load16(there[d] ? (uint32_t)((token * a.k + j) * a.N + col) * 4 + q * pitch : 0u);
     }
-  }
-  // Every slot's part counts for its token; the part that completes the count finds all of them in memory.
-  int t = 0;
-  uint32_t valid = 0;  // the token's slots that have an expert
-  if (tid < it.rows) {
-    t = rows[tid] / a.k;
-    int e[kMostChosen];
 #pragma unroll
-    for (int j = 0; j < kMostChosen; ++j) e[j] = a.ids[t * a.k + min(j, a.k - 1)];
+    for (int d = 0; d < AHEAD; ++d)
 #pragma unroll
-    for (int j = 0; j < kMostChosen; ++j) valid |= j < a.k && e[j] >= 0 && e[j] < a.E ? 1u << j : 0u;
+      for (int i = 0; i < 4; ++i) y[i] = there[d] ? __builtin_fmaf(gate[d], v[d][i], y[i]) : y[i];
   }
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  bf16x4 b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = (__bf16)y[i];
+  *reinterpret_cast<bf16x4*>(a.out + (int64_t)token * a.N + col) = b;
+}
+
+// Y of the tokens whose parts are all in memory, counted as in join_first, but by tokens: every slot's part of a block of columns counts
+// for its token.  Whoever completes a count notes the token, and all threads of the work-group add up what was noted.
+template <int TILE, class Shared>
+__device__ __forceinline__ void join_second(Shared& s, const Experts& a, const Items<TILE>& items) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), total = items.total();
+  struct Done {
+    uint32_t token, valid;  // token: its block of columns in the upper half
+  };
+  constexpr int ROOM = sizeof(s.sum) / sizeof(Done);
+  Done* done = reinterpret_cast<Done*>(s.sum);
   wait_all_mem();
   if (tid == 0) s.found = 0;
   __syncthreads();
-  if (tid < it.rows) {
-    uint32_t* count = a.arrived + (int64_t)t * a.blocks + it.block;
-    if (__hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(__builtin_popcount(valid) * items.splits - 1)) {
-      __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
-      const int at = atomicAdd(&s.found, 1);
-      s.done[at] = t;
-      s.valid[at] = valid;
+  for (int n = blockIdx.x + wave * gridDim.x; n < total; n += gridDim.x * Shared::kWave) {
+    const Item it = items.find(s, a, n, 0);
+    const int mine = it.slots[lane < it.rows ? lane : 0] / a.k;  // lane r: the token of row r
+    int e[kMostChosen];
+#pragma unroll
+    for (int j = 0; j < kMostChosen; ++j) e[j] = a.ids[mine * a.k + min(j, a.k - 1)];
+    uint32_t valid = 0;  // its slots that have an expert
+#pragma unroll
+    for (int j = 0; j < kMostChosen; ++j) valid |= j < a.k && e[j] >= 0 && e[j] < a.E ? 1u << j : 0u;
+    bool over = false;  // complete, but there is no room to note it
+    if (lane < it.rows) {
+      uint32_t* count = a.arrived + (int64_t)mine * a.blocks + it.block;
+      if (__hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(__builtin_popcount(valid) * items.splits - 1)) {
+        __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // as the next launch expects it
+        const int at = atomicAdd(&s.found, 1);
+        over = at >= ROOM;
+        if (!over) done[at] = Done{(uint32_t)(mine | it.block << 16), valid};
+      }
+    }
+    for (uint64_t left = __ballot(over); left; left &= left - 1) {
+      const int r = __builtin_ctzll(left), token = __shfl(mine, r);
+      const uint32_t mask = (uint32_t)__shfl((int)valid, r);
+      if (lane < 32) sum_token(a, items.splits, token, mask, it.block);
     }
   }
   __syncthreads();
-  const int found = uniform(s.found), c = col0 + 4 * (tid % 32);
-  if (c < a.N)
-    for (int i = tid / 32; i < found; i += Shared::kThreads / 32) {
-      const int token = s.done[i];
-      const uint32_t mask = s.valid[i], pitch = (uint32_t)(slots * a.N * 4);
-      // terms: slots in order, a slot's parts of K in order; sixteen in flight
-      constexpr int AHEAD = 16;
-      f32x4 y = {0.f, 0.f, 0.f, 0.f};
-      const int terms = a.k * items.splits;
-      for (int n = 0; n < terms; n += AHEAD) {
-        f32x4 v[AHEAD];
-        bool there[AHEAD];
-#pragma unroll
-        for (int d = 0; d < AHEAD; ++d) {
-          const int term = min(n + d, terms - 1), j = term / items.splits, q = term - j * items.splits;
-          there[d] = n + d < terms && (mask >> j & 1);
-          v[d] = part.load16(there[d] ? (uint32_t)((token * a.k + j) * a.N + c) * 4 + q * pitch : 0u);
-        }
-#pragma unroll
-        for (int d = 0; d < AHEAD; ++d)
-#pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4) y[i4] += there[d] ? v[d][i4] : 0.f;
-      }
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      bf16x4 b;
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) b[i4] = (__bf16)y[i4];
-      *reinterpret_cast<bf16x4*>(a.out + (int64_t)token * a.N + c) = b;
-    }
+  const int found = min(uniform(s.found), ROOM);
+  for (int i = tid / 32; i < found; i += Shared::kThreads / 32) sum_token(a, items.splits, (int)(done[i].token & 0xFFFFu), done[i].valid, (int)(done[i].token >> 16));
 }
 
 // Zeros for the tokens without an expert.
@@ -803,14 +821,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Bf16Weights
       constexpr int MT = decltype(mt)::value;
       f32x4 acc[MT][8];
       Bf16Weights::stream<MT, ACT == ACT_SWIGLU && !SECOND, SECOND>(it, a, items.from(it), items.end(a, it), acc);
-      if constexpr (SECOND) finish_second<Bf16Weights, MT>(s, a, items, it, acc);
+      if constexpr (SECOND) finish_second<Bf16Weights, MT>(s, a, it, acc);
       else finish_first<Bf16Weights, ACT, MT>(s, a, items, it, acc);
     };
     if (MOST == 1 || it.rows <= 16) run(int_constant<1>());
     else if (MOST > 2 && it.rows <= 32) run(int_constant<2>());
     else run(int_constant<MOST>());
   }
-  if constexpr (SECOND) clear_idle(a);
+  if constexpr (SECOND) {
+    join_second(s, a, items);
+    clear_idle(a);
+  } else {
+    join_first<Bf16Weights, ACT>(s, a, items);
+  }
 }
 
 // Items of 4-bit weights.  A work-group has most of a CU's LDS to itself, so nothing else would stream while it ends an item: its
@@ -848,11 +871,11 @@ __global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
     Item it = next;
     for (int i = 0; i < NS - 1; ++i) request();
     for (int n = blockIdx.x; n < total; n += gridDim.x) {
-      f32x4 acc[MT][8];
+      f32x4 acc[MT][W::J];
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < W::J; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
       const int steps = items.end(a, it) - items.from(it), stages = max(NS - 1, steps);
       for (int i = 0; i < stages; ++i) {
         wait_vm<(NS - 2) * W::loads(MT)>();
@@ -867,13 +890,18 @@ __global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
         }
         at = at == NS - 1 ? 0 : at + 1;
       }
-      if constexpr (SECOND) finish_second<W, MT>(s, a, items, it, acc);
+      if constexpr (SECOND) finish_second<W, MT>(s, a, it, acc);
       else finish_first<W, ACT, MT>(s, a, items, it, acc);
       it = next;  // (the last item's requests stay with it)
     }
     wait_vm<0>();  // no load is left that writes LDS
   }
-  if constexpr (SECOND) clear_idle(a);
+  if constexpr (SECOND) {
+    join_second(s, a, items);
+    clear_idle(a);
+  } else {
+    join_first<W, ACT>(s, a, items);
+  }
 }
 
 }  // namespace mlp2
