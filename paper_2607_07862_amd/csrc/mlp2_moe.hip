@@ -22,6 +22,7 @@ namespace mlp2 {
 constexpr int kMostExperts = 512, kMostSlots = 8192, kMostChosen = 16;
 constexpr int kWaves = 4;
 constexpr int kRoutePart = 512;  // the most of K in a part of the router
+constexpr int kMostParts = 16;   // of K in the experts' products
 
 // ------------------------------------------------------------------ memory that other XCDs write and read in the same launch
 
@@ -60,7 +61,7 @@ struct Route {
   int32_t* ids;     // [T, k]
   float* gates;
   int T, H, E, k, splits, per;  // per: K of a split, a multiple of 64
-  int width;        // threads that share a row of Wr: a power of two, at least E where that is at most 256
+  int width;        // threads that share a row of Wr: 2^width, at least E where that is at most 256
 };
 
 __device__ __forceinline__ double widen(uint16_t v) { return (double)__builtin_bit_cast(float, (uint32_t)v << 16); }
@@ -140,12 +141,12 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
   __shared__ int seen;
   constexpr int AHEAD = 16;
   const int tid = threadIdx.x, t0 = blockIdx.x * TT, split = blockIdx.y;
-  const int sub = tid / a.width, subs = 256 / a.width, e0 = tid % a.width;
+  const int width = 1 << a.width, sub = tid >> a.width, subs = 256 >> a.width, e0 = tid & (width - 1);
   const int from = split * a.per, deep = min(a.H - from, a.per);
   const W* Wr = (const W*)a.Wr + (int64_t)from * a.E;
-  const int chunks = (a.E + a.width - 1) / a.width;  // of experts; one but for E > 256
+  const int chunks = (a.E + width - 1) >> a.width;  // of experts; one but for E > 256
   for (int c = 0; c < chunks; ++c) {
-    const int e = c * a.width + e0;
+    const int e = (c << a.width) + e0;
     W w[AHEAD];
     auto request = [&](int k0) {
 #pragma unroll
@@ -156,10 +157,9 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
     };
     request(sub);
     if (c) __syncthreads();
-    for (int i = tid; i < deep * TT; i += 256) {
-      const int t = i / deep, kk = i % deep;
-      lds[kk * TT + t] = t0 + t < a.T ? widen(a.X[(int64_t)(t0 + t) * a.H + from + kk]) : 0.0;
-    }
+    for (int kk = tid & 63; kk < deep; kk += 64)
+#pragma unroll
+      for (int t = tid >> 6; t < TT; t += 4) lds[kk * TT + t] = t0 + t < a.T ? widen(a.X[(int64_t)(t0 + t) * a.H + from + kk]) : 0.0;
     __syncthreads();
     double acc[TT] = {};
     for (int k0 = sub; k0 < deep; k0 += AHEAD * subs) {
@@ -180,13 +180,13 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
     // the rows of K meet
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < TT; ++t) lds[(sub * TT + t) * a.width + e0] = acc[t];
+    for (int t = 0; t < TT; ++t) lds[((sub * TT + t) << a.width) + e0] = acc[t];
     __syncthreads();
-    for (int i = tid; i < TT * a.width; i += 256) {
-      const int t = i / a.width, en = c * a.width + i % a.width;
+    for (int i = tid; i < TT << a.width; i += 256) {
+      const int t = i >> a.width, en = (c << a.width) + (i & (width - 1));
       double sum = 0.0;
 #pragma unroll 8
-      for (int s = 0; s < subs; ++s) sum += lds[(s * TT + t) * a.width + i % a.width];
+      for (int s = 0; s < subs; ++s) sum += lds[((s * TT + t) << a.width) + (i & (width - 1))];
       if (t0 + t < a.T && en < a.E) store_far(a.part + ((int64_t)split * a.T + t0 + t) * a.E + en, sum);
     }
   }
@@ -196,18 +196,19 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
   __syncthreads();
   if (uniform(seen) != a.splits - 1) return;
   if (tid == 0) __hip_atomic_store(a.arrived + blockIdx.x * kLine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  // The parts, 8 at a time; all in the order 0, 1, ... whichever came last.
+  // The parts, 32 in flight; all in the order 0, 1, ... whichever came last.
+  constexpr int ALL = 32;
   const Far part(a.part);
   const int here = min(TT, a.T - t0) * a.E;
   for (int i = tid; i < here; i += 256) {
     const uint32_t first = (uint32_t)((t0 * a.E + i) * 8), pitch = (uint32_t)(a.T * a.E * 8);
     double sum = 0.0;
-    for (int s = 0; s < a.splits; s += 8) {
-      double v[8];
+    for (int s = 0; s < a.splits; s += ALL) {
+      double v[ALL];
 #pragma unroll
-      for (int d = 0; d < 8; ++d) v[d] = part.load_double(first + min(s + d, a.splits - 1) * pitch);
+      for (int d = 0; d < ALL; ++d) v[d] = part.load_double(first + min(s + d, a.splits - 1) * pitch);
 #pragma unroll
-      for (int d = 0; d < 8; ++d)
+      for (int d = 0; d < ALL; ++d)
         if (s + d < a.splits) sum += v[d];
     }
     lds[i] = sum;
@@ -231,7 +232,8 @@ struct Experts {
   int T, E, k, K, N;
   int blocks;          // of columns
   int steps;           // of K
-  int item;            // what an item costs beside its steps, in steps
+  float item;          // what an item costs beside its steps, in steps
+  float join;          // and a part of K where there are several
   int most;            // parts of K
 };
 
@@ -527,14 +529,17 @@ struct Items {
       __syncthreads();
       units = uniform(s.total);
     }
-    // Parts of K: as many as make the work-groups' shares alike, each item costing about as much as a.item steps more than it streams.  (A CU takes in
-    // at most 40 to 50 GB/s, whatever its loads in flight, so the last round of a few items is as long as a whole one.)
-    int least = 0x7FFFFFFF;
+    // Parts of K: as many as make the work-groups' shares alike, each item costing about as much as a.item steps more than it streams, and
+    // joining the parts a.join.  (A CU takes in at most 40 to 50 GB/s, whatever its loads in flight, so the last round of a few items is as
+    // long as a whole one.)  In floats: integer divisions, one after the other, took 3 us.
+    float least = 1e30f;
     splits = 1;
-    const int grid = gridDim.x;
-    for (int n = 1; n <= a.most; ++n) {
-      const int rounds = (units * n + grid - 1) / grid, steps = (a.steps + n - 1) / n, cost = rounds * (steps + a.item) + (n > 1 ? a.item / 2 : 0);
-      if (cost < least) {
+    const float rounds1 = (float)units / (float)gridDim.x;
+#pragma unroll
+    for (int n = 1; n <= kMostParts; ++n) {
+      const float steps = __builtin_ceilf((float)a.steps * (1.0f / n) - 1e-3f);
+      const float cost = __builtin_ceilf(rounds1 * n - 1e-3f) * (steps + a.item) + (n > 1 ? a.join * n : 0.f);
+      if (n <= a.most && cost < least) {
         least = cost;
         splits = n;
       }
@@ -731,16 +736,21 @@ __device__ __forceinline__ void sum_token(const Experts& a, int splits, int toke
   const Far part(a.part);
   const uint32_t pitch = (uint32_t)((int64_t)a.T * a.k * a.N * 4);
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  int j = 0, q = 0;  // the next term
   for (int t = 0; t < terms; t += AHEAD) {
     f32x4 v[AHEAD];
     float gate[AHEAD];
     bool there[AHEAD];
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d) {
-      const int term = min(t + d, terms - 1), j = term / splits, q = term - j * splits;
       there[d] = t + d < terms && (valid >> j & 1);
-      gate[d] = a.gates[token * a.k + j];
-      v[d] = part.load16(there[d] ? (uint32_t)((token * a.k + j) * a.N + col) * 4 + q * pitch : 0u);
+      const int slot = token * a.k + min(j, a.k - 1);
+      gate[d] = a.gates[slot];
+      v[d] = part.load16(there[d] ? (uint32_t)(slot * a.N + col) * 4 + q * pitch : 0u);
+      if (++q == splits) {
+        q = 0;
+        ++j;
+      }
     }
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d)
@@ -770,12 +780,16 @@ __device__ __forceinline__ void join_second(Shared& s, const Experts& a, const I
   for (int n = blockIdx.x + wave * gridDim.x; n < total; n += gridDim.x * Shared::kWave) {
     const Item it = items.find(s, a, n, 0);
     const int mine = it.slots[lane < it.rows ? lane : 0] / a.k;  // lane r: the token of row r
-    int e[kMostChosen];
-#pragma unroll
-    for (int j = 0; j < kMostChosen; ++j) e[j] = a.ids[mine * a.k + min(j, a.k - 1)];
     uint32_t valid = 0;  // its slots that have an expert
+    if (items.few) {
+      valid = (uint32_t)(__ballot(items.id >= 0) >> (mine * a.k)) & ((1u << a.k) - 1);
+    } else {
+      int e[kMostChosen];
 #pragma unroll
-    for (int j = 0; j < kMostChosen; ++j) valid |= j < a.k && e[j] >= 0 && e[j] < a.E ? 1u << j : 0u;
+      for (int j = 0; j < kMostChosen; ++j) e[j] = a.ids[mine * a.k + min(j, a.k - 1)];
+#pragma unroll
+      for (int j = 0; j < kMostChosen; ++j) valid |= j < a.k && e[j] >= 0 && e[j] < a.E ? 1u << j : 0u;
+    }
     bool over = false;  // complete, but there is no room to note it
     if (lane < it.rows) {
       uint32_t* count = a.arrived + (int64_t)mine * a.blocks + it.block;
@@ -924,7 +938,6 @@ namespace {
 int status(hipError_t e) { return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP); }
 
 constexpr int kRouteTokens = 8;
-constexpr int kMostParts = 16;  // of K
 // K of a part of the router: 32 parts, of 64 to 512 each (more than 32 only for H > 16384).
 int route_part(int64_t H) {
   const int64_t per = round_up((H + 31) / 32, 64);
@@ -933,8 +946,8 @@ int route_part(int64_t H) {
 
 template <class W>
 hipError_t route(const mlp2_moe_s* p, int64_t T, const void* X, const void* Wr, int32_t* ids, float* gates, hipStream_t s) {
-  Route a{(const uint16_t*)X, Wr, p->logits, p->routed, ids, gates, (int)T, (int)p->H, p->E, p->k, 1, 0, 1};
-  while (a.width < p->E && a.width < 256) a.width *= 2;
+  Route a{(const uint16_t*)X, Wr, p->logits, p->routed, ids, gates, (int)T, (int)p->H, p->E, p->k, 1, 0, 0};
+  while (1 << a.width < p->E && a.width < 8) ++a.width;
   // Tokens of a group share the reads of Wr, and are chosen for by four waves: four of them, eight where there are many.
   const int tokens = T == 1 ? 1 : T <= 64 ? kRouteTokens / 2 : kRouteTokens;
   const int64_t groups = (T + tokens - 1) / tokens;
@@ -969,12 +982,13 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
   const int64_t slots = T * p->k, active = slots < p->E ? slots : p->E;  // experts that have a slot, at most
   const int most_blocks = narrow(slots, p->E) ? 1 : Weights::MOST;
   const int64_t resident = (int64_t)Weights::resident(most_blocks) * p->num_cus;  // work-groups that the chip holds at once
-  auto fill = [&](Experts& a, int64_t K, int64_t N, int64_t width, bool gated) {  // width: floats of a slot's part
+  auto fill = [&](Experts& a, int64_t K, int64_t N, int64_t width, bool gated, float join) {  // width: floats of a slot's part
     const int64_t tile = 16 * most_blocks, room = p->part_floats / (slots * width);
     a.K = (int)K;
     a.N = (int)N;
     a.blocks = (int)((N + Weights::cols(gated) - 1) / Weights::cols(gated));
     a.item = Weights::ITEM;
+    a.join = join;
     a.steps = (int)((K + Weights::STEP - 1) / Weights::STEP);
     a.most = (int)(room < 1 ? 1 : room > kMostParts ? kMostParts : room);
     const int fewest = Weights::ITEM / 2;  // steps of a part
@@ -995,7 +1009,7 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
   a.scales = (const char*)W1s;
   a.out = p->Z;
   a.arrived = p->joined;
-  const unsigned g1 = fill(a, p->H, p->F, p->nb * p->F, p->nb == 2);
+  const unsigned g1 = fill(a, p->H, p->F, p->nb * p->F, p->nb == 2, 0.5f * Weights::ITEM);
   if (p->act == MLP2_ACT_SWIGLU) launch<Weights, ACT_SWIGLU, false>(a, g1, s);
   else if (p->act == MLP2_ACT_GELU_TANH) launch<Weights, ACT_GELU_TANH, false>(a, g1, s);
   else launch<Weights, ACT_IDENTITY, false>(a, g1, s);
@@ -1005,7 +1019,7 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
   b.scales = (const char*)W2s;
   b.out = (uint16_t*)Y;
   b.arrived = p->arrived;
-  const unsigned g2 = fill(b, p->F, p->H, p->H, false);
+  const unsigned g2 = fill(b, p->F, p->H, p->H, false, 0.03f * Weights::ITEM * p->k);
   launch<Weights, ACT_IDENTITY, true>(b, g2, s);
   return hipGetLastError();
 }

@@ -10,13 +10,14 @@
 // and operand: the same bytes, lanes and cycles as 16 x 16 x 32 of bf16.  So the
 // tiles, rings and slots are those of the 16-bit products (a stage of 64 16-bit
 // elements holds 256 of K) and the estimates that choose tile and split count K in
-// units of 64 x 16 bits.  What comes on top are the scales: each panel's stage
-// carries two words a row behind its codes, one more direct-to-LDS load (4 bytes a
-// lane) for every wave.
+// units of 64 x 16 bits.  What comes on top are the scales: two words a row and
+// stage, one more direct-to-LDS load (4 bytes a lane) for each wave and side.  They
+// are not hidden: the loop of the 256 x 256 tile takes 241 us without them, 290
+// with a load a panel and 16-bit reads (4096 x 14336 x 4096, gated).
 //
 // K is dealt to the lanes so that a lane's two 16-byte chunks of a stage are
 // neighbours, chunks 2 g and 2 g + 1 for lane group g = lane / 16: their scales are
-// the two halves of one 16-bit LDS read, which the instruction picks by itself.
+// neighbouring bytes of one word, of which the instruction picks one by itself.
 #pragma once
 
 #include "mlp2_product.hpp"
@@ -62,15 +63,15 @@ struct MxSide {
   bool gated;     // a tile's second panel is the same rows of the next matrix
 };
 
-// Where a panel's stage lies in LDS: E rows of 128 bytes of codes, then two times E words of scales.
-template <int E>
-constexpr int mx_panel() { return E * 136; }
-
+// A stage in LDS: the panels' codes, rows of 128 bytes; then the scales of the rows, a word for each 128 of K, and of the columns.
 template <class T>
 struct MxTile {
-  static constexpr int RPANEL = mx_panel<T::ER>(), CPANEL = mx_panel<T::EC>();
-  static constexpr int STAGE = T::ROWP * RPANEL + T::COLP * CPANEL;
-  static constexpr int LOADS = T::LOADS + T::ROWP + T::COLP;  // of a wave and stage
+  static constexpr int RPANEL = T::ER * 128, CPANEL = T::EC * 128, C0 = T::ROWP * RPANEL;
+  // the second 128's words lie 16 banks on, so that one read of both halves' words meets no bank twice
+  static constexpr int RPITCH = T::BM * 4 + 64, CPITCH = T::BN * 4 + 64;
+  static constexpr int RSCALES = C0 + T::COLP * CPANEL, CSCALES = RSCALES + 2 * RPITCH;
+  static constexpr int STAGE = (CSCALES + 2 * CPITCH + 1023) / 1024 * 1024;
+  static constexpr int LOADS = T::LOADS + 2;  // of a wave and stage
   static constexpr int LDS = T::NS * STAGE;
 };
 
@@ -79,68 +80,50 @@ __device__ __forceinline__ void dma4_buffer(u32x4 rsrc, uint32_t voff, uint32_t 
   asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds_addr) : "memory");
 }
 
-// Loads of one panel, stage by stage: each wave 1 KB pieces of the codes and one
-// piece of 64 rows of the scales (with fewer pieces than waves, two waves load
-// the same one).
-// The ranges: rows past the matrix's end read as zeros.  A last stage of which
-// only 128 of K exist has its other chunks asked for from past the range; their
-// scales lie past the end of the matrix's scales (zeros: 2^-127, never NaN).
-// Every panel of a side has the same offsets in its lanes; bases and ranges are scalars.
+// Loads of one panel's codes, stage by stage: rows past the matrix's end read as zeros, and so do the chunks that do not exist in a last
+// stage of 128 of K.  Every panel of a side has the same offsets in its lanes; bases and ranges are scalars.
+//
+// Chunk c = 2 g + ks of row r lies at (4 ks + g) ^ swz_inner(r): the reads of one ks meet no bank twice, as those of the 16-bit panels.
 template <class T, bool COL>
 struct MxLanes {
   static constexpr int E = COL ? T::EC : T::ER, PIECES = E * 128 / 1024 / T::NWAVES;
-  uint32_t voff[PIECES], soff;
+  uint32_t voff[PIECES];
   bool upper;  // this lane's chunk lies in the upper half of a stage
   __device__ __forceinline__ explicit MxLanes(const MxSide& s) {
     const int tid = thread_here(), lane = tid & 63, wave = uniform(tid >> 6);
-    const int row = 8 * wave + lane / 8, chunk = (lane % 8) ^ swz_inner(row), i = row & 15;
+    const int row = 8 * wave + lane / 8, place = (lane % 8) ^ swz_inner(row), chunk = 2 * (place & 3) + (place >> 2), i = row & 15;
     static_assert(T::NWAVES * 8 % 32 == 0, "swizzle and permutation repeat from piece to piece");
     const int at = COL ? (row & ~31) + 8 * (i >> 2) + 4 * ((row >> 4) & 1) + (i & 3) : row;
     upper = chunk >= 4;
     voff[0] = (uint32_t)(at * s.ld + 16 * chunk);
 #pragma unroll
     for (int j = 1; j < PIECES; ++j) voff[j] = voff[0] + (uint32_t)(j * T::NWAVES * 8 * s.ld);
-    soff = (uint32_t)((scale_k(wave) * s.rows + scale_row(wave) + lane) * 4);
   }
-  static constexpr int SP = 2 * E / 64;  // pieces of the scales
-  static_assert(T::NWAVES % SP == 0, "every piece of the scales has its waves");
-  static __device__ __forceinline__ int scale_k(int wave) { return wave % SP / (E / 64); }
-  static __device__ __forceinline__ int scale_row(int wave) { return 64 * (wave % SP % (E / 64)); }
 };
 
 template <class T, bool COL>
 struct MxPanelLoad {
   using Lanes = MxLanes<T, COL>;
   static constexpr int E = Lanes::E;
-  const char *base, *sbase;
-  uint32_t range;
-  uint32_t sleft;  // bytes of scales from sbase on (the scales of 2^18 by 2^18 are 2^31)
-  uint32_t sstep;
+  const char* base;
+  uint32_t range, lds;
   int rest;       // stages that have not been requested
   bool ragged;    // of the last one only half exists
-  uint32_t lds, slds;
 
   __device__ __forceinline__ MxPanelLoad(const MxSide& s, int i0, int panel, int stage0, int nk, uint32_t lds_off) {
     const int wave = uniform((int)threadIdx.x >> 6);
     const int which = s.gated ? panel : 0, first = i0 + (s.gated ? 0 : panel * E);
-    const int64_t matrix = which * s.rows, there = s.rows - first;
-    const int64_t rows = there < 0 ? 0 : there > E ? E : there;
-    base = (const char*)(s.codes + (matrix + first) * s.ld + (int64_t)stage0 * 128);
+    const int64_t there = s.rows - first, rows = there < 0 ? 0 : there > E ? E : there;
+    base = (const char*)(s.codes + (which * s.rows + first) * s.ld + (int64_t)stage0 * 128);
     range = (uint32_t)(rows * s.ld);  // the same for every stage: the base moves on inside the rows
-    const int64_t kb = s.ld / 64;     // groups of 128
     rest = rows > 0 ? nk : 0;
-    ragged = (stage0 + nk) * 2 > kb;
-    sbase = (const char*)(s.scales + (matrix * kb + 2 * (int64_t)stage0 * s.rows + first) * 4);
-    sleft = (uint32_t)(((kb - 2 * (int64_t)stage0) * s.rows - first) * 4);
-    sstep = (uint32_t)(8 * s.rows);
+    ragged = (stage0 + nk) * 2 > s.ld / 64;
     lds = lds_off + (uint32_t)wave * 1024u;
-    slds = lds_off + (uint32_t)(E * 128 + (Lanes::scale_k(wave) * E + Lanes::scale_row(wave)) * 4);
   }
   // The next stage, into the ring slot at stage_lds; zeros, from nowhere, behind the last one.
   __device__ __forceinline__ void load(const Lanes& l, uint32_t stage_lds) {
-    const uint64_t b = (uint64_t)base, sb = (uint64_t)sbase;  // 48 bits
+    const uint64_t b = (uint64_t)base;  // 48 bits
     const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32), rest > 0 ? range : 0u, 0x00027000u};
-    const u32x4 sr = {(uint32_t)sb, (uint32_t)(sb >> 32), rest > 0 ? sleft : 0u, 0x00027000u};
     const bool half = ragged && rest == 1;
 #pragma unroll
     for (int j = 0; j < Lanes::PIECES; ++j) {
@@ -149,58 +132,85 @@ struct MxPanelLoad {
       if (j == 0) dma16_buffer<5>(r, from, to);
       else dma16_buffer<1>(r, from, to);
     }
-    dma4_buffer(sr, l.soff, uniform(stage_lds + slds));
     base += 128;
-    sbase += sstep;
-    sleft -= sstep;
     --rest;
   }
 };
 
-__device__ __forceinline__ int pair_of(const char* lo, const char* hi) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  const u16x2 v = {*reinterpret_cast<const uint16_t*>(lo), *reinterpret_cast<const uint16_t*>(hi)};
-  return __builtin_bit_cast(int, v);
-}
+// Loads of a side's scales: a wave brings 64 rows' words of one half of the stage (the smallest tiles have fewer pieces than waves: two
+// waves bring the same).  What lies past the matrix's scales, the second half of a ragged last stage, reads as zeros: 2^-127, never NaN.
+template <class T, bool COL>
+struct MxScaleLoad {
+  static constexpr int ROWS = COL ? T::BN : T::BM, E = COL ? T::EC : T::ER, PIECES = 2 * ROWS / 64;
+  static_assert(T::NWAVES % PIECES == 0, "every piece has its waves");
+  const char* base;
+  uint32_t left, step, voff, lds;  // left: bytes from base to the end of the matrix's scales (those of 2^18 by 2^18 are 2^31)
+  int rest;                        // stages whose words exist
+  __device__ __forceinline__ MxScaleLoad(const MxSide& s, int i0, int stage0, int nk) {
+    const int tid = thread_here(), wave = uniform(tid >> 6), piece = wave % PIECES, k = piece / (ROWS / 64), r = 64 * (piece % (ROWS / 64));
+    const int panel = s.gated ? r / E : 0, first = i0 + (s.gated ? r % E : r);
+    const int64_t kb = s.ld / 64;  // groups of 128
+    const int64_t words = (2 * (int64_t)stage0 + k) * s.rows + first;
+    base = (const char*)(s.scales + (panel * s.rows * kb + words) * 4);
+    left = (uint32_t)((kb * s.rows - words) * 4);
+    step = (uint32_t)(8 * s.rows);
+    voff = (uint32_t)((tid & 63) * 4);
+    lds = (COL ? MxTile<T>::CSCALES + k * MxTile<T>::CPITCH : MxTile<T>::RSCALES + k * MxTile<T>::RPITCH) + 4 * r;
+    rest = first < s.rows ? min(nk, ((int)kb - k + 1) / 2 - stage0) : 0;
+  }
+  __device__ __forceinline__ void load(uint32_t stage_lds) {
+    const uint64_t b = (uint64_t)base;
+    const u32x4 r = {(uint32_t)b, (uint32_t)(b >> 32), rest > 0 ? left : 0u, 0x00027000u};
+    dma4_buffer(r, voff, uniform(stage_lds + lds));
+    base += step;
+    left -= step;
+    --rest;
+  }
+};
 
 // Fragments: block tm of the row side, block i of the column side; both chunks of a stage and their scales.
 template <class T>
 struct MxRowFrag {
-  uint32_t off[2], soff;
+  uint32_t off[2], soff, halves;
   __device__ __forceinline__ MxRowFrag(int wm) {
     const int lane = thread_here() & 63, g = lane >> 4;
     const int first = T::row_of(wm, 0), row = first % T::ER + (lane & 15);
     const uint32_t panel = (uint32_t)(first / T::ER * MxTile<T>::RPANEL);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) off[ks] = panel + (uint32_t)(row * 128 + (((2 * g + ks) ^ swz_inner(row)) << 4));
-    soff = panel + (uint32_t)(T::ER * 128 + ((g >> 1) * T::ER + row) * 4 + 2 * (g & 1));
+    for (int ks = 0; ks < 2; ++ks) off[ks] = panel + (uint32_t)(row * 128 + (((4 * ks + g) ^ swz_inner(row)) << 4));
+    soff = (uint32_t)(MxTile<T>::RSCALES + (g >> 1) * MxTile<T>::RPITCH + (first + (lane & 15)) * 4);
+    halves = g & 1 ? 0x07060302u : 0x05040100u;
   }
   static constexpr int half(int tm) { return (T::QUAD ? tm >> 2 : 0) * MxTile<T>::RPANEL; }
   static constexpr int blk(int tm) { return T::QUAD ? tm & 3 : tm; }
   __device__ __forceinline__ u32x4 read(const char* stage, int ks, int tm) const {
     return *reinterpret_cast<const u32x4*>(stage + half(tm) + off[ks] + blk(tm) * 16 * 128);
   }
-  // The scales of blocks tm and tm + 1: bytes 0 and 1, 2 and 3 (one for each chunk).
+  // The scales of blocks tm and tm + 1: bytes 0 and 1, 2 and 3, one for each chunk.
   __device__ __forceinline__ int scales(const char* stage, int tm) const {
-    const char* p = stage + half(tm) + soff + blk(tm) * 16 * 4;
-    return pair_of(p, p + 16 * 4);
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(stage + soff + ((T::QUAD ? tm >> 2 : 0) * 128 + blk(tm) * 16) * 4);
+    return (int)__builtin_amdgcn_perm(p[16], p[0], halves);
   }
 };
 template <class T>
 struct MxColFrag {
-  uint32_t off[2], soff;
+  uint32_t off[2], soff, halves;
   __device__ __forceinline__ MxColFrag(int wn) {
     const int lane = thread_here() & 63, g = lane >> 4, i = lane & 15, row = 32 * wn + i;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) off[ks] = (uint32_t)(row * 128 + (((2 * g + ks) ^ swz_inner(row)) << 4));
+    for (int ks = 0; ks < 2; ++ks) off[ks] = (uint32_t)(MxTile<T>::C0 + row * 128 + (((4 * ks + g) ^ swz_inner(row)) << 4));
     // LDS row 16 t + i holds matrix row 8 (i / 4) + 4 t + i % 4 of every 32; the scales are in the matrix's order
-    soff = (uint32_t)(T::EC * 128 + ((g >> 1) * T::EC + 32 * wn + 8 * (i >> 2) + (i & 3)) * 4 + 2 * (g & 1));
+    soff = (uint32_t)(MxTile<T>::CSCALES + (g >> 1) * MxTile<T>::CPITCH + (32 * wn + 8 * (i >> 2) + (i & 3)) * 4);
+    halves = g & 1 ? 0x07060302u : 0x05040100u;
   }
-  __device__ __forceinline__ u32x4 read(const char* panel, int ks, int t) const {
-    return *reinterpret_cast<const u32x4*>(panel + off[ks] + t * 16 * 128);
+  __device__ __forceinline__ u32x4 read(const char* stage, int panel, int ks, int t) const {
+    return *reinterpret_cast<const u32x4*>(stage + panel * MxTile<T>::CPANEL + off[ks] + t * 16 * 128);
   }
-  // The scales of both blocks.
-  __device__ __forceinline__ int scales(const char* panel) const { return pair_of(panel + soff, panel + soff + 16); }
+  // The scales of both blocks of a panel.
+  __device__ __forceinline__ int scales(const char* stage, int panel) const {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(stage + soff + panel * T::EC * 4);
+    return (int)__builtin_amdgcn_perm(p[4], p[0], halves);
+  }
 };
 
 // The plain loop: as product_loop, a stage's fragments read while the stage before it is multiplied.
@@ -217,17 +227,20 @@ __device__ __forceinline__ void mx_loop(const MxSide& rs, const MxSide& cs, int 
       for (int j = 0; j < T::TM; ++j) acc[p][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (nk <= 0) return;
   const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-  constexpr int C0 = T::ROWP * X::RPANEL;  // the column panels of a stage
   const MxLanes<T, false> rl(rs);
   const MxLanes<T, true> cl(cs);
   MxPanelLoad<T, false> r0(rs, m0, 0, st0, nk, 0), r1(rs, m0, T::ROWP - 1, st0, nk, (T::ROWP - 1) * X::RPANEL);
-  MxPanelLoad<T, true> c0(cs, n0, 0, st0, nk, C0), c1(cs, n0, T::COLP - 1, st0, nk, C0 + (T::COLP - 1) * X::CPANEL);
+  MxPanelLoad<T, true> c0(cs, n0, 0, st0, nk, X::C0), c1(cs, n0, T::COLP - 1, st0, nk, X::C0 + (T::COLP - 1) * X::CPANEL);
+  MxScaleLoad<T, false> rsc(rs, m0, st0, nk);
+  MxScaleLoad<T, true> csc(cs, n0, st0, nk);
   uint32_t to = lds_base;  // the ring slot that is requested next
   auto issue = [&]() {
     r0.load(rl, to);
     if constexpr (T::ROWP == 2) r1.load(rl, to);
+    rsc.load(to);
     c0.load(cl, to);
     if constexpr (T::COLP == 2) c1.load(cl, to);
+    csc.load(to);
     to = to == lds_base + (T::NS - 1) * X::STAGE ? lds_base : to + X::STAGE;
   };
   const MxRowFrag<T> rf(wm);
@@ -241,7 +254,7 @@ __device__ __forceinline__ void mx_loop(const MxSide& rs, const MxSide& cs, int 
 #pragma unroll
     for (int tm = 0; tm < T::TM; tm += 2) f.sx[tm / 2] = rf.scales(stage, tm);
 #pragma unroll
-    for (int p = 0; p < T::COLP; ++p) f.sw[p] = cf.scales(stage + C0 + p * X::CPANEL);
+    for (int p = 0; p < T::COLP; ++p) f.sw[p] = cf.scales(stage, p);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
@@ -249,20 +262,22 @@ __device__ __forceinline__ void mx_loop(const MxSide& rs, const MxSide& cs, int 
 #pragma unroll
       for (int p = 0; p < T::COLP; ++p)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) f.w[ks][p][i] = cf.read(stage + C0 + p * X::CPANEL, ks, i);
+        for (int i = 0; i < 2; ++i) f.w[ks][p][i] = cf.read(stage, p, ks, i);
     }
     stage = stage == lds + (T::NS - 1) * X::STAGE ? lds : stage + X::STAGE;
   };
   auto mma = [&](const Frags& f) {
+    auto chunk = [&](auto ks_) {
+      constexpr int ks = decltype(ks_)::value;
 #pragma unroll
-    for (int p = 0; p < T::COLP; ++p)
+      for (int p = 0; p < T::COLP; ++p)
 #pragma unroll
-      for (int tm = 0; tm < T::TM; tm += 2) {
-        mx_block<0>(acc[p][0][tm], acc[p][0][tm + 1], acc[p][1][tm], acc[p][1][tm + 1], f.w[0][p][0], f.w[0][p][1], f.x[0][tm], f.x[0][tm + 1],
-                    f.sw[p], f.sx[tm / 2]);
-        mx_block<1>(acc[p][0][tm], acc[p][0][tm + 1], acc[p][1][tm], acc[p][1][tm + 1], f.w[1][p][0], f.w[1][p][1], f.x[1][tm], f.x[1][tm + 1],
-                    f.sw[p], f.sx[tm / 2]);
-      }
+        for (int tm = 0; tm < T::TM; tm += 2)
+          mx_block<ks>(acc[p][0][tm], acc[p][0][tm + 1], acc[p][1][tm], acc[p][1][tm + 1], f.w[ks][p][0], f.w[ks][p][1], f.x[ks][tm], f.x[ks][tm + 1],
+                       f.sw[p], f.sx[tm / 2]);
+    };
+    chunk(int_constant<0>());
+    chunk(int_constant<1>());
   };
   // Every wave's loads of stage st have arrived, and every wave holds the fragments of the stages before it.
   auto resident = [&](int st) {
@@ -296,8 +311,9 @@ __device__ __forceinline__ void mx_loop(const MxSide& rs, const MxSide& cs, int 
   __syncthreads();
 }
 
-// The ping-pong loop of the 256 x 256 tile: the slots, visibility and reuse of product_pingpong.  A panel's stage is three
-// loads of a wave here (two of codes, one of scales), so the waits count three where those count two.
+// The ping-pong loop of the 256 x 256 tile: the slots, visibility and reuse of product_pingpong.  The scales of all rows come with panel A0
+// (its load is three of a wave, two of codes and one of scales) and are read with it, those of all columns with B0; so they are requested
+// again where those panels are, two slots after they were read.  The waits count the loads of the five panels behind the one waited for.
 template <class T>
 __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, int m0, int n0, int st0, int nk, Acc<T>& acc, char* lds) {
   using X = MxTile<T>;
@@ -317,50 +333,60 @@ __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, 
   const MxLanes<T, false> rl(rs);
   const MxLanes<T, true> cl(cs);
   MxPanelLoad<T, false> pa[2] = {{rs, m0, 0, st0, nk, 0}, {rs, m0, 1, st0, nk, X::RPANEL}};
-  MxPanelLoad<T, true> pb[2] = {{cs, n0, 0, st0, nk, 2 * X::RPANEL}, {cs, n0, 1, st0, nk, 2 * X::RPANEL + X::CPANEL}};
-  auto load_a = [&](int half, int st) { pa[half].load(rl, lds_base + (uint32_t)(st & 1) * X::STAGE); };  // a panel's stages come in order
-  auto load_b = [&](int half, int st) { pb[half].load(cl, lds_base + (uint32_t)(st & 1) * X::STAGE); };
+  MxPanelLoad<T, true> pb[2] = {{cs, n0, 0, st0, nk, X::C0}, {cs, n0, 1, st0, nk, X::C0 + X::CPANEL}};
+  MxScaleLoad<T, false> sa(rs, m0, st0, nk);
+  MxScaleLoad<T, true> sb(cs, n0, st0, nk);
+  auto load_a = [&](int half, int st) {  // a panel's stages come in order
+    pa[half].load(rl, lds_base + (uint32_t)(st & 1) * X::STAGE);
+    if (half == 0) sa.load(lds_base + (uint32_t)(st & 1) * X::STAGE);
+  };
+  auto load_b = [&](int half, int st) {
+    pb[half].load(cl, lds_base + (uint32_t)(st & 1) * X::STAGE);
+    if (half == 0) sb.load(lds_base + (uint32_t)(st & 1) * X::STAGE);
+  };
 
   const MxRowFrag<T> rf(wm);
   const MxColFrag<T> cf(wn);
-  struct XFrag {
-    u32x4 v[2][4];
-    int s[2];
-  };
-  struct WFrag {
-    u32x4 v[2][2];
-    int s;
-  };
-  XFrag xa, xb;
-  WFrag w0, w1;
-  auto read_a = [&](XFrag& x, int half, int st) {
+  u32x4 xa[2][4], xb[2][4], w0[2][2], w1[2][2];
+  int sx[2][2], sw[2], next[2];  // scales, two blocks a word; `next`: of the next stage's panel A1, read with A0
+  auto read_a = [&](u32x4 (&x)[2][4], int half, int st) {
     const char* stage = lds + (st & 1) * X::STAGE;
+    if (half == 0) {
 #pragma unroll
-    for (int tm = 0; tm < 4; tm += 2) x.s[tm / 2] = rf.scales(stage, 4 * half + tm);
+      for (int i = 0; i < 2; ++i) {
+        sx[0][i] = rf.scales(stage, 2 * i);
+        next[i] = rf.scales(stage, 4 + 2 * i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sx[1][i] = next[i];
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int tm = 0; tm < 4; ++tm) x.v[ks][tm] = rf.read(stage, ks, 4 * half + tm);
+      for (int tm = 0; tm < 4; ++tm) x[ks][tm] = rf.read(stage, ks, 4 * half + tm);
   };
-  auto read_b = [&](WFrag& w, int half, int st) {
-    const char* panel = lds + (st & 1) * X::STAGE + 2 * X::RPANEL + half * X::CPANEL;
-    w.s = cf.scales(panel);
+  auto read_b = [&](u32x4 (&w)[2][2], int half, int st) {
+    const char* stage = lds + (st & 1) * X::STAGE;
+    if (half == 0)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) sw[p] = cf.scales(stage, p);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w.v[ks][i] = cf.read(panel, ks, i);
+      for (int i = 0; i < 2; ++i) w[ks][i] = cf.read(stage, half, ks, i);
   };
-  auto mma = [&](const WFrag& w, const XFrag& x, auto bh, auto ah) {
-    constexpr int b = decltype(bh)::value, a = 4 * decltype(ah)::value;
-    auto both = [&](auto ks_) {
+  auto mma = [&](const u32x4 (&w)[2][2], const u32x4 (&x)[2][4], auto bh, auto ah) {
+    constexpr int b = decltype(bh)::value, h = decltype(ah)::value, a = 4 * h;
+    auto chunk = [&](auto ks_) {
       constexpr int ks = decltype(ks_)::value;
 #pragma unroll
       for (int tm = 0; tm < 4; tm += 2)
-        mx_block<ks>(acc[b][0][a + tm], acc[b][0][a + tm + 1], acc[b][1][a + tm], acc[b][1][a + tm + 1], w.v[ks][0], w.v[ks][1], x.v[ks][tm],
-                     x.v[ks][tm + 1], w.s, x.s[tm / 2]);
+        mx_block<ks>(acc[b][0][a + tm], acc[b][0][a + tm + 1], acc[b][1][a + tm], acc[b][1][a + tm + 1], w[ks][0], w[ks][1], x[ks][tm], x[ks][tm + 1],
+                     sw[b], sx[h][tm / 2]);
     };
-    both(int_constant<0>());
-    both(int_constant<1>());
+    chunk(int_constant<0>());
+    chunk(int_constant<1>());
   };
   using Lo = int_constant<0>;
   using Hi = int_constant<1>;
@@ -388,7 +414,7 @@ __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, 
   auto stage = [&](int it) {
     read_b(w0, 0, it);
     load_a(1, it + 1);
-    vm_wait(int_constant<15>());  // B1 of this stage
+    vm_wait(int_constant<12>());  // B1 of this stage
     slot_end();
     products_begin();
     mma(w0, xa, Lo(), Lo());
@@ -396,7 +422,7 @@ __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, 
 
     read_b(w1, 1, it);
     load_a(0, it + 2);
-    vm_wait(int_constant<15>());  // A1 of this stage
+    vm_wait(int_constant<13>());  // A1 of this stage
     slot_end();
     products_begin();
     mma(w1, xa, Hi(), Lo());
@@ -404,7 +430,7 @@ __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, 
 
     read_a(xb, 1, it);
     load_b(0, it + 2);
-    vm_wait(int_constant<15>());  // A0 of the next stage
+    vm_wait(int_constant<13>());  // A0 of the next stage
     slot_end();
     products_begin();
     mma(w1, xb, Hi(), Hi());
@@ -412,7 +438,7 @@ __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, 
 
     read_a(xa, 0, it + 1);
     load_b(1, it + 2);
-    vm_wait(int_constant<15>());  // B0 of the next stage
+    vm_wait(int_constant<12>());  // B0 of the next stage
     slot_end();
     products_begin();
     mma(w0, xb, Lo(), Hi());
@@ -427,7 +453,7 @@ __device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, 
   load_a(0, 1);
   load_b(0, 1);
   load_b(1, 1);
-  wait_vm<15>();  // A0, B0
+  wait_vm<12>();  // A0, B0
   slot_end();
   read_a(xa, 0, 0);
   __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
