@@ -262,7 +262,7 @@ struct Bf16Weights {
   };
   uint32_t off, row;  // of this lane's first row, and from row to row
   __device__ __forceinline__ Bf16Weights(const Experts& a, int col) {
-    const int lane = threadIdx.x & 63;
+    const int lane = thread_here() & 63;
     row = (uint32_t)(2 * a.N);
     // columns past the last are read as the last eight
     off = (uint32_t)(2 * (min(col + 8 * (lane & 15), a.N - 8) + 8 * (lane >> 4) * a.N));
@@ -295,7 +295,7 @@ struct Bf16Weights {
   __device__ static __forceinline__ void stream(const Item& it, const Experts& a, int from, int end, f32x4 (&acc)[MT][8]) {
     constexpr int SHARE = GATED ? 2 : kWaves;
     const Bf16Weights w(a, 128 * it.block);
-    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const int lane = thread_here() & 63, wave = uniform((int)threadIdx.x >> 6);
     uint32_t xo[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -610,7 +610,7 @@ struct Items {
 template <class Weights, bool GATED, class Shared>
 __device__ __forceinline__ void collect(Shared& s, const f32x4 (&acc)[Weights::J], float (&v)[8], float (&u)[8]) {
   constexpr int SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : kWaves;
-  const int tid = threadIdx.x, r = tid / 16, c = 8 * (tid % 16);
+  const int tid = thread_here(), r = tid / 16, c = 8 * (tid % 16);
   __syncthreads();  // the sums before these have been read
   Weights::put(s.sum, acc);
   __syncthreads();
@@ -639,7 +639,7 @@ template <class Weights, int ACT, int MT, int TILE, class Shared>
 __device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
   constexpr bool GATED = ACT == ACT_SWIGLU;
   constexpr int NB = GATED ? 2 : 1, COLS = Weights::cols(GATED);
-  const int tid = threadIdx.x, r = tid / 16, c = 8 * (tid % 16), col = it.block * COLS + c;
+  const int tid = thread_here(), r = tid / 16, c = 8 * (tid % 16), col = it.block * COLS + c;
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
 #pragma unroll
@@ -712,7 +712,7 @@ __device__ __forceinline__ void join_first(Shared& s, const Experts& a, const It
 // The item's part of Z W2, to memory.
 template <class Weights, int MT, class Shared>
 __device__ __forceinline__ void finish_second(Shared& s, const Experts& a, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
-  const int tid = threadIdx.x, r = tid / 16, col = it.block * 128 + 8 * (tid % 16);
+  const int tid = thread_here(), r = tid / 16, col = it.block * 128 + 8 * (tid % 16);
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
 #pragma unroll

@@ -315,155 +315,164 @@ __device__ __forceinline__ void mx_loop(const MxSide& rs, const MxSide& cs, int 
 // (its load is three of a wave, two of codes and one of scales) and are read with it, those of all columns with B0; so they are requested
 // again where those panels are, two slots after they were read.  The waits count the loads of the five panels behind the one waited for.
 template <class T>
-__device__ __forceinline__ void mx_pingpong(const MxSide& rs, const MxSide& cs, int m0, int n0, int st0, int nk, Acc<T>& acc, char* lds) {
+struct MxPingPong {
   using X = MxTile<T>;
   static_assert(T::ER == 128 && T::EC == 128 && T::ROWP == 2 && T::COLP == 2 && T::NWAVES == 8 && T::NS == 2 && T::TM == 8, "256 x 256 tile");
-  const int wave = uniform((int)threadIdx.x >> 6);
-  const int wm = wave % T::WM, wn = wave / T::WM;
-  const bool trailing = wave >= 4;
-#pragma unroll
-  for (int p = 0; p < 2; ++p)
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[p][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (nk <= 0) return;
+  MxPanelLoad<T, false> pa[2];
+  MxPanelLoad<T, true> pb[2];
+  MxScaleLoad<T, false> sa;
+  MxScaleLoad<T, true> sb;
+  int nk;
 
-  const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-  const MxLanes<T, false> rl(rs);
-  const MxLanes<T, true> cl(cs);
-  MxPanelLoad<T, false> pa[2] = {{rs, m0, 0, st0, nk, 0}, {rs, m0, 1, st0, nk, X::RPANEL}};
-  MxPanelLoad<T, true> pb[2] = {{cs, n0, 0, st0, nk, X::C0}, {cs, n0, 1, st0, nk, X::C0 + X::CPANEL}};
-  MxScaleLoad<T, false> sa(rs, m0, st0, nk);
-  MxScaleLoad<T, true> sb(cs, n0, st0, nk);
-  auto load_a = [&](int half, int st) {  // a panel's stages come in order
-    pa[half].load(rl, lds_base + (uint32_t)(st & 1) * X::STAGE);
-    if (half == 0) sa.load(lds_base + (uint32_t)(st & 1) * X::STAGE);
-  };
-  auto load_b = [&](int half, int st) {
-    pb[half].load(cl, lds_base + (uint32_t)(st & 1) * X::STAGE);
-    if (half == 0) sb.load(lds_base + (uint32_t)(st & 1) * X::STAGE);
-  };
+  __device__ __forceinline__ void load_a(const MxLanes<T, false>& rl, uint32_t ring, int half, int st) {  // a panel's stages come in order
+    pa[half].load(rl, ring + (uint32_t)(st & 1) * X::STAGE);
+    if (half == 0) sa.load(ring + (uint32_t)(st & 1) * X::STAGE);
+  }
+  __device__ __forceinline__ void load_b(const MxLanes<T, true>& cl, uint32_t ring, int half, int st) {
+    pb[half].load(cl, ring + (uint32_t)(st & 1) * X::STAGE);
+    if (half == 0) sb.load(ring + (uint32_t)(st & 1) * X::STAGE);
+  }
+  // Requests a tile's first stage and all of its second but A1; the ring is free.
+  __device__ __forceinline__ MxPingPong(const MxSide& rs, const MxSide& cs, const MxLanes<T, false>& rl, const MxLanes<T, true>& cl, int m0, int n0, int st0,
+                                        int nk_, char* lds)
+      : pa{{rs, m0, 0, st0, nk_, 0}, {rs, m0, 1, st0, nk_, X::RPANEL}},
+        pb{{cs, n0, 0, st0, nk_, X::C0}, {cs, n0, 1, st0, nk_, X::C0 + X::CPANEL}},
+        sa(rs, m0, st0, nk_),
+        sb(cs, n0, st0, nk_),
+        nk(nk_) {
+    const uint32_t ring = (uint32_t)(uintptr_t)lds;
+    load_a(rl, ring, 0, 0);
+    load_b(cl, ring, 0, 0);
+    load_b(cl, ring, 1, 0);
+    load_a(rl, ring, 1, 0);
+    load_a(rl, ring, 0, 1);
+    load_b(cl, ring, 0, 1);
+    load_b(cl, ring, 1, 1);
+  }
 
-  const MxRowFrag<T> rf(wm);
-  const MxColFrag<T> cf(wn);
-  u32x4 xa[2][4], xb[2][4], w0[2][2], w1[2][2];
-  int sx[2][2], sw[2], next[2];  // scales, two blocks a word; `next`: of the next stage's panel A1, read with A0
-  auto read_a = [&](u32x4 (&x)[2][4], int half, int st) {
-    const char* stage = lds + (st & 1) * X::STAGE;
-    if (half == 0) {
+  __device__ __forceinline__ void run(const MxLanes<T, false>& rl, const MxLanes<T, true>& cl, Acc<T>& acc, char* lds) {
+    const int wave = uniform((int)threadIdx.x >> 6);
+    const int wm = wave % T::WM, wn = wave / T::WM;
+    const bool trailing = wave >= 4;
+    const uint32_t ring = (uint32_t)(uintptr_t)lds;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        sx[0][i] = rf.scales(stage, 2 * i);
-        next[i] = rf.scales(stage, 4 + 2 * i);
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[p][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const MxRowFrag<T> rf(wm);
+    const MxColFrag<T> cf(wn);
+    u32x4 xa[2][4], xb[2][4], w0[2][2], w1[2][2];
+    int sx[2][2], sw[2], next[2];  // scales, two blocks a word; `next`: of the next stage's panel A1, read with A0
+    auto read_a = [&](u32x4 (&x)[2][4], int half, int st) {
+      const char* stage = lds + (st & 1) * X::STAGE;
+      if (half == 0) {
+  #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sx[0][i] = rf.scales(stage, 2 * i);
+          next[i] = rf.scales(stage, 4 + 2 * i);
+        }
+      } else {
+  #pragma unroll
+        for (int i = 0; i < 2; ++i) sx[1][i] = next[i];
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) sx[1][i] = next[i];
-    }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int tm = 0; tm < 4; ++tm) x[ks][tm] = rf.read(stage, ks, 4 * half + tm);
-  };
-  auto read_b = [&](u32x4 (&w)[2][2], int half, int st) {
-    const char* stage = lds + (st & 1) * X::STAGE;
-    if (half == 0)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) sw[p] = cf.scales(stage, p);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) w[ks][i] = cf.read(stage, half, ks, i);
-  };
-  auto mma = [&](const u32x4 (&w)[2][2], const u32x4 (&x)[2][4], auto bh, auto ah) {
-    constexpr int b = decltype(bh)::value, h = decltype(ah)::value, a = 4 * h;
-    auto chunk = [&](auto ks_) {
-      constexpr int ks = decltype(ks_)::value;
-#pragma unroll
-      for (int tm = 0; tm < 4; tm += 2)
-        mx_block<ks>(acc[b][0][a + tm], acc[b][0][a + tm + 1], acc[b][1][a + tm], acc[b][1][a + tm + 1], w[ks][0], w[ks][1], x[ks][tm], x[ks][tm + 1],
-                     sw[b], sx[h][tm / 2]);
+  #pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+  #pragma unroll
+        for (int tm = 0; tm < 4; ++tm) x[ks][tm] = rf.read(stage, ks, 4 * half + tm);
     };
-    chunk(int_constant<0>());
-    chunk(int_constant<1>());
-  };
-  using Lo = int_constant<0>;
-  using Hi = int_constant<1>;
+    auto read_b = [&](u32x4 (&w)[2][2], int half, int st) {
+      const char* stage = lds + (st & 1) * X::STAGE;
+      if (half == 0)
+  #pragma unroll
+        for (int p = 0; p < 2; ++p) sw[p] = cf.scales(stage, p);
+  #pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+  #pragma unroll
+        for (int i = 0; i < 2; ++i) w[ks][i] = cf.read(stage, half, ks, i);
+    };
+    auto mma = [&](const u32x4 (&w)[2][2], const u32x4 (&x)[2][4], auto bh, auto ah) {
+      constexpr int b = decltype(bh)::value, h = decltype(ah)::value, a = 4 * h;
+      auto chunk = [&](auto ks_) {
+        constexpr int ks = decltype(ks_)::value;
+  #pragma unroll
+        for (int tm = 0; tm < 4; tm += 2)
+          mx_block<ks>(acc[b][0][a + tm], acc[b][0][a + tm + 1], acc[b][1][a + tm], acc[b][1][a + tm + 1], w[ks][0], w[ks][1], x[ks][tm], x[ks][tm + 1],
+                       sw[b], sx[h][tm / 2]);
+      };
+      chunk(int_constant<0>());
+      chunk(int_constant<1>());
+    };
+    using Lo = int_constant<0>;
+    using Hi = int_constant<1>;
 
-  auto slot_end = [&]() {  // a barrier that neither the compiler's memory operations nor its products cross
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  auto vm_wait = [&](auto n) { wait_vm<decltype(n)::value>(); };
-  auto products_begin = [&]() {  // this wave's fragment reads are complete
+    auto slot_end = [&]() {  // a barrier that neither the compiler's memory operations nor its products cross
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto vm_wait = [&](auto n) { wait_vm<decltype(n)::value>(); };
+    auto products_begin = [&]() {  // this wave's fragment reads are complete
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+    };
+    auto products_end = [&]() {
+      __builtin_amdgcn_s_setprio(0);
+      slot_end();
+    };
+
+    // One stage.  It requests two stages ahead to the end: what lies behind the last stage arrives as zeros that are not read.  (With
+    // the last two stages as copies of their own, which request less, 256 registers did not hold the sums.)
+    auto stage = [&](int it) {
+      read_b(w0, 0, it);
+      load_a(rl, ring, 1, it + 1);
+      vm_wait(int_constant<12>());  // B1 of this stage
+      slot_end();
+      products_begin();
+      mma(w0, xa, Lo(), Lo());
+      products_end();
+
+      read_b(w1, 1, it);
+      load_a(rl, ring, 0, it + 2);
+      vm_wait(int_constant<13>());  // A1 of this stage
+      slot_end();
+      products_begin();
+      mma(w1, xa, Hi(), Lo());
+      products_end();
+
+      read_a(xb, 1, it);
+      load_b(cl, ring, 0, it + 2);
+      vm_wait(int_constant<13>());  // A0 of the next stage
+      slot_end();
+      products_begin();
+      mma(w1, xb, Hi(), Hi());
+      products_end();
+
+      read_a(xa, 0, it + 1);
+      load_b(cl, ring, 1, it + 2);
+      vm_wait(int_constant<12>());  // B0 of the next stage
+      slot_end();
+      products_begin();
+      mma(w0, xb, Lo(), Hi());
+      products_end();
+    };
+
+    wait_vm<12>();  // A0, B0 (what was stored since they were requested makes the wait longer, never shorter)
+    slot_end();
+    read_a(xa, 0, 0);
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_setprio(1);
-  };
-  auto products_end = [&]() {
-    __builtin_amdgcn_s_setprio(0);
-    slot_end();
-  };
 
-  // One stage.  It requests two stages ahead to the end: what lies behind the last stage arrives as zeros that are not read.  (With
-  // the last two stages as copies of their own, which request less, 256 registers did not hold the sums.)
-  auto stage = [&](int it) {
-    read_b(w0, 0, it);
-    load_a(1, it + 1);
-    vm_wait(int_constant<12>());  // B1 of this stage
-    slot_end();
-    products_begin();
-    mma(w0, xa, Lo(), Lo());
-    products_end();
-
-    read_b(w1, 1, it);
-    load_a(0, it + 2);
-    vm_wait(int_constant<13>());  // A1 of this stage
-    slot_end();
-    products_begin();
-    mma(w1, xa, Hi(), Lo());
-    products_end();
-
-    read_a(xb, 1, it);
-    load_b(0, it + 2);
-    vm_wait(int_constant<13>());  // A0 of the next stage
-    slot_end();
-    products_begin();
-    mma(w1, xb, Hi(), Hi());
-    products_end();
-
-    read_a(xa, 0, it + 1);
-    load_b(1, it + 2);
-    vm_wait(int_constant<12>());  // B0 of the next stage
-    slot_end();
-    products_begin();
-    mma(w0, xb, Lo(), Hi());
-    products_end();
-  };
-
-  // Prologue: the first stage and all of the second but A1.
-  load_a(0, 0);
-  load_b(0, 0);
-  load_b(1, 0);
-  load_a(1, 0);
-  load_a(0, 1);
-  load_b(0, 1);
-  load_b(1, 1);
-  wait_vm<12>();  // A0, B0
-  slot_end();
-  read_a(xa, 0, 0);
-  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-
-  if (trailing) slot_end();
-  for (int it = 0; it < nk; ++it) stage(it);
-  if (!trailing) slot_end();
-  wait_vm<0>();
-  __syncthreads();  // every wave is done with the ring, its loads among them, before it is reused
-}
+    if (trailing) slot_end();
+    for (int it = 0; it < nk; ++it) stage(it);
+    if (!trailing) slot_end();
+    wait_vm<0>();
+    __syncthreads();  // every wave is done with the ring, its loads among them, before it is reused
+  }
+};
 
 template <class Epi_>
 struct MxProblem {
@@ -483,15 +492,48 @@ template <class T, class P>
 __global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void k_mx_product(const P a) {
   __shared__ __align__(1024) char lds[MxTile<T>::LDS];
   constexpr int COLS = P::Epi::kGated ? T::EC : T::BN;  // result columns of a tile
-  const int item = blockIdx.x, total = a.walk.total(), s = item / total, tile = item - s * total;
-  int tm_, tn_;
-  a.walk.at(tile, tm_, tn_);
-  const int m0 = tm_ * T::BM, n0 = tn_ * COLS;
-  const int st0 = s * a.per, nk = min(a.per, a.nk - st0);
+  const int total = a.walk.total();
+  struct Place {
+    int s, tile, tm, tn, st0, nk;
+  };
+  auto place_of = [&](int item) {
+    Place p;
+    p.s = item / total;
+    p.tile = item - p.s * total;
+    a.walk.at(p.tile, p.tm, p.tn);
+    p.st0 = p.s * a.per;
+    p.nk = min(a.per, a.nk - p.st0);
+    return p;
+  };
   Acc<T> acc;
-  if constexpr (T::QUAD) mx_pingpong<T>(a.r, a.c, m0, n0, st0, nk, acc, lds);
-  else mx_loop<T>(a.r, a.c, m0, n0, st0, nk, acc, lds);
-  finish_product<T>(a, acc, 0, tile, s, tm_, tn_, lds);
+  if constexpr (T::QUAD) {
+    // One work-group to a CU goes through several tiles, and requests the next tile's first stages before it stores this one's results.
+    const MxLanes<T, false> rl(a.r);
+    const MxLanes<T, true> cl(a.c);
+    const int items = a.items();
+    int item = blockIdx.x;
+    Place p = place_of(item);
+    MxPingPong<T> loop(a.r, a.c, rl, cl, p.tm * T::BM, p.tn * COLS, p.st0, p.nk, lds);
+    for (;;) {
+      loop.run(rl, cl, acc, lds);
+      const int next = item + gridDim.x;
+      const bool more = next < items, ahead = more && a.split == 1;  // (parts of K meet through LDS)
+      const Place q = more ? place_of(next) : p;
+      if (ahead) loop = MxPingPong<T>(a.r, a.c, rl, cl, q.tm * T::BM, q.tn * COLS, q.st0, q.nk, lds);
+      finish_product<T>(a, acc, 0, p.tile, p.s, p.tm, p.tn, lds);
+      if (!more) return;
+      if (!ahead) {
+        __syncthreads();
+        loop = MxPingPong<T>(a.r, a.c, rl, cl, q.tm * T::BM, q.tn * COLS, q.st0, q.nk, lds);
+      }
+      item = next;
+      p = q;
+    }
+  } else {
+    const Place p = place_of(blockIdx.x);
+    mx_loop<T>(a.r, a.c, p.tm * T::BM, p.tn * COLS, p.st0, p.nk, acc, lds);
+    finish_product<T>(a, acc, 0, p.tile, p.s, p.tm, p.tn, lds);
+  }
 }
 
 }  // namespace mlp2
