@@ -442,13 +442,17 @@ def _stream(stream, device) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _dtype_code(dtype) -> int:
-    import torch
+_dtype_codes = {}
 
-    codes = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
-    if dtype not in codes:
+
+def _dtype_code(dtype) -> int:
+    if not _dtype_codes:
+        import torch
+
+        _dtype_codes.update({torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32})
+    if dtype not in _dtype_codes:
         raise TypeError(f"{dtype} is not supported: bfloat16 or float32")
-    return codes[dtype]
+    return _dtype_codes[dtype]
 
 
 def _check_shape(t, name, shape, dtype, device, rows=False):
@@ -635,6 +639,25 @@ class OrthoPlan(_Owned):
                                            self._on(stream)), "run")
 
 
+_calls = None
+
+
+def _torch_calls():
+    """torch's own calls for the current device and its current stream's handle, and bfloat16: the smallest calls last no longer than
+    the objects that torch.cuda's functions make of them."""
+    global _calls
+    if _calls is None:
+        import torch
+
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _calls = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device), raw, torch.bfloat16)
+    return _calls
+
+
+def _lib_of():
+    return _lib if _lib is not None else load()
+
+
 def _mx_shapes(rows, K, count):
     groups = -(-K // 128)
     return (count, rows, 64 * groups), (count, groups, rows, 4)
@@ -688,24 +711,26 @@ def mx_quantize(X, out: MxMatrix, values=None, down: bool = False, stream=None) 
     Blocks of 32 lie along a row, so that ``out`` holds ``[rows, K = cols]``, or with ``down`` down a column: the library's weights
     ``[K, N]`` become ``[N, K]``.  X's rows must be contiguous, at any distance.  ``values`` (bf16, X's shape, contiguous) receives
     what the codes stand for."""
-    import torch
-
+    device = X.device
+    current, raw_stream, bf16 = _torch_calls()
     code = _dtype_code(X.dtype)
-    if X.dim() not in (2, 3):
-        raise ValueError(f"X must have two or three dimensions, has {X.dim()}")
-    if X.device.type != "cuda" or X.device.index != torch.cuda.current_device():
+    shape, strides = tuple(X.shape), X.stride()
+    if len(shape) not in (2, 3):
+        raise ValueError(f"X must have two or three dimensions, has {len(shape)}")
+    if device.type != "cuda" or device.index != current():
         raise ValueError("X must live on the current device")
-    rows, cols = int(X.shape[-2]), int(X.shape[-1])
-    count = int(X.shape[0]) if X.dim() == 3 else 1
-    _check_mx(out, "out", cols if down else rows, rows if down else cols, count, X.device)
+    rows, cols = shape[-2:]
+    count = shape[0] if len(shape) == 3 else 1
+    _check_mx(out, "out", cols if down else rows, rows if down else cols, count, device)
     if values is not None:
-        _check_shape(values, "values", tuple(X.shape), torch.bfloat16, X.device)
-    ld = X.stride(-2) if rows > 1 else cols
-    matrix = X.stride(0) if count > 1 else rows * ld
-    if (cols > 1 and X.stride(-1) != 1) or ld < cols or (count > 1 and matrix < (rows - 1) * ld + cols):
+        _check_shape(values, "values", shape, bf16, device)
+    ld = strides[-2] if rows > 1 else cols
+    matrix = strides[0] if count > 1 else rows * ld
+    if (cols > 1 and strides[-1] != 1) or ld < cols or (count > 1 and matrix < (rows - 1) * ld + cols):
         raise ValueError("X's rows must be contiguous and apart from each other")
-    rc = load().mlp2_mx_quantize(count, rows, cols, int(bool(down)), _ptr(X), code, ld, matrix, _ptr(out.codes), _ptr(out.scales),
-                                 _ptr(values), _stream(stream, X.device))
+    stream = raw_stream(device.index) if stream is None else _stream(stream, device)
+    rc = _lib_of().mlp2_mx_quantize(count, rows, cols, 1 if down else 0, _ptr(X), code, ld, matrix, _ptr(out.codes), _ptr(out.scales),
+                                    _ptr(values), stream)
     if rc != OK:
         raise Mlp2Error(rc, "mlp2_mx_quantize")
 

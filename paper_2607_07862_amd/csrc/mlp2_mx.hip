@@ -48,7 +48,6 @@ struct Quantise {
   uint8_t *codes, *scales;
   uint16_t* values;     // or null
   int rows, cols;       // of X
-  int across, down;     // pieces of a matrix
 };
 
 template <int CTRL>
@@ -60,8 +59,7 @@ __device__ __forceinline__ uint32_t dpp(uint32_t v) {
 // whole line of 128 bytes.
 template <class X>
 __global__ __launch_bounds__(256) void k_mx_quantise_rows(const Quantise a) {
-  const int lane16 = threadIdx.x & 15, piece = blockIdx.x;
-  const int n = a.across * a.down, m = piece / n, in = piece - m * n, col0 = in / a.down * kMxGroup, row0 = in % a.down * 32;
+  const int lane16 = threadIdx.x & 15, row0 = blockIdx.x * 32, col0 = blockIdx.y * kMxGroup, m = blockIdx.z;
   const X* x = (const X*)a.X + m * a.matrix;
   const int64_t kp = mx_padded(a.cols);
   const int col = col0 + 8 * lane16, left = a.cols - col;
@@ -123,9 +121,8 @@ __device__ __forceinline__ void store_words(uint16_t* p, int n, const uint32_t (
 template <class X>
 __global__ __launch_bounds__(256) void k_mx_quantise_down(const Quantise a) {
   constexpr int C = 16 / sizeof(X);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = blockIdx.x;
-  const int n = a.across * a.down, m = piece / n, in = piece - m * n;
-  const int col = (in % a.across * 4 + wave) * (8 * C) + C * (lane & 7), block = in / a.across * 8 + (lane >> 3), k0 = block * kMxBlock;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = blockIdx.z;
+  const int col = (blockIdx.x * 4 + wave) * (8 * C) + C * (lane & 7), block = blockIdx.y * 8 + (lane >> 3), k0 = block * kMxBlock;
   const int64_t kp = mx_padded(a.rows);
   const int left = a.cols - col, deep = a.rows - k0;
   if (left <= 0 || k0 >= kp) return;
@@ -275,7 +272,7 @@ int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const 
                      void* codes, void* scales, void* values, void* stream) {
   if (count < 0 || rows < 0 || cols < 0 || (down != 0 && down != 1) || (dtype != MLP2_DTYPE_BF16 && dtype != MLP2_DTYPE_F32))
     return record_error(MLP2_ERR_INVALID_ARG);
-  if (count > 65536 || rows > (1 << 20) || cols > (1 << 20)) return record_error(MLP2_ERR_UNSUPPORTED);
+  if (count > 65535 || rows > (1 << 20) || cols > (1 << 20)) return record_error(MLP2_ERR_UNSUPPORTED);
   if (count == 0 || rows == 0 || cols == 0) return MLP2_OK;
   if (!X || !codes || !scales || ldx < cols || (count > 1 && matrix_stride < (rows - 1) * ldx + cols)) return record_error(MLP2_ERR_INVALID_ARG);
   const int64_t size = dtype == MLP2_DTYPE_F32 ? 4 : 2;
@@ -286,18 +283,12 @@ int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const 
   const Span in[] = {x}, outs[] = {{codes, count * out * kp / 2}, {scales, count * out * kp / kMxBlock}, {values, values ? count * rows * cols * 2 : 0}};
   if (outputs_overlap(in, outs)) return record_error(MLP2_ERR_INVALID_ARG);
   if (const int rc = usable_device()) return record_error(rc);
-  Quantise a{X, ldx, matrix_stride, (uint8_t*)codes, (uint8_t*)scales, (uint16_t*)values, (int)rows, (int)cols, 0, 0};
-  if (down) {
-    a.across = (int)((cols * size + 511) / 512);
-    a.down = (int)((kp + 255) / 256);
-  } else {
-    a.across = (int)(kp / kMxGroup);
-    a.down = (int)((rows + 31) / 32);
-  }
-  const int64_t pieces = count * a.across * a.down;
-  if (pieces >= 1 << 24) return record_error(MLP2_ERR_UNSUPPORTED);  // a launch holds fewer than 2^32 work-items
+  const Quantise a{X, ldx, matrix_stride, (uint8_t*)codes, (uint8_t*)scales, (uint16_t*)values, (int)rows, (int)cols};
+  // a launch's grid, so that no work-group divides: rows, then columns (down: 512 bytes of columns, then 256 rows), then matrices
+  const dim3 grid = down ? dim3((unsigned)((cols * size + 511) / 512), (unsigned)((kp + 255) / 256), (unsigned)count)
+                         : dim3((unsigned)((rows + 31) / 32), (unsigned)(kp / kMxGroup), (unsigned)count);
+  if ((int64_t)grid.x * grid.y * grid.z >= 1 << 24) return record_error(MLP2_ERR_UNSUPPORTED);  // a launch holds fewer than 2^32 work-items
   hipStream_t s = (hipStream_t)stream;
-  const unsigned grid = (unsigned)pieces;
   if (down && size == 2) k_mx_quantise_down<uint16_t><<<grid, 256, 0, s>>>(a);
   else if (down) k_mx_quantise_down<float><<<grid, 256, 0, s>>>(a);
   else if (size == 2) k_mx_quantise_rows<uint16_t><<<grid, 256, 0, s>>>(a);
