@@ -496,8 +496,9 @@ void mlp2_mx_destroy(mlp2_mx_t plan);
  * Plan it for up to max_tokens tokens: H and F multiples of 64 up to 32768, 1 <= k <= E <= 512, k <= 16, max_tokens * k <=
  * 8192, act in enum mlp2_act; w_dtype: the experts' weights in bf16, W1 [E, H, F] (SwiGLU [E, 2, H, F]: Wg, Wu) and W2 [E, F,
  * H], or MLP2_DTYPE_MXFP4, W1 as E (SwiGLU: 2 E, Wg and Wu of each in turn) matrices [F, K = H] and W2 as E matrices [H, K = F], codes and
- * scales as for mlp2_mx_quantize with down = 1.  X and the intermediate are bf16
- * either way; 4-bit weights are taken as the bf16 numbers they stand for.  All sums are fp32.
+ * scales as for mlp2_mx_quantize with down = 1.  X is bf16 either way; 4-bit weights
+ * are taken as the bf16 numbers they stand for.  The intermediate act(...) is held as the sum of two bf16 numbers (16 significant
+ * bits).  All sums are fp32.
  * A plan's calls are ordered on one stream.  NULL on failure (mlp2_last_error). */
 typedef struct mlp2_moe_s* mlp2_moe_t;
 mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, int64_t k, int act, int w_dtype);

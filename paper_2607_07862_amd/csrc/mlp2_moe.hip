@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
 // ------------------------------------------------------------------ the experts' products
 
 struct Experts {
-  const uint16_t* X;   // first: [T, H]; second: Z [T k, F]
+  const uint16_t* X;   // first: [T, H]; second: Z [2, T k, F]
   const int32_t* ids;
   const float* gates;
   const char* W;       // bf16 [E, nb, K, N], or MXFP4 codes of E nb matrices [N, K]
@@ -237,6 +237,9 @@ struct Experts {
   int most;            // parts of K
 };
 
+// An offset past the range of every buffer here: zeros, and no memory is read.  The rows that an item does not have are read there.
+constexpr uint32_t kNowhere = 0x80000000u;
+
 // An item of work: up to `tile` slots of an expert, a block of columns, a part of K.
 struct Item {
   int expert, block, split, first, rows;
@@ -249,16 +252,16 @@ struct Item {
 struct Bf16Weights {
   static constexpr int STEP = 32;  // K of a step (of one wave)
   static constexpr int ITEM = 8;   // what an item costs beside its steps
-  static constexpr int MOST = 4;   // blocks of 16 rows that one pass over the weights serves
-  static constexpr int WAVES = kWaves;
+  static constexpr int most(bool second) { return second ? 2 : 4; }  // blocks of 16 rows that one pass over the weights serves
+  static constexpr int WAVES = kWaves, COPIES = 4, ROWS = 64;  // copies of sums in LDS; rows of an item, at most
   static constexpr int RING = 2;   // steps in registers
   static constexpr int cols(bool) { return 128; }     // result columns of an item
   static constexpr int UP_WAVE = 2, UP_COL = 0;       // where the second matrix's sums are
   static constexpr int J = 8;                         // instruction groups of a wave: 16 columns each
   static constexpr int resident(int most) { return most == 1 ? 3 : 2; }  // work-groups of a CU, by their registers
-  template <int MT>
+  template <int XT>  // blocks of 16 rows of X; of Z two for each
   struct Regs {
-    u32x4 w[8], x[MT];
+    u32x4 w[8], x[XT];
   };
   uint32_t off, row;  // of this lane's first row, and from row to row
   __device__ __forceinline__ Bf16Weights(const Experts& a, int col) {
@@ -268,26 +271,26 @@ struct Bf16Weights {
     off = (uint32_t)(2 * (min(col + 8 * (lane & 15), a.N - 8) + 8 * (lane >> 4) * a.N));
   }
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return (int64_t)a.K * a.N * 2; }
-  template <int MT>
   // Steps from `end` on load zeros, from nowhere.
-  __device__ __forceinline__ void load(Regs<MT>& r, const char* w, const uint16_t* x, const uint32_t (&xo)[MT], const Experts& a, int step, int end) const {
-    const int range = step < end ? -1 : 0;
+  template <int XT>
+  __device__ __forceinline__ void load(Regs<XT>& r, const char* w, const uint16_t* x, const uint32_t (&xo)[XT], const Experts& a, int step, int end) const {
+    const int range = step < end ? 0x7FFFFFFF : 0;
     const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(w + (int64_t)step * STEP * a.N * 2), 0, range, 0x00027000);
     const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + step * STEP), 0, range, 0x00027000);
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.w[i] = __builtin_amdgcn_raw_buffer_load_b128(wr, (int)off, (int)(i * row), kNt);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) r.x[m] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)xo[m], 0, 0);
+    for (int m = 0; m < XT; ++m) r.x[m] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)xo[m], 0, 0);
   }
-  template <int MT>
-  __device__ __forceinline__ void multiply(const Regs<MT>& r, f32x4 (&acc)[MT][8]) const {
+  template <int MT, int XT>
+  __device__ __forceinline__ void multiply(const Regs<XT>& r, f32x4 (&acc)[MT][8]) const {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       u32x4 f;
 #pragma unroll
       for (int d = 0; d < 4; ++d) f[d] = __builtin_amdgcn_perm(r.w[2 * d + 1][j / 2], r.w[2 * d][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) acc[m][j] = Bf16::mfma(f, r.x[m], acc[m][j]);
+      for (int m = 0; m < XT; ++m) acc[m * MT / XT][j] = Bf16::mfma(f, r.x[m], acc[m * MT / XT][j]);
     }
   }
   // Sums over this wave's steps of from .. end - 1: every fourth, with a gate every second one of the wave's matrix.
@@ -296,11 +299,14 @@ struct Bf16Weights {
     constexpr int SHARE = GATED ? 2 : kWaves;
     const Bf16Weights w(a, 128 * it.block);
     const int lane = thread_here() & 63, wave = uniform((int)threadIdx.x >> 6);
-    uint32_t xo[MT];
+    constexpr int XT = SECOND ? 2 * MT : MT;
+    uint32_t xo[XT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const int r = 16 * m + (lane & 15), slot = it.slots[r < it.rows ? r : 0];
-      xo[m] = (uint32_t)(((int64_t)(SECOND ? slot : slot / a.k) * a.K + 8 * (lane >> 4)) * 2);
+      const uint32_t to = (uint32_t)(((int64_t)(SECOND ? slot : slot / a.k) * a.K + 8 * (lane >> 4)) * 2);
+      xo[m * XT / MT] = r < it.rows ? to : kNowhere;
+      if constexpr (SECOND) xo[2 * m + 1] = r < it.rows ? to + (uint32_t)((int64_t)a.T * a.k * a.K * 2) : kNowhere;
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -308,16 +314,16 @@ struct Bf16Weights {
     // A ring of steps in registers: while one is multiplied the others are in flight.  What is requested behind the last step arrives
     // as zeros, so that every request is unconditional and the waits count the same loads on every path.  (Four steps in place of two
     // streamed no faster.)
-    Regs<MT> ring[RING];
+    Regs<XT> ring[RING];
     int step = from + wave % SHARE;
 #pragma unroll
-    for (int d = 0; d < RING - 1; ++d) w.load<MT>(ring[d], base, a.X, xo, a, step + d * SHARE, end);
+    for (int d = 0; d < RING - 1; ++d) w.load<XT>(ring[d], base, a.X, xo, a, step + d * SHARE, end);
     for (; step < end; step += RING * SHARE) {
 #pragma unroll
       for (int d = 0; d < RING; ++d) {
-        w.load<MT>(ring[(d + RING - 1) % RING], base, a.X, xo, a, step + (d + RING - 1) * SHARE, end);
+        w.load<XT>(ring[(d + RING - 1) % RING], base, a.X, xo, a, step + (d + RING - 1) * SHARE, end);
         __builtin_amdgcn_sched_barrier(0);
-        w.multiply<MT>(ring[d], acc);
+        w.multiply<MT, XT>(ring[d], acc);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -348,26 +354,28 @@ struct Bf16Weights {
 // of the stage's k with half of its rows.  A lane turns 16 codes of a row into two bf16 operands (exactly: two significant bits and a power of
 // two).  Two waves to a SIMD: with one, reads, conversions and products waited for each other (3.8 TB/s).
 struct MxWeights {
-  static constexpr int WAVES = 8;
+  static constexpr int WAVES = 8, COPIES = 2, ROWS = 32;
   static constexpr int STEP = 256;  // (of all waves)
   static constexpr int ITEM = 2;
-  static constexpr int MOST = 2;
+  static constexpr int most(bool second) { return second ? 1 : 2; }
   static constexpr int resident(int) { return 1; }
   static constexpr int cols(bool gated) { return gated ? 64 : 128; }   // result columns of an item
   static constexpr int UP_WAVE = 0, UP_COL = 64;                       // where the second matrix's sums are
   static constexpr int J = 4;                                          // instruction groups of a wave: 16 columns each
   static constexpr int CODES = 16384, X0 = CODES + 1024;
-  static constexpr int stage(int mt) { return X0 + 8192 * mt; }
-  static constexpr int depth(int mt) { return mt == 1 ? 4 : 3; }       // stages of the ring
-  static constexpr int loads(int mt) { return 2 + 1 + mt; }            // of a wave and stage
+  // by blocks of 16 rows of X (of Z two for each)
+  static constexpr int stage(int xt) { return X0 + 8192 * xt; }
+  static constexpr int DEPTH = 4;  // stages of the ring
+  static constexpr int loads(int xt) { return 2 + 1 + xt; }  // of a wave and stage
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return a.N * (mx_padded(a.K) / 2); }
 
   // The stages of an item, one by one.
   template <int MT, bool GATED, bool SECOND>
   struct Requests {
+    static constexpr int XT = SECOND ? 2 * MT : MT;
     const char *base, *sbase;
     int step, rest, last, length, groups;  // the next step, how many are left, the part's last one and length
-    uint32_t wo[2], so, xo[MT];
+    uint32_t wo[2], so, xo[XT];
     __device__ __forceinline__ void begin(const Item& it, const Experts& a, int from, int to) {
       const int lane = thread_here() & 63, wave = uniform((int)threadIdx.x >> 6), col = it.block * cols(GATED);
       const int64_t ld = mx_padded(a.K) / 2;
@@ -393,7 +401,9 @@ struct MxWeights {
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int r = 2 * (wave + 8 * i) + (lane >> 5), slot = it.slots[r < it.rows ? r : 0];
-        xo[i] = (uint32_t)((int64_t)(SECOND ? slot : slot / a.k) * a.K * 2 + 16 * x_chunk(lane, wave));
+        const uint32_t at = (uint32_t)((int64_t)(SECOND ? slot : slot / a.k) * a.K * 2 + 16 * x_chunk(lane, wave));
+        xo[i * XT / MT] = r < it.rows ? at : kNowhere;
+        if constexpr (SECOND) xo[2 * i + 1] = r < it.rows ? at + (uint32_t)((int64_t)a.T * a.k * a.K * 2) : kNowhere;
       }
     }
     // Chunk c of row r of the codes lies at c ^ (r / 2 % 8), chunk c of row r of X at c ^ (r % 16).
@@ -409,25 +419,26 @@ struct MxWeights {
       const u32x4 sr = {uniform((uint32_t)sb), uniform((uint32_t)(sb >> 32)), half && (wave >> 1 & 1) ? 0u : range, 0x00027000u};
       const u32x4 xr = {uniform((uint32_t)xb), uniform((uint32_t)(xb >> 32)), range, 0x00027000u};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) dma16_stream(wr, half && chunk(lane, i) >= 4 ? 0x80000000u : wo[i], uniform(to + 2048u * wave + 1024 * i));
+      for (int i = 0; i < 2; ++i) dma16_stream(wr, half && chunk(lane, i) >= 4 ? kNowhere : wo[i], uniform(to + 2048u * wave + 1024 * i));
       dma4_buffer(sr, so, uniform(to + CODES + 256u * (wave & 3)));
       const int deep = (a.K - step * STEP) / 8;  // chunks of X that exist
 #pragma unroll
-      for (int i = 0; i < MT; ++i) dma16_buffer<5>(xr, x_chunk(lane, wave) >= deep ? 0x80000000u : xo[i], uniform(to + X0 + 1024u * (wave + 8 * i)));
+      for (int i = 0; i < XT; ++i) dma16_buffer<5>(xr, x_chunk(lane, wave) >= deep ? kNowhere : xo[i], uniform(to + X0 + 1024u * (wave + 8 * i)));
       step = step == last ? step + 1 - length : step + 1;
       --rest;
     }
   };
 
-  // One stage: a quarter of its k, one half of its rows; the first HERE blocks of X's rows.  Lane group g has 16 k of every row, two
+  // One stage: a quarter of its k, one half of its rows; the first HERE blocks of X's rows, of Z both numbers.  Lane group g has 16 k of every row, two
   // operands; everything that the stage holds for this lane is read before the first product.
-  template <int MT, int HERE>
+  template <int MT, int HERE, bool SECOND>
   __device__ static __forceinline__ void multiply(const char* stage, f32x4 (&acc)[MT][J]) {
+    constexpr int EACH = SECOND ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15, k = wave % 4, upper = wave / 4;
     const char* codes = stage + 8192 * upper + 128 * i16 + 16 * ((2 * k + (g >> 1)) ^ (i16 >> 1)) + 8 * (g & 1);
     const char* scales = stage + CODES + 512 * (k >> 1) + 256 * upper + 4 * i16 + 2 * (k & 1) + (g >> 1);
     const char* xs = stage + X0 + 512 * i16;
-    u32x4 x[HERE][2];
+    u32x4 x[HERE * EACH][2];
     u32x2 c[J];
     uint32_t sc[J];
 #pragma unroll
@@ -436,7 +447,7 @@ struct MxWeights {
       sc[j] = *reinterpret_cast<const uint8_t*>(scales + 64 * j);
     }
 #pragma unroll
-    for (int m = 0; m < HERE; ++m)
+    for (int m = 0; m < HERE * EACH; ++m)
 #pragma unroll
       for (int p = 0; p < 2; ++p) x[m][p] = *reinterpret_cast<const u32x4*>(xs + 8192 * m + 16 * ((8 * k + 2 * g + p) ^ i16));
     __builtin_amdgcn_sched_barrier(0);
@@ -451,16 +462,22 @@ struct MxWeights {
         f[2] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j][p], scale, 2));
         f[3] = __builtin_bit_cast(uint32_t, (mx_bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j][p], scale, 3));
 #pragma unroll
-        for (int m = 0; m < HERE; ++m) acc[m][j] = Bf16::mfma(f, x[m][p], acc[m][j]);
+        for (int m = 0; m < HERE * EACH; ++m) acc[m / EACH][j] = Bf16::mfma(f, x[m][p], acc[m / EACH][j]);
       }
   }
-  // Where the four sums of instruction group j lie: columns 16 j + 4 g + i of the wave's half.
+  // Where the four sums of instruction group j lie: columns 16 j + 4 g + i of the wave's half.  Two copies, to which two quarters of k each
+  // are added: with four there would be no room for the ring's last stage.
   template <class Sums>
   __device__ static __forceinline__ void put(Sums& sum, const f32x4 (&c)[J]) {
-    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    float* to = sum[wave % 4][lane & 15] + 64 * (wave / 4) + 4 * (lane >> 4);
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), k = wave % 4;
+    float* to = sum[k % 2][lane & 15] + 64 * (wave / 4) + 4 * (lane >> 4);
+    if (k >= 2)
 #pragma unroll
-    for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4*>(to + 16 * j) = c[j];
+      for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4*>(to + 16 * j) = c[j];
+    __syncthreads();
+    if (k < 2)
+#pragma unroll
+      for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4*>(to + 16 * j) += c[j];
   }
 };
 
@@ -472,10 +489,10 @@ struct MoeShared {
   static constexpr bool kIds = RING > 0;
   alignas(1024) char ring[RING ? RING : 16];
   int16_t ids[kIds ? kIdsInLds : 1];
-  float sum[kWaves][16][128 + 4];  // the waves' sums; behind the last item, tokens that are complete
+  float sum[Weights::COPIES][16][128 + 4];  // the waves' sums; behind the last item, tokens that are complete
   int count[kMostExperts];  // slots of an expert
   int start[kMostExperts];  // its first unit (an expert's chunk of rows and a block of columns)
-  int rows[2][kWave][64];  // slots of an item and of the next one, a copy for each wave
+  int rows[2][kWave][Weights::ROWS];  // slots of an item and of the next one, a copy for each wave
   int total, found;
 };
 
@@ -605,11 +622,11 @@ struct Items {
   }
 };
 
-// The waves' sums of one block of rows meet in LDS, four copies of them.  Thread 16 r + c / 8 (of the first 256) gets eight columns of row r:
+// The waves' sums of one block of rows meet in LDS.  Thread 16 r + c / 8 (of the first 256) gets eight columns of row r:
 // v those from column c on, and with a gate u those of the second matrix.
 template <class Weights, bool GATED, class Shared>
 __device__ __forceinline__ void collect(Shared& s, const f32x4 (&acc)[Weights::J], float (&v)[8], float (&u)[8]) {
-  constexpr int SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : kWaves;
+  constexpr int SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : Weights::COPIES;
   const int tid = thread_here(), r = tid / 16, c = 8 * (tid % 16);
   __syncthreads();  // the sums before these have been read
   Weights::put(s.sum, acc);
@@ -626,12 +643,23 @@ __device__ __forceinline__ void collect(Shared& s, const f32x4 (&acc)[Weights::J
     }
 }
 
+// act of eight columns of a slot's row, to Z.  Z is held as two bf16 numbers, the nearest one and what that leaves: 16 significant bits.
+// So the second product adds no rounding of its own to that of Y: with one bf16 number, Y's error against 64 bits was 1.4 times that of
+// rounding Y alone.  It costs two instructions and two reads of Z for each of one, where the weights' stream is what bounds it.
 template <int ACT>
-__device__ __forceinline__ u32x4 activate(const float (&v)[8], const float (&u)[8]) {
-  float z[8];
+__device__ __forceinline__ void store_z(const Experts& a, int slot, int col, const float (&v)[8], const float (&u)[8]) {
+  float z[8], low[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) z[e] = ACT == ACT_SWIGLU ? silu(v[e]) * u[e] : ACT == ACT_GELU_TANH ? gelu_tanh(v[e]) : v[e];
-  return pack_bf16x8(z);
+  const u32x4 high = pack_bf16x8(z);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float h = __builtin_bit_cast(float, e & 1 ? high[e / 2] & 0xFFFF0000u : high[e / 2] << 16);
+    low[e] = __builtin_isfinite(h) ? z[e] - h : 0.f;  // infinities and NaN stand in the first number alone
+  }
+  uint16_t* to = a.out + (int64_t)slot * a.N + col;
+  *reinterpret_cast<u32x4*>(to) = high;
+  *reinterpret_cast<u32x4*>(to + (int64_t)a.T * a.k * a.N) = pack_bf16x8(low);
 }
 
 // Z = act(X W1) of the item's rows, or a part of X W1, from the waves' sums.
@@ -650,7 +678,7 @@ __device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const 
     if (tid >= 256 || c >= COLS || col >= a.N || 16 * m + r >= it.rows) continue;
     const int slot = it.slots[16 * m + r];
     if (items.splits == 1) {
-      *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col) = activate<ACT>(v, u);
+      store_z<ACT>(a, slot, col, v, u);
     } else {
       const uint32_t to = (uint32_t)((it.split * slots + slot) * NB * a.N + col) * 4;
       part.store16(to, f32x4{v[0], v[1], v[2], v[3]});
@@ -704,7 +732,7 @@ __device__ __forceinline__ void join_first(Shared& s, const Experts& a, const It
             if (NB == 2) u[e] += q + d < items.splits ? x[d][2 * NB - 2 + e / 4][e % 4] : 0.f;
           }
       }
-      *reinterpret_cast<u32x4*>(a.out + (int64_t)slot * a.N + col) = activate<ACT>(v, u);
+      store_z<ACT>(a, slot, col, v, u);
     }
   }
 }
@@ -856,7 +884,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Bf16Weights
 template <int ACT, int MT, bool SECOND>
 __global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
   using W = MxWeights;
-  constexpr int NS = W::depth(MT), STAGE = W::stage(MT);
+  constexpr int XT = SECOND ? 2 * MT : MT, NS = W::DEPTH, STAGE = W::stage(XT);
   constexpr bool GATED = ACT == ACT_SWIGLU && !SECOND;
   __shared__ MoeShared<W, STAGE * NS> s;
   const Items<16 * MT> items(s, a);
@@ -892,15 +920,15 @@ __global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
         for (int j = 0; j < W::J; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
       const int steps = items.end(a, it) - items.from(it), stages = max(NS - 1, steps);
       for (int i = 0; i < stages; ++i) {
-        wait_vm<(NS - 2) * W::loads(MT)>();
+        wait_vm<(NS - 2) * W::loads(XT)>();
         __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): this wave holds what it read of the stage before
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         request();  // into the place of the stage before
         if (i < steps) {
           const char* stage = s.ring + at * STAGE;
-          if (MT == 1 || it.rows > 16) W::multiply<MT, MT>(stage, acc);
-          else W::multiply<MT, 1>(stage, acc);
+          if (MT == 1 || it.rows > 16) W::multiply<MT, MT, SECOND>(stage, acc);
+          else W::multiply<MT, 1, SECOND>(stage, acc);
         }
         at = at == NS - 1 ? 0 : at + 1;
       }
@@ -969,10 +997,10 @@ void launch(const Experts& a, unsigned grid, hipStream_t s) {
   const bool few = narrow((int64_t)a.T * a.k, a.E);
   if constexpr (std::is_same_v<Weights, Bf16Weights>) {
     if (few) k_moe_bf16<ACT, 1, SECOND><<<grid, 256, 0, s>>>(a);
-    else k_moe_bf16<ACT, Weights::MOST, SECOND><<<grid, 256, 0, s>>>(a);
+    else k_moe_bf16<ACT, Weights::most(SECOND), SECOND><<<grid, 256, 0, s>>>(a);
   } else {
     if (few) k_moe_mx<ACT, 1, SECOND><<<grid, 512, 0, s>>>(a);
-    else k_moe_mx<ACT, Weights::MOST, SECOND><<<grid, 512, 0, s>>>(a);
+    else k_moe_mx<ACT, Weights::most(SECOND), SECOND><<<grid, 512, 0, s>>>(a);
   }
 }
 
@@ -980,9 +1008,9 @@ template <class Weights>
 hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t* ids, const float* gates, const void* W1, const void* W1s, const void* W2,
                    const void* W2s, void* Y, hipStream_t s) {
   const int64_t slots = T * p->k, active = slots < p->E ? slots : p->E;  // experts that have a slot, at most
-  const int most_blocks = narrow(slots, p->E) ? 1 : Weights::MOST;
-  const int64_t resident = (int64_t)Weights::resident(most_blocks) * p->num_cus;  // work-groups that the chip holds at once
-  auto fill = [&](Experts& a, int64_t K, int64_t N, int64_t width, bool gated, float join) {  // width: floats of a slot's part
+  auto fill = [&](Experts& a, bool second, int64_t K, int64_t N, int64_t width, bool gated, float join) {  // width: floats of a slot's part
+    const int most_blocks = narrow(slots, p->E) ? 1 : Weights::most(second);
+    const int64_t resident = (int64_t)Weights::resident(most_blocks) * p->num_cus;  // work-groups that the chip holds at once
     const int64_t tile = 16 * most_blocks, room = p->part_floats / (slots * width);
     a.K = (int)K;
     a.N = (int)N;
@@ -1009,7 +1037,7 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
   a.scales = (const char*)W1s;
   a.out = p->Z;
   a.arrived = p->joined;
-  const unsigned g1 = fill(a, p->H, p->F, p->nb * p->F, p->nb == 2, 0.5f * Weights::ITEM);
+  const unsigned g1 = fill(a, false, p->H, p->F, p->nb * p->F, p->nb == 2, 0.5f * Weights::ITEM);
   if (p->act == MLP2_ACT_SWIGLU) launch<Weights, ACT_SWIGLU, false>(a, g1, s);
   else if (p->act == MLP2_ACT_GELU_TANH) launch<Weights, ACT_GELU_TANH, false>(a, g1, s);
   else launch<Weights, ACT_IDENTITY, false>(a, g1, s);
@@ -1019,7 +1047,7 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
   b.scales = (const char*)W2s;
   b.out = (uint16_t*)Y;
   b.arrived = p->arrived;
-  const unsigned g2 = fill(b, p->F, p->H, p->H, false, 0.03f * Weights::ITEM * p->k);
+  const unsigned g2 = fill(b, true, p->F, p->H, p->H, false, 0.03f * Weights::ITEM * p->k);
   launch<Weights, ACT_IDENTITY, true>(b, g2, s);
   return hipGetLastError();
 }
@@ -1085,7 +1113,7 @@ mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, in
   // room for 16 parts of K of either product while they are small; one part of the second always fits
   const int64_t wide = p->nb * F > H ? p->nb * F : H, all = kMostParts * slots * wide, few = (int64_t)16 << 20, one = slots * H;
   p->part_floats = all < few ? all : one > few ? one : few;
-  const int64_t z = round_up(slots * F * 2, 256), part = round_up(p->part_floats * 4, 256);
+  const int64_t z = round_up(2 * slots * F * 2, 256), part = round_up(p->part_floats * 4, 256);
   const int64_t logits = round_up(max_tokens * ((H + route_part(H) - 1) / route_part(H)) * E * 8, 256);
   const int64_t tokens_blocks = max_tokens * ((H + 127) / 128), slots_blocks = slots * (F / 64);
   const int64_t counters = (tokens_blocks + slots_blocks + groups * kLine) * 4;

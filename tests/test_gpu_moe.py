@@ -25,9 +25,9 @@ def weights(gen, E, H, F, act, w):
 
 
 def expected(X, ids, gates, of, E, name):
-    """Y and its bounds.  Each expert's Z is rounded to bf16 (2^-8 of it) after sums that are off by at most (H + 8) 2^-24 of their terms;
-    its second product by (F + 8) 2^-24 of its terms, and by the roundings of Z: independent, so within the lesser of the worst case and
-    six standard deviations of their sum; the weighted sum adds a rounding a slot and the output's own."""
+    """Y and its bounds.  Each expert's Z, after sums that are off by at most (H + 8) 2^-24 of their terms, is held as two bf16 numbers,
+    the second a rounding (2^-8) of what the first left (at most 2^-8 of Z); its second product is off by (2 F + 40) 2^-24 of its terms, two
+    for each of Z; the weighted sum adds a rounding a slot and the output's own."""
     T, H = X.shape
     Y, tol = np.zeros((T, H)), np.zeros((T, H))
     for e in range(E):
@@ -42,7 +42,7 @@ def expected(X, ids, gates, of, E, name):
         dz = act_tol(name, p, dp)
         F = z.shape[1]
         y, mag = z @ W2, np.abs(z) @ np.abs(W2)
-        off = (1 + U16) * (dz @ np.abs(W2)) + 1.02 * U16 * min(F**0.5, 3.5) * np.sqrt((z * z) @ (W2 * W2)) + (F + 40) * U32 * mag
+        off = (1 + U16) * (dz @ np.abs(W2)) + U16 * U16 * mag + (2 * F + 40) * (1 + U16) * U32 * mag
         np.add.at(Y, token, g * y)
         np.add.at(tol, token, np.abs(g) * (off + 16 * U32 * mag))
     return Y, tol + U16 * (np.abs(Y) + tol) + 1e-37
