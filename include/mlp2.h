@@ -469,8 +469,8 @@ typedef struct mlp2_mx_s* mlp2_mx_t;
  * NaN or an infinity makes its block NaN (codes 0, scale 255).  `values` (or
  * NULL) receives what codes and scales stand for, bf16 [count, rows, cols] in
  * X's order; they are bf16 numbers, so nothing is rounded again.
- * 0 <= count <= 65535, 0 <= rows, cols <= 1<<20 (0: nothing to do), and at most 2^24 pieces of 32 x 128 (down: 512 bytes of columns by
- * 256 rows).  The current device, no workspace. */
+ * 0 <= count <= 65535, 0 <= rows, cols <= 1<<20 (0: nothing to do), ldx and matrix_stride <= 1<<40, and at most 2^24 pieces of 32 x 128
+ * (down: 512 bytes of columns by 256 rows).  The current device, no workspace. */
 int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const void* X, int dtype, int64_t ldx, int64_t matrix_stride,
                      void* codes, void* scales, void* values, void* stream);
 
@@ -498,7 +498,9 @@ void mlp2_mx_destroy(mlp2_mx_t plan);
  * H], or MLP2_DTYPE_MXFP4, W1 as E (SwiGLU: 2 E, Wg and Wu of each in turn) matrices [F, K = H] and W2 as E matrices [H, K = F], codes and
  * scales as for mlp2_mx_quantize with down = 1.  X is bf16 either way; 4-bit weights
  * are taken as the bf16 numbers they stand for.  The intermediate act(...) is held as the sum of two bf16 numbers (16 significant
- * bits).  All sums are fp32.
+ * bits), so an infinite weight of W2 may give NaN where one factor would give an infinity.  All sums are fp32.  The workspace holds that
+ * intermediate (4 bytes an element), up to 64 MB of partial sums or one fp32 [max_tokens * k, H] if that is more, and the router's: up
+ * to 64 fp64 [max_tokens, E].
  * A plan's calls are ordered on one stream.  NULL on failure (mlp2_last_error). */
 typedef struct mlp2_moe_s* mlp2_moe_t;
 mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, int64_t k, int act, int w_dtype);

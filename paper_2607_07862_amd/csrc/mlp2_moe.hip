@@ -46,6 +46,9 @@ struct Far {
   }
 };
 
+// An offset past the range of every buffer here but Far's: zeros, and no memory is read.  Rows that do not exist are read there.
+constexpr uint32_t kNowhere = 0x80000000u;
+
 // dma16_buffer for what is read once.
 __device__ __forceinline__ void dma16_stream(u32x4 rsrc, uint32_t voff, uint32_t lds_addr) {
   asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen nt lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds_addr) : "memory");
@@ -108,7 +111,7 @@ __device__ __forceinline__ void choose_experts(const double* logits, int E, int 
     int at = kMostExperts;  // this lane's best expert
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (!(gone >> i & 1) && (v[i] > best || at == kMostExperts)) {
+      if (64 * i < E && !(gone >> i & 1) && (v[i] > best || at == kMostExperts)) {
         best = v[i];
         at = lane + 64 * i;
       }
@@ -133,47 +136,56 @@ __device__ __forceinline__ void choose_experts(const double* logits, int E, int 
 
 // Logits of TT tokens over one part of K, in fp64: which experts are chosen hangs on logits next to each other, and fp32 sums would
 // put some of them in another order.  256 threads are `width` experts by 256 / width rows of K.  Latencies bound it: the part's X and
-// the first weights are requested together, the parts' sums are read all at once.
+// the first weights are requested together, the parts' sums are read all at once.  (6.2 us for one token of 4096 and eight experts, 8.4
+// for 16 of 2048 and 64, 10.2 for nine of 1024 and 251, 35 for 128 of 7168 and 256, there by the reads of X from LDS.)
 template <class W, int TT>
 __global__ __launch_bounds__(256) void k_moe_route(const Route a) {
   constexpr int MOST = TT * kMostExperts > TT * kRoutePart ? TT * kMostExperts : TT * kRoutePart;
   __shared__ __align__(16) double lds[256 * TT > MOST ? 256 * TT : MOST];
   __shared__ int seen;
-  constexpr int AHEAD = 16;
+  constexpr int AHEAD = 16, GROUP = 4;  // rows of K of a thread that are requested and multiplied at a time
   const int tid = threadIdx.x, t0 = blockIdx.x * TT, split = blockIdx.y;
   const int width = 1 << a.width, sub = tid >> a.width, subs = 256 >> a.width, e0 = tid & (width - 1);
   const int from = split * a.per, deep = min(a.H - from, a.per);
-  const W* Wr = (const W*)a.Wr + (int64_t)from * a.E;
+  const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)((const W*)a.Wr + (int64_t)from * a.E), 0, deep * a.E * (int)sizeof(W), 0x00027000);
   const int chunks = (a.E + width - 1) >> a.width;  // of experts; one but for E > 256
   for (int c = 0; c < chunks; ++c) {
     const int e = (c << a.width) + e0;
+    // from this thread's first row on; zeros past the part and for the experts past the last
+    const uint32_t first = e < a.E ? (uint32_t)((sub * a.E + e) * (int)sizeof(W)) : kNowhere;
     W w[AHEAD];
     auto request = [&](int k0) {
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
-        const int kk = k0 + i * subs;
-        w[i] = Wr[kk < deep && e < a.E ? (int64_t)kk * a.E + e : 0];
+        const int off = (int)(first + (uint32_t)((k0 + i * subs) * a.E * (int)sizeof(W)));
+        if constexpr (sizeof(W) == 4) w[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(wr, off, 0, 0));
+        else w[i] = __builtin_amdgcn_raw_buffer_load_b16(wr, off, 0, 0);
       }
     };
-    request(sub);
+    request(0);
     if (c) __syncthreads();
-    for (int kk = tid & 63; kk < deep; kk += 64)
+    // (rows of K behind the part's last: zeros, as their weights are, so that the products need no branch; behind one, each row waited for
+    // its own read of LDS, 190 clocks)
+    const int padded = (deep + GROUP * subs - 1) / (GROUP * subs) * (GROUP * subs);
+    for (int kk = tid & 63; kk < padded; kk += 64)
 #pragma unroll
-      for (int t = tid >> 6; t < TT; t += 4) lds[kk * TT + t] = t0 + t < a.T ? widen(a.X[(int64_t)(t0 + t) * a.H + from + kk]) : 0.0;
+      for (int t = tid >> 6; t < TT; t += 4) lds[kk * TT + t] = t0 + t < a.T && kk < deep ? widen(a.X[(int64_t)(t0 + t) * a.H + from + kk]) : 0.0;
     __syncthreads();
     double acc[TT] = {};
-    for (int k0 = sub; k0 < deep; k0 += AHEAD * subs) {
+    for (int k0 = 0; k0 < deep; k0 += AHEAD * subs) {
       W now[AHEAD];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) now[i] = w[i];
-      request(k0 + AHEAD * subs);
+      if (k0 + AHEAD * subs < deep) request(k0 + AHEAD * subs);
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int kk = k0 + i * subs;
-        if (kk < deep) {
-          const double v = widen(now[i]);
+      for (int g = 0; g < AHEAD; g += GROUP) {
+        if (k0 + g * subs >= deep) break;
+        const double* x = lds + (k0 + g * subs + sub) * TT;
 #pragma unroll
-          for (int t = 0; t < TT; ++t) acc[t] = __builtin_fma(v, lds[kk * TT + t], acc[t]);
+        for (int i = 0; i < GROUP; ++i) {
+          const double v = widen(now[g + i]);
+#pragma unroll
+          for (int t = 0; t < TT; ++t) acc[t] = __builtin_fma(v, x[i * subs * TT + t], acc[t]);
         }
       }
     }
@@ -236,9 +248,6 @@ struct Experts {
   float join;          // and a part of K where there are several
   int most;            // parts of K
 };
-
-// An offset past the range of every buffer here: zeros, and no memory is read.  The rows that an item does not have are read there.
-constexpr uint32_t kNowhere = 0x80000000u;
 
 // An item of work: up to `tile` slots of an expert, a block of columns, a part of K.
 struct Item {
@@ -496,11 +505,11 @@ struct MoeShared {
   int total, found;
 };
 
-// Items, from ids.  Up to 64 slots every wave keeps them in a register and goes through the experts that it finds there; beyond,
-// the work-group counts the slots of every expert in LDS.  Either way a wave finds its item and rows without a barrier.
+// Items, from ids.  Up to 64 slots every wave keeps them in its lanes, an expert's units with the first of its slots; beyond, the
+// work-group counts the slots of every expert in LDS.  Either way a wave finds its item and rows without a barrier.
 template <int TILE>
 struct Items {
-  int id;       // few slots: this lane's
+  int id, count, unit0, unit1;  // few slots: this lane's, its expert's slots and units, where it is the expert's first
   bool few;
   int units, splits, per;  // per: steps of a part
   __device__ __forceinline__ static int chunks(int slots) { return (slots + TILE - 1) / TILE; }
@@ -509,15 +518,25 @@ struct Items {
     const int tid = threadIdx.x, lane = tid & 63, slots = a.T * a.k;
     few = slots <= 64;
     id = -1;
-    units = 0;
+    count = unit0 = unit1 = 0;
     if (few) {
       if (lane < slots) id = a.ids[lane];
       if (id >= a.E) id = -1;
-      for (uint64_t left = __ballot(id >= 0); left;) {
-        const uint64_t same = __ballot(id == __builtin_amdgcn_readlane(id, __builtin_ctzll(left)));
-        units += chunks(__builtin_popcountll(same)) * a.blocks;
-        left &= ~same;
+      bool first = id >= 0;
+      for (int i = 0; i < slots; ++i) {
+        const bool same = id == __builtin_amdgcn_readlane(id, i);
+        count += same;
+        first &= !same || i >= lane;
       }
+      const int mine = first ? chunks(count) * a.blocks : 0;
+      unit1 = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int v = __shfl_up(unit1, d);
+        if (lane >= d) unit1 += v;
+      }
+      unit0 = unit1 - mine;
+      units = __builtin_amdgcn_readlane(unit1, 63);
     } else {
       for (int e = tid; e < a.E; e += Shared::kThreads) s.count[e] = 0;
       __syncthreads();
@@ -577,19 +596,13 @@ struct Items {
     Item it;
     it.slots = s.rows[copy][wave];
     it.split = n / units;
-    int in = n - it.split * units, count = 0;
+    int in = n - it.split * units, total;
     it.expert = 0;
     if (few) {
-      for (uint64_t left = __ballot(id >= 0); left;) {
-        const int e = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-        const uint64_t same = __ballot(id == e);
-        it.expert = e;
-        count = __builtin_popcountll(same);
-        const int here = chunks(count) * a.blocks;
-        if (in < here) break;
-        in -= here;
-        left &= ~same;
-      }
+      const int first = __builtin_ctzll(__ballot(in >= unit0 && in < unit1));
+      it.expert = __builtin_amdgcn_readlane(id, first);
+      total = __builtin_amdgcn_readlane(count, first);
+      in -= __builtin_amdgcn_readlane(unit0, first);
     } else {
       for (int e0 = 0; e0 < a.E; e0 += 64) {
         const int e = e0 + lane;
@@ -602,11 +615,11 @@ struct Items {
       }
       it.expert = uniform(it.expert);
       in -= uniform(s.start[it.expert]);
-      count = uniform(s.count[it.expert]);
+      total = uniform(s.count[it.expert]);
     }
     it.block = in % a.blocks;
     it.first = in / a.blocks * TILE;
-    it.rows = min(TILE, count - it.first);
+    it.rows = min(TILE, total - it.first);
     int before = -it.first;
     for (int i0 = 0; i0 < slots; i0 += 64) {
       const int i = i0 + lane;
@@ -965,7 +978,7 @@ namespace {
 
 int status(hipError_t e) { return e == hipSuccess ? MLP2_OK : record_error(MLP2_ERR_HIP); }
 
-constexpr int kRouteTokens = 8;
+constexpr int kRouteGroups = 1024;
 // K of a part of the router: 32 parts, of 64 to 512 each (more than 32 only for H > 16384).
 int route_part(int64_t H) {
   const int64_t per = round_up((H + 31) / 32, 64);
@@ -975,16 +988,19 @@ int route_part(int64_t H) {
 template <class W>
 hipError_t route(const mlp2_moe_s* p, int64_t T, const void* X, const void* Wr, int32_t* ids, float* gates, hipStream_t s) {
   Route a{(const uint16_t*)X, Wr, p->logits, p->routed, ids, gates, (int)T, (int)p->H, p->E, p->k, 1, 0, 0};
+  a.width = 3;  // 8 experts at least: the padded rows of K (four of a thread) fit the room for the most of K
   while (1 << a.width < p->E && a.width < 8) ++a.width;
-  // Tokens of a group share the reads of Wr, and are chosen for by four waves: four of them, eight where there are many.
-  const int tokens = T == 1 ? 1 : T <= 64 ? kRouteTokens / 2 : kRouteTokens;
-  const int64_t groups = (T + tokens - 1) / tokens;
   a.per = route_part(p->H);
   a.splits = (int)((p->H + a.per - 1) / a.per);
+  // Tokens of a work-group share the reads of Wr, but follow each other in its sums: as few as keep the work-groups down to kRouteGroups.
+  // (us, fp32 or bf16 router, one, two and four tokens: 9 x 1024, 251 experts 10.2, 12.5, 16.8; 48 x 4096, 32 experts 8.8, 7.8, 8.2;
+  // 128 x 4096, 128 experts 21.1, 17.5, 17.0; eight were slower than four throughout.)
+  const int tokens = T * a.splits <= kRouteGroups ? 1 : T * a.splits <= 2 * kRouteGroups ? 2 : 4;
+  const int64_t groups = (T + tokens - 1) / tokens;
   const dim3 grid((unsigned)groups, (unsigned)a.splits);
   if (tokens == 1) k_moe_route<W, 1><<<grid, 256, 0, s>>>(a);
-  else if (tokens < kRouteTokens) k_moe_route<W, kRouteTokens / 2><<<grid, 256, 0, s>>>(a);
-  else k_moe_route<W, kRouteTokens><<<grid, 256, 0, s>>>(a);
+  else if (tokens == 2) k_moe_route<W, 2><<<grid, 256, 0, s>>>(a);
+  else k_moe_route<W, 4><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -1109,7 +1125,7 @@ mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, in
   p->nb = act == MLP2_ACT_SWIGLU ? 2 : 1;
   p->device = device;
   p->num_cus = cus;
-  const int64_t slots = max_tokens * k, groups = (max_tokens + kRouteTokens - 1) / kRouteTokens + 16;  // up to 64 tokens: of four
+  const int64_t slots = max_tokens * k, groups = max_tokens < kRouteGroups ? max_tokens : max_tokens / 4 + kRouteGroups;
   // room for 16 parts of K of either product while they are small; one part of the second always fits
   const int64_t wide = p->nb * F > H ? p->nb * F : H, all = kMostParts * slots * wide, few = (int64_t)16 << 20, one = slots * H;
   p->part_floats = all < few ? all : one > few ? one : few;

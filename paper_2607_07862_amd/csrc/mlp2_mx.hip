@@ -272,7 +272,7 @@ int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const 
                      void* codes, void* scales, void* values, void* stream) {
   if (count < 0 || rows < 0 || cols < 0 || (down != 0 && down != 1) || (dtype != MLP2_DTYPE_BF16 && dtype != MLP2_DTYPE_F32))
     return record_error(MLP2_ERR_INVALID_ARG);
-  if (count > 65535 || rows > (1 << 20) || cols > (1 << 20)) return record_error(MLP2_ERR_UNSUPPORTED);
+  if (count > 65535 || rows > (1 << 20) || cols > (1 << 20) || ldx > (int64_t)1 << 40 || matrix_stride > (int64_t)1 << 40) return record_error(MLP2_ERR_UNSUPPORTED);
   if (count == 0 || rows == 0 || cols == 0) return MLP2_OK;
   if (!X || !codes || !scales || ldx < cols || (count > 1 && matrix_stride < (rows - 1) * ldx + cols)) return record_error(MLP2_ERR_INVALID_ARG);
   const int64_t size = dtype == MLP2_DTYPE_F32 ? 4 : 2;

@@ -187,6 +187,23 @@ def test_nan_and_infinity_stay_with_their_tokens(lib):
     assert hit.any() and torch.equal(Y.isnan().any(dim=1), hit) and Y[hit][:, 100].isnan().all()
 
 
+@pytest.mark.parametrize("T", [1, 40])
+def test_infinite_weight(lib, T):
+    """An infinity in W2 makes its column infinite or NaN for the tokens that chose the expert, and nothing else."""
+    H, F, E, k = 192, 128, 4, 2
+    plan, X, Wr, W1, W2, _ = case(T, H, F, E, k, B.ACT_GELU_TANH)
+    clean, ids, gates = outputs(T, H, k)
+    plan.forward(X, Wr, W1, W2, clean, ids, gates)
+    e = int(ids[0, 0])
+    W2[e, 5, 70] = float("inf")
+    Y = torch.full_like(clean, float("nan"))
+    plan.experts(X, ids, gates, W1, W2, Y)
+    hit = (ids == e).any(dim=1)
+    assert not Y[hit][:, 70].isfinite().any()
+    Y[hit, 70], clean[hit, 70] = 0, 0
+    assert torch.equal(Y, clean)
+
+
 def test_extreme_scales_of_weights(lib):
     """Scales 0 and 255 of a 4-bit expert: 2^-127, and NaN in the columns that have it."""
     T, H, F, E, k = 3, 128, 128, 2, 1

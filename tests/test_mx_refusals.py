@@ -26,6 +26,7 @@ def test_plans_refuse_before_touching_a_device(clib, args, code):  # noqa: F811
 @pytest.mark.parametrize("change,code", [
     ({0: -1}, B.ERR_INVALID_ARG), ({1: -1}, B.ERR_INVALID_ARG), ({2: -1}, B.ERR_INVALID_ARG), ({3: 2}, B.ERR_INVALID_ARG), ({5: 2}, B.ERR_INVALID_ARG),
     ({0: 65536}, B.ERR_UNSUPPORTED), ({1: (1 << 20) + 1}, B.ERR_UNSUPPORTED),
+    ({6: (1 << 40) + 1}, B.ERR_UNSUPPORTED), ({7: (1 << 40) + 1}, B.ERR_UNSUPPORTED),
     ({4: None}, B.ERR_INVALID_ARG), ({8: None}, B.ERR_INVALID_ARG), ({9: None}, B.ERR_INVALID_ARG),
     ({6: 63}, B.ERR_INVALID_ARG), ({7: 64 * 3}, B.ERR_INVALID_ARG),
     ({4: P + 1}, B.ERR_ALIGNMENT), ({8: 9 * P + 8}, B.ERR_ALIGNMENT), ({9: 17 * P + 4}, B.ERR_ALIGNMENT), ({10: 25 * P + 1}, B.ERR_ALIGNMENT),
