@@ -4,9 +4,10 @@
 //   Y[t] = sum over j of gates[t][j] * (act(X[t] W1[e]) W2[e]),  e = ids[t][j]
 //
 // Three launches: the router, the first products with the activation, the second products with the weighted sum.  A few tokens
-// reach few rows of every expert, so the products are bound by the stream of the experts' weights.  They go from memory to
+// reach few rows of every expert, so the products are bound by the stream of the experts' weights.  In bf16 they go from memory to
 // registers without LDS: a wave takes 128 columns and every fourth (of four waves) step of K, 16 bytes a lane and load, eight loads
-// a step, the next step's in flight while this one is multiplied; the waves' sums meet in LDS at the end.
+// a step, the next step's in flight while this one is multiplied; the waves' sums meet in LDS at the end.  In 4 bits they go through
+// LDS.
 //
 // A row here is a slot: row r = t k + j is token t with its j-th expert.  Every work-group counts the slots of each expert by
 // itself, from ids (at most 8192 words), and finds the items of work from that: an item is an expert with at least one slot, up to
@@ -258,9 +259,15 @@ struct Item {
 // Weights as they lie in the rest of the library, [K, N] in bf16.  A lane loads 8 columns of 8 consecutive k; taken by columns,
 // with one byte permute for each pair, those are the 8 operands (16 columns, 8 k a lane) of eight instructions, the columns of
 // instruction j being j, 8 + j, 16 + j, ...
+//
+// 470 MB of first weights stream in 83 us (5.6 TB/s; one token, two experts of 4096 x 14336), 577 MB in 102 (16 tokens, 50 experts of
+// 2048 x 1408); without the mark that the weights are read once, 113 us there.  The second products, with the sum over experts behind them,
+// 235 MB in 45 and 288 in 64: there 800 items meet 768 places of work-groups, or a multiple.  Two or four steps in registers and ITEM of 4
+// to 32 were all the same.
 struct Bf16Weights {
   static constexpr int STEP = 32;  // K of a step (of one wave)
   static constexpr int ITEM = 8;   // what an item costs beside its steps
+  static constexpr int NARROW = 2;  // slots an expert up to which items have one block of 16 rows
   static constexpr int most(bool second) { return second ? 2 : 4; }  // blocks of 16 rows that one pass over the weights serves
   static constexpr int WAVES = kWaves, COPIES = 4, ROWS = 64;  // copies of sums in LDS; rows of an item, at most
   static constexpr int RING = 2;   // steps in registers
@@ -362,10 +369,15 @@ struct Bf16Weights {
 // and 512 bytes of each X row, brought by direct-to-LDS loads of whole lines into a ring of stages.  Every wave multiplies a quarter
 // of the stage's k with half of its rows.  A lane turns 16 codes of a row into two bf16 operands (exactly: two significant bits and a power of
 // two).  Two waves to a SIMD: with one, reads, conversions and products waited for each other (3.8 TB/s).
+//
+// 570 MB of first weights stream in 114 us (5.0 TB/s; 48 tokens, four each of 32 experts, 4096 x 4096), 285 of second ones in 70: Z's two
+// numbers are twice the products and reads of X there (with one number 60; both in one block of 16 rows where there are at most eight
+// tokens, 73).  Five stages in place of four gained nothing.
 struct MxWeights {
   static constexpr int WAVES = 8, COPIES = 2, ROWS = 32;
   static constexpr int STEP = 256;  // (of all waves)
   static constexpr int ITEM = 2;
+  static constexpr int NARROW = 6;
   static constexpr int most(bool second) { return second ? 1 : 2; }
   static constexpr int resident(int) { return 1; }
   static constexpr int cols(bool gated) { return gated ? 64 : 128; }   // result columns of an item
@@ -1005,12 +1017,15 @@ hipError_t route(const mlp2_moe_s* p, int64_t T, const void* X, const void* Wr, 
 }
 
 // Whether items hold up to 16 rows of an expert only: with few slots an expert, more rows than that are rare (they make a second item,
-// which streams the weights again), and the smaller kernel leaves more work-groups to a CU.
-bool narrow(int64_t slots, int E) { return slots <= 16 || slots <= 6ll * E; }
+// which streams the weights again), and the smaller kernel leaves more work-groups to a CU.  (us, narrow and not, swiglu: 64 bf16 experts of
+// 1024 x 1408, three slots each 102 and 97, six 113 and 105, 12 138 and 118; 16 of 2048 x 4096 16 each 188 and 161; 217 of 768 x 768 with one
+// each 63 and 71.  4 bits: 64 experts, three each 60 and 62; 32 of 4096 x 4096, six each 186 and 193; 16 of 2048 x 4096, 12 each 83 and 78.)
+template <class Weights>
+bool narrow(int64_t slots, int E) { return slots <= (int64_t)Weights::NARROW * E; }
 
 template <class Weights, int ACT, bool SECOND>
 void launch(const Experts& a, unsigned grid, hipStream_t s) {
-  const bool few = narrow((int64_t)a.T * a.k, a.E);
+  const bool few = narrow<Weights>((int64_t)a.T * a.k, a.E);
   if constexpr (std::is_same_v<Weights, Bf16Weights>) {
     if (few) k_moe_bf16<ACT, 1, SECOND><<<grid, 256, 0, s>>>(a);
     else k_moe_bf16<ACT, Weights::most(SECOND), SECOND><<<grid, 256, 0, s>>>(a);
@@ -1025,7 +1040,7 @@ hipError_t experts(const mlp2_moe_s* p, int64_t T, const void* X, const int32_t*
                    const void* W2s, void* Y, hipStream_t s) {
   const int64_t slots = T * p->k, active = slots < p->E ? slots : p->E;  // experts that have a slot, at most
   auto fill = [&](Experts& a, bool second, int64_t K, int64_t N, int64_t width, bool gated, float join) {  // width: floats of a slot's part
-    const int most_blocks = narrow(slots, p->E) ? 1 : Weights::most(second);
+    const int most_blocks = narrow<Weights>(slots, p->E) ? 1 : Weights::most(second);
     const int64_t resident = (int64_t)Weights::resident(most_blocks) * p->num_cus;  // work-groups that the chip holds at once
     const int64_t tile = 16 * most_blocks, room = p->part_floats / (slots * width);
     a.K = (int)K;

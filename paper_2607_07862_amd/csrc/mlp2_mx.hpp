@@ -10,10 +10,15 @@
 // and operand: the same bytes, lanes and cycles as 16 x 16 x 32 of bf16.  So the
 // tiles, rings and slots are those of the 16-bit products (a stage of 64 16-bit
 // elements holds 256 of K) and the estimates that choose tile and split count K in
-// units of 64 x 16 bits.  What comes on top are the scales: two words a row and
-// stage, one more direct-to-LDS load (4 bytes a lane) for each wave and side.  They
-// are not hidden: the loop of the 256 x 256 tile takes 241 us without them, 290
-// with a load a panel and 16-bit reads (4096 x 14336 x 4096, gated).
+// units of 64 x 16 bits.  (Of 14 products from 1 x 4096 x 14336 to 4096 cubed the
+// choice was the best of every tile with 1 to 16 parts, or within 12 % of it: 7.3
+// against 6.6 us for 16 x 4096 x 4096, 8.7 against 8.1 for 128 rows of it.)  What
+// comes on top are the scales: two words a row and stage, one more direct-to-LDS
+// load (4 bytes a lane) for each wave and side.
+//
+// Few rows are bound by the weights (64 x 14336 x 4096, gated: 64 MB in 12.6 us, partly
+// out of the caches), many by the matrix cores and their power (4096 x 14336 x 4096,
+// gated: 240 us, 4.0 PFLOP/s; matrix cores busy for 44 % of the clocks, at 2 GHz).
 //
 // K is dealt to the lanes so that a lane's two 16-byte chunks of a stage are
 // neighbours, chunks 2 g and 2 g + 1 for lane group g = lane / 16: their scales are
@@ -311,6 +316,9 @@ __device__ __forceinline__ void mx_loop(const MxSide& rs, const MxSide& cs, int 
   __syncthreads();
 }
 
+// (Tried for it: four waves of 128 x 128 each, which read a third less from LDS, 300 us for the case above; requests between the
+// products in place of between the slots, 248; both against 239 as it is.)
+//
 // The ping-pong loop of the 256 x 256 tile: the slots, visibility and reuse of product_pingpong.  The scales of all rows come with panel A0
 // (its load is three of a wave, two of codes and one of scales) and are read with it, those of all columns with B0; so they are requested
 // again where those panels are, two slots after they were read.  The waits count the loads of the five panels behind the one waited for.
@@ -507,7 +515,8 @@ __global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   };
   Acc<T> acc;
   if constexpr (T::QUAD) {
-    // One work-group to a CU goes through several tiles, and requests the next tile's first stages before it stores this one's results.
+    // One work-group to a CU goes through several tiles, and requests the next tile's first stages before it stores this one's results
+    // (267 us for 4096 x 14336 x 4096 gated with a launch's work-group for each tile, 239 so).
     const MxLanes<T, false> rl(a.r);
     const MxLanes<T, true> cl(a.c);
     const int items = a.items();
