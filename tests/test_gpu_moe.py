@@ -92,6 +92,43 @@ def test_larger(lib, T, H, F, E, k, w, router):
     check(T, H, F, E, k, B.ACT_SWIGLU, w, router)
 
 
+@pytest.mark.parametrize("w", ["bf16", "mxfp4"])
+@pytest.mark.parametrize("T,H,F,E,k,act", [(1, 2048, 1024, 3, 2, 2), (5, 1088, 2112, 6, 3, 1), (20, 2048, 1088, 3, 2, 0), (40, 1088, 1024, 3, 2, 2),
+                                           (100, 1024, 2112, 2, 2, 1)])
+def test_parts_of_k(lib, T, H, F, E, k, act, w):
+    """Few items: K is cut in parts, with slots in lanes and slots counted in LDS."""
+    check(T, H, F, E, k, act, w)
+
+
+@pytest.mark.parametrize("T,H,E,k,router", [(300, 256, 9, 2, BF), (515, 256, 70, 4, F32), (1030, 256, 257, 2, BF), (2000, 64, 5, 4, F32), (8192, 64, 3, 1, BF)])
+def test_many_tokens(lib, T, H, E, k, router):
+    """One, two and four tokens to a work-group of the router; up to the most slots."""
+    check(T, H, 64, E, k, B.ACT_IDENTITY, "bf16", router)
+
+
+@pytest.mark.parametrize("w", ["bf16", "mxfp4"])
+def test_largest_experts(lib, w):
+    """H and F of 32768, the second expert: weights past 4 GB, with four elements that are not zero."""
+    T, n = 3, 32768
+    W1, W2 = torch.zeros((2, n, n), dtype=BF, device="cuda"), torch.zeros((2, n, n), dtype=BF, device="cuda")
+    W1[1, n - 1, n - 1], W1[1, 0, n - 1] = 1, 2
+    W2[1, n - 1, n - 1], W2[1, n - 1, 0] = 1, 3
+    if w == "mxfp4":
+        a, b = B.MxMatrix(n, n, 2), B.MxMatrix(n, n, 2)
+        B.mx_quantize(W1, a, down=True)
+        B.mx_quantize(W2, b, down=True)
+        W1, W2 = a, b
+    gen = torch.Generator().manual_seed(1)
+    X = bf16(gen, (T, n)).cuda()
+    ids, gates = torch.ones((T, 1), dtype=torch.int32, device="cuda"), torch.ones((T, 1), device="cuda")
+    Y = torch.full((T, n), float("nan"), dtype=BF, device="cuda")
+    B.MoePlan(T, n, n, 2, 1, B.ACT_IDENTITY, BF if w == "bf16" else "mxfp4").experts(X, ids, gates, W1, W2, Y)
+    z = f64(X[:, n - 1]) + 2 * f64(X[:, 0])
+    ref = np.zeros((T, n))
+    ref[:, n - 1], ref[:, 0] = z, 3 * z
+    assert_within(Y, ref, (U16 + 2 * U16 * U16) * np.abs(ref), "Y")  # the intermediate's two roundings (2^-16) and Y's
+
+
 def test_fewer_tokens_than_planned(lib):
     plan = B.MoePlan(150, 128, 192, 10, 3, B.ACT_GELU_TANH)
     for T in (150, 1, 16, 17, 9, 64, 149, 2):

@@ -87,6 +87,21 @@ def test_extreme_scales(lib, M):
     assert_within(Y, ref, tol, "Y")
 
 
+@pytest.mark.parametrize("M", [1, 300])
+def test_largest_depth(lib, M):
+    """K of 2^18 and codes past 4 GB: all ones under scales that differ from row to row, so that every result is exact."""
+    N, K = 1 << 16, 1 << 18
+    A, W = B.MxMatrix(M, K), B.MxMatrix(N, K)
+    A.codes.fill_(0x22)
+    A.scales.fill_(127)
+    W.codes.fill_(0x22)
+    power = torch.arange(N, device="cuda") % 5
+    W.scales.copy_((125 + power).to(torch.uint8).view(1, 1, N, 1).expand_as(W.scales))
+    Y = torch.full((M, N), float("nan"), device="cuda")
+    B.MxPlan(M, N, K, B.ACT_IDENTITY, F32).product(A, W, Y)
+    assert torch.equal(Y, (K * 2.0 ** (power - 2)).float().expand_as(Y))
+
+
 def test_same_bits_every_time(lib):
     """Parts of K are joined in one order, whichever work-group comes last."""
     plan, A, W, Y = check(16, 320, 16384, 0, F32)
