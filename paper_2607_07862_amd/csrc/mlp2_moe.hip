@@ -380,14 +380,14 @@ struct MxWeights {
   static constexpr int ITEM = 2, FEWEST = 2;
   static constexpr int NARROW = 6;
   static constexpr int most(bool second) { return second ? 1 : 2; }
-  static constexpr int resident(int) { return 1; }
+  static constexpr int resident(int) { return 2; }
   static constexpr int cols(bool gated) { return gated ? 64 : 128; }   // result columns of an item
   static constexpr int UP_WAVE = 0, UP_COL = 64;                       // where the second matrix's sums are
   static constexpr int J = 4;                                          // instruction groups of a wave: 16 columns each
   static constexpr int CODES = 16384, X0 = CODES + 1024;
   // by blocks of 16 rows of X (of Z two for each)
   static constexpr int stage(int xt) { return X0 + 8192 * xt; }
-  static constexpr int DEPTH = 4;  // stages of the ring
+  static constexpr int DEPTH = 2;  // stages of the ring
   static constexpr int loads(int xt) { return 2 + 1 + xt; }  // of a wave and stage
   __device__ static __forceinline__ int64_t matrix(const Experts& a) { return a.N * (mx_padded(a.K) / 2); }
 
@@ -488,7 +488,7 @@ struct MxWeights {
       }
   }
   // Where the four sums of instruction group j lie: columns 16 j + 4 g + i of the wave's half.  Two copies, to which two quarters of k each
-  // are added: with four there would be no room for the ring's last stage.
+  // are added: four would not fit a place of the ring.
   template <class Sums>
   __device__ static __forceinline__ void put(Sums& sum, const f32x4 (&c)[J]) {
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), k = wave % 4;
@@ -509,13 +509,15 @@ struct MoeShared {
   static constexpr int kWave = Weights::WAVES, kThreads = 64 * kWave;
   // (4-bit weights) the ring of stages, and the slots' experts: reading those from memory would wait for every stage in flight
   static constexpr bool kIds = RING > 0;
-  alignas(1024) char ring[RING ? RING : 16];
+  using Sums = float[Weights::COPIES][16][128 + 4];  // the waves' sums; behind the last item, tokens that are complete
+  alignas(1024) char ring[RING ? RING : sizeof(Sums)];
   int16_t ids[kIds ? kIdsInLds : 1];
-  float sum[Weights::COPIES][16][128 + 4];  // the waves' sums; behind the last item, tokens that are complete
   int count[kMostExperts];  // slots of an expert
   int start[kMostExperts];  // its first unit (an expert's chunk of rows and a block of columns)
   int rows[2][kWave][Weights::ROWS];  // slots of an item and of the next one, a copy for each wave
   int total, found;
+  // The sums: in the place of the ring whose stage was multiplied last.
+  __device__ __forceinline__ Sums& sums(int place) { return *reinterpret_cast<Sums*>(ring + place); }
 };
 
 // Items, from ids.  Up to 64 slots every wave keeps them in its lanes, an expert's units with the first of its slots; beyond, the
@@ -650,12 +652,12 @@ struct Items {
 
 // The waves' sums of one block of rows meet in LDS.  Thread 16 r + c / 8 (of the first 256) gets eight columns of row r:
 // v those from column c on, and with a gate u those of the second matrix.
-template <class Weights, bool GATED, class Shared>
-__device__ __forceinline__ void collect(Shared& s, const f32x4 (&acc)[Weights::J], float (&v)[8], float (&u)[8]) {
+template <class Weights, bool GATED, class Sums>
+__device__ __forceinline__ void collect(Sums& sum, const f32x4 (&acc)[Weights::J], float (&v)[8], float (&u)[8]) {
   constexpr int SHARE = GATED && Weights::UP_WAVE ? Weights::UP_WAVE : Weights::COPIES;
   const int tid = thread_here(), r = tid / 16, c = 8 * (tid % 16);
   __syncthreads();  // the sums before these have been read
-  Weights::put(s.sum, acc);
+  Weights::put(sum, acc);
   __syncthreads();
   if (tid >= 256 || c >= Weights::cols(GATED)) return;
 #pragma unroll
@@ -664,8 +666,8 @@ __device__ __forceinline__ void collect(Shared& s, const f32x4 (&acc)[Weights::J
   for (int i = 0; i < SHARE; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      v[e] += s.sum[i][r][c + e];
-      if (GATED) u[e] += s.sum[Weights::UP_WAVE + i][r][Weights::UP_COL + c + e];
+      v[e] += sum[i][r][c + e];
+      if (GATED) u[e] += sum[Weights::UP_WAVE + i][r][Weights::UP_COL + c + e];
     }
 }
 
@@ -689,8 +691,8 @@ __device__ __forceinline__ void store_z(const Experts& a, int slot, int col, con
 }
 
 // Z = act(X W1) of the item's rows, or a part of X W1, from the waves' sums.
-template <class Weights, int ACT, int MT, int TILE, class Shared>
-__device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const Items<TILE>& items, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
+template <class Weights, int ACT, int MT, int TILE, class Sums>
+__device__ __forceinline__ void finish_first(Sums& sum, const Experts& a, const Items<TILE>& items, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
   constexpr bool GATED = ACT == ACT_SWIGLU;
   constexpr int NB = GATED ? 2 : 1, COLS = Weights::cols(GATED);
   const int tid = thread_here(), r = tid / 16, c = 8 * (tid % 16), col = it.block * COLS + c;
@@ -700,7 +702,7 @@ __device__ __forceinline__ void finish_first(Shared& s, const Experts& a, const 
   for (int m = 0; m < MT; ++m) {
     if (16 * m >= it.rows) break;
     float v[8], u[8];
-    collect<Weights, GATED>(s, acc[m], v, u);
+    collect<Weights, GATED>(sum, acc[m], v, u);
     if (tid >= 256 || c >= COLS || col >= a.N || 16 * m + r >= it.rows) continue;
     const int slot = it.slots[16 * m + r];
     if (items.splits == 1) {
@@ -764,8 +766,8 @@ __device__ __forceinline__ void join_first(Shared& s, const Experts& a, const It
 }
 
 // The item's part of Z W2, to memory.
-template <class Weights, int MT, class Shared>
-__device__ __forceinline__ void finish_second(Shared& s, const Experts& a, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
+template <class Weights, int MT, class Sums>
+__device__ __forceinline__ void finish_second(Sums& sum, const Experts& a, const Item& it, const f32x4 (&acc)[MT][Weights::J]) {
   const int tid = thread_here(), r = tid / 16, col = it.block * 128 + 8 * (tid % 16);
   const int64_t slots = (int64_t)a.T * a.k;
   const Far part(a.part);
@@ -773,7 +775,7 @@ __device__ __forceinline__ void finish_second(Shared& s, const Experts& a, const
   for (int m = 0; m < MT; ++m) {
     if (16 * m >= it.rows) break;
     float v[8], u[8];
-    collect<Weights, false>(s, acc[m], v, u);
+    collect<Weights, false>(sum, acc[m], v, u);
     if (tid >= 256 || col >= a.N || 16 * m + r >= it.rows) continue;
     const uint32_t to = (uint32_t)((it.split * slots + it.slots[16 * m + r]) * a.N + col) * 4;
     part.store16(to, f32x4{v[0], v[1], v[2], v[3]});
@@ -826,8 +828,8 @@ __device__ __forceinline__ void join_second(Shared& s, const Experts& a, const I
   struct Done {
     uint32_t token, valid;  // token: its block of columns in the upper half
   };
-  constexpr int ROOM = sizeof(s.sum) / sizeof(Done);
-  Done* done = reinterpret_cast<Done*>(s.sum);
+  constexpr int ROOM = sizeof(typename Shared::Sums) / sizeof(Done);
+  Done* done = reinterpret_cast<Done*>(s.ring);
   wait_all_mem();
   if (tid == 0) s.found = 0;
   __syncthreads();
@@ -889,8 +891,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Bf16Weights
       constexpr int MT = decltype(mt)::value;
       f32x4 acc[MT][8];
       Bf16Weights::stream<MT, ACT == ACT_SWIGLU && !SECOND, SECOND>(it, a, items.from(it), items.end(a, it), acc);
-      if constexpr (SECOND) finish_second<Bf16Weights, MT>(s, a, it, acc);
-      else finish_first<Bf16Weights, ACT, MT>(s, a, items, it, acc);
+      if constexpr (SECOND) finish_second<Bf16Weights, MT>(s.sums(0), a, it, acc);
+      else finish_first<Bf16Weights, ACT, MT>(s.sums(0), a, items, it, acc);
     };
     if (MOST == 1 || it.rows <= 16) run(int_constant<1>());
     else if (MOST > 2 && it.rows <= 32) run(int_constant<2>());
@@ -904,11 +906,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(Bf16Weights
   }
 }
 
-// Items of 4-bit weights.  A work-group has most of a CU's LDS to itself, so nothing else would stream while it ends an item: its
-// requests run on into the next item's stages.  An item with fewer stages than are in flight is filled up with empty ones, so that
-// requests are never more than one item ahead.
+// Items of 4-bit weights.  Requests run on into the next item's stages while one ends (an item with fewer stages than are in flight is
+// filled up with empty ones, so that requests are never more than one item ahead), and one of two work-groups to a CU streams while the
+// other multiplies or ends an item: with one, of four stages, the first products above took 120 us in place of 107, those of 54 slots of 251
+// experts of 1024 x 2112 41 in place of 33.
 template <int ACT, int MT, bool SECOND>
-__global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k_moe_mx(const Experts a) {
   using W = MxWeights;
   constexpr int XT = SECOND ? 2 * MT : MT, NS = W::DEPTH, STAGE = W::stage(XT);
   constexpr bool GATED = ACT == ACT_SWIGLU && !SECOND;
@@ -958,8 +961,9 @@ __global__ __launch_bounds__(512) void k_moe_mx(const Experts a) {
         }
         at = at == NS - 1 ? 0 : at + 1;
       }
-      if constexpr (SECOND) finish_second<W, MT>(s, a, it, acc);
-      else finish_first<W, ACT, MT>(s, a, items, it, acc);
+      auto& sums = s.sums((at == 0 ? NS - 1 : at - 1) * STAGE);  // requested into again behind the next barrier
+      if constexpr (SECOND) finish_second<W, MT>(sums, a, it, acc);
+      else finish_first<W, ACT, MT>(sums, a, items, it, acc);
       it = next;  // (the last item's requests stay with it)
     }
     wait_vm<0>();  // no load is left that writes LDS
