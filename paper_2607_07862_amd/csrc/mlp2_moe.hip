@@ -371,14 +371,13 @@ struct Bf16Weights {
 // of the stage's k with half of its rows.  A lane turns 16 codes of a row into two bf16 operands (exactly: two significant bits and a power of
 // two).  Two waves to a SIMD: with one, reads, conversions and products waited for each other (3.8 TB/s).
 //
-// 570 MB of first weights stream in 114 us (5.0 TB/s; 48 tokens, four each of 32 experts, 4096 x 4096), 285 of second ones in 70: Z's two
-// numbers are twice the products and reads of X there (with one number 60; both in one block of 16 rows where there are at most eight
-// tokens, 73).  Five stages in place of four gained nothing.
+// 570 MB of first weights stream in 105 us (5.4 TB/s; 48 tokens, four each of 32 experts, 4096 x 4096), 285 of second ones in 64: Z's two
+// numbers are twice the products and reads of X there, which cost a sixth of the time.
 struct MxWeights {
   static constexpr int WAVES = 8, COPIES = 2, ROWS = 32;
   static constexpr int STEP = 256;  // (of all waves)
   static constexpr int ITEM = 2, FEWEST = 2;
-  static constexpr int NARROW = 6;
+  static constexpr int NARROW = 8;
   static constexpr int most(bool second) { return second ? 1 : 2; }
   static constexpr int resident(int) { return 2; }
   static constexpr int cols(bool gated) { return gated ? 64 : 128; }   // result columns of an item
@@ -1024,7 +1023,7 @@ hipError_t route(const mlp2_moe_s* p, int64_t T, const void* X, const void* Wr, 
 // Whether items hold up to 16 rows of an expert only: with few slots an expert, more rows than that are rare (they make a second item,
 // which streams the weights again), and the smaller kernel leaves more work-groups to a CU.  (us, narrow and not, swiglu: 64 bf16 experts of
 // 1024 x 1408, three slots each 102 and 97, six 113 and 105, 12 138 and 118; 16 of 2048 x 4096 16 each 188 and 161; 217 of 768 x 768 with one
-// each 63 and 71.  4 bits: 64 experts, three each 60 and 62; 32 of 4096 x 4096, six each 186 and 193; 16 of 2048 x 4096, 12 each 83 and 78.)
+// each 63 and 71.  4 bits: 64 experts, three each 52 and 53; 32 of 4096 x 4096, eight each 170 and 174; 16 of 2048 x 4096, 16 each 84 and 73.)
 template <class Weights>
 bool narrow(int64_t slots, int E) { return slots <= (int64_t)Weights::NARROW * E; }
 
