@@ -369,7 +369,7 @@ struct Bf16Weights {
 // go through LDS, and X with them: a stage is 128 rows (with a gate 64 of either matrix) by 256 k of codes, two words of scales a row
 // and 512 bytes of each X row, brought by direct-to-LDS loads of whole lines into a ring of stages.  Every wave multiplies a quarter
 // of the stage's k with half of its rows.  A lane turns 16 codes of a row into two bf16 operands (exactly: two significant bits and a power of
-// two).  Two waves to a SIMD: with one, reads, conversions and products waited for each other (3.8 TB/s).
+// two).  Two waves of a work-group to a SIMD, as one's reads, conversions and products wait for each other (3.8 TB/s with one).
 //
 // 570 MB of first weights stream in 105 us (5.4 TB/s; 48 tokens, four each of 32 experts, 4096 x 4096), 285 of second ones in 64: Z's two
 // numbers are twice the products and reads of X there, which cost a sixth of the time.
