@@ -506,9 +506,9 @@ typedef struct mlp2_moe_s* mlp2_moe_t;
 mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, int64_t k, int act, int w_dtype);
 
 /* Y [T, H] bf16, ids [T, k] int32 and gates [T, k] fp32 from X [T, H] bf16 and the router's weight Wr [H, E] (wr_dtype bf16 or
- * F32): ids are the k largest logits X . Wr of a token in order, ties to the lowest index, NaN counting as the
- * largest; gates are the softmax over those k.  The logits are summed in fp64, so the choice is that of the exact ones but for
- * differences of 1e-15.  W1_scales and W2_scales are NULL for bf16 weights.  0 <= T <= max_tokens (0 does nothing). */
+ * F32): ids are the k largest logits X . Wr of a token in order, ties to the lowest index, NaN ahead of +infinity; gates are
+ * the softmax over those k (NaN where one of them is NaN or the largest is infinite).  The logits are summed in fp64, so the choice is
+ * that of the exact ones but for differences of 1e-15.  W1_scales and W2_scales are NULL for bf16 weights.  0 <= T <= max_tokens (0 does nothing). */
 int mlp2_moe_forward(mlp2_moe_t plan, int64_t T, const void* X, const void* Wr, int wr_dtype, const void* W1, const void* W1_scales,
                      const void* W2, const void* W2_scales, void* Y, void* ids, void* gates, void* stream);
 

@@ -92,7 +92,9 @@ __device__ __forceinline__ double wave_largest(double v) {
   return largest_of(largest_of(lane_value(v, 0), lane_value(v, 16)), largest_of(lane_value(v, 32), lane_value(v, 48)));
 }
 
-// The k largest of a token's logits (in LDS; ties: the lowest index; NaN counts as the largest) and the softmax over them, by one wave.
+// The k largest of a token's logits (in LDS; ties: the lowest index; NaN counts as larger than infinity) and the softmax over them, by one
+// wave.  Finite logits stay below 2^272 (at most 2^15 products of a bf16 and an fp32 number), so 2^1000 stands for infinity in the
+// comparisons and infinity for NaN.
 __device__ __forceinline__ void choose_experts(const double* logits, int E, int k, int32_t* ids, float* gates) {
   const int lane = threadIdx.x & 63;
   constexpr int PER = kMostExperts / 64;
@@ -101,7 +103,7 @@ __device__ __forceinline__ void choose_experts(const double* logits, int E, int 
   for (int i = 0; i < PER; ++i) {
     const int e = lane + 64 * i;
     v[i] = e < E ? logits[e] : 0.0;
-    if (v[i] != v[i]) v[i] = __builtin_huge_val();
+    v[i] = v[i] != v[i] ? __builtin_huge_val() : v[i] == __builtin_huge_val() ? 0x1p1000 : v[i];
   }
   uint32_t gone = 0;  // of this lane's experts, those that are chosen already or do not exist
 #pragma unroll
