@@ -461,10 +461,11 @@ void mlp2_ortho_destroy(mlp2_ortho_t plan);
 typedef struct mlp2_mx_s* mlp2_mx_t;
 
 /* Quantise `count` matrices X [rows, cols] of `dtype` (bf16 or F32; rows ldx
- * elements apart, matrices matrix_stride apart; any element's address) into
- * MXFP4, blocks of 32 along a row (down = 0: matrices [rows, K = cols]) or down
- * a column (down = 1: X is [K, N] as the library's weights are and becomes
- * matrices [N = cols, K = rows]).  A block's scale is 2^(floor(log2 max|x|) - 2), at least 2^-127;
+ * elements apart, matrices matrix_stride apart, one behind the other or beside
+ * each other as columns of one buffer; any element's address) into MXFP4, blocks
+ * of 32 along a row (down = 0: matrices [rows, K = cols]) or down a column
+ * (down = 1: X is [K, N] as the library's weights are and becomes matrices
+ * [N = cols, K = rows]).  A block's scale is 2^(floor(log2 max|x|) - 2), at least 2^-127;
  * codes are the nearest ones, ties to the even code, and 6 for what lies above; a
  * NaN or an infinity makes its block NaN (codes 0, scale 255).  `values` (or
  * NULL) receives what codes and scales stand for, bf16 [count, rows, cols] in

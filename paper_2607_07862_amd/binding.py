@@ -709,8 +709,8 @@ def mx_quantize(X, out: MxMatrix, values=None, down: bool = False, stream=None) 
     """Enqueue the quantisation of X, bf16 or float32 ``[rows, cols]`` or ``[count, rows, cols]``, into ``out``.
 
     Blocks of 32 lie along a row, so that ``out`` holds ``[rows, K = cols]``, or with ``down`` down a column: the library's weights
-    ``[K, N]`` become ``[N, K]``.  X's rows must be contiguous, at any distance.  ``values`` (bf16, X's shape, contiguous) receives
-    what the codes stand for."""
+    ``[K, N]`` become ``[N, K]``.  X's rows must be contiguous, at any distance; its matrices may be columns of one buffer.
+    ``values`` (bf16, X's shape, contiguous) receives what the codes stand for."""
     device = X.device
     current, raw_stream, bf16 = _torch_calls()
     code = _dtype_code(X.dtype)
@@ -726,7 +726,8 @@ def mx_quantize(X, out: MxMatrix, values=None, down: bool = False, stream=None) 
         _check_shape(values, "values", shape, bf16, device)
     ld = strides[-2] if rows > 1 else cols
     matrix = strides[0] if count > 1 else rows * ld
-    if (cols > 1 and strides[-1] != 1) or ld < cols or (count > 1 and matrix < (rows - 1) * ld + cols):
+    behind = count <= 1 or matrix >= (rows - 1) * ld + cols
+    if (cols > 1 and strides[-1] != 1) or ld < cols or not (behind or matrix >= cols and (count - 1) * matrix + cols <= ld):
         raise ValueError("X's rows must be contiguous and apart from each other")
     stream = raw_stream(device.index) if stream is None else _stream(stream, device)
     rc = _lib_of().mlp2_mx_quantize(count, rows, cols, 1 if down else 0, _ptr(X), code, ld, matrix, _ptr(out.codes), _ptr(out.scales),

@@ -275,12 +275,15 @@ int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const 
     return record_error(MLP2_ERR_INVALID_ARG);
   if (count > 65535 || rows > (1 << 20) || cols > (1 << 20) || ldx > (int64_t)1 << 40 || matrix_stride > (int64_t)1 << 40) return record_error(MLP2_ERR_UNSUPPORTED);
   if (count == 0 || rows == 0 || cols == 0) return MLP2_OK;
-  if (!X || !codes || !scales || ldx < cols || (count > 1 && matrix_stride < (rows - 1) * ldx + cols)) return record_error(MLP2_ERR_INVALID_ARG);
+  // several matrices: one behind the other, or beside each other in the rows of one buffer
+  const bool beside = count > 1 && matrix_stride >= cols && (count - 1) * matrix_stride + cols <= ldx;
+  if (!X || !codes || !scales || ldx < cols || (count > 1 && !beside && matrix_stride < (rows - 1) * ldx + cols)) return record_error(MLP2_ERR_INVALID_ARG);
   const int64_t size = dtype == MLP2_DTYPE_F32 ? 4 : 2;
   if ((((uintptr_t)codes | (uintptr_t)scales) & 15u) || (uintptr_t)X % size || (uintptr_t)values % 2) return record_error(MLP2_ERR_ALIGNMENT);
   const int64_t out = down ? cols : rows, kp = mx_padded(down ? rows : cols);
-  const Span x = count == 1 || matrix_stride == rows * ldx ? Span{X, cols * size, count * rows, ldx * size}
-                                                           : Span{X, ((count - 1) * matrix_stride + (rows - 1) * ldx + cols) * size};
+  const Span x = beside                                       ? Span{X, ((count - 1) * matrix_stride + cols) * size, rows, ldx * size}
+                 : count == 1 || matrix_stride == rows * ldx ? Span{X, cols * size, count * rows, ldx * size}
+                                                             : Span{X, ((count - 1) * matrix_stride + (rows - 1) * ldx + cols) * size};
   const Span in[] = {x}, outs[] = {{codes, count * out * kp / 2}, {scales, count * out * kp / kMxBlock}, {values, values ? count * rows * cols * 2 : 0}};
   if (outputs_overlap(in, outs)) return record_error(MLP2_ERR_INVALID_ARG);
   if (const int rc = usable_device()) return record_error(rc);
