@@ -252,7 +252,7 @@ hipError_t mx_product(const mlp2_mx_s* p, const MxSide& r, const MxSide& c, int6
     using T = decltype(tile);
     using P = MxProblem<Epi>;
     const P a = make_problem<T, P>(r, c, M, p->N, K, 1, epi, ch.split, p->split);
-    const int grid = T::QUAD && a.items() > p->num_cus ? p->num_cus : a.items();
+    const int grid = T::QUAD && a.split == 1 && a.items() > p->num_cus ? p->num_cus : a.items();
     k_mx_product<T, P><<<grid, T::THREADS, 0, s>>>(a);
     return hipGetLastError();
   });

@@ -515,8 +515,9 @@ __global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   };
   Acc<T> acc;
   if constexpr (T::QUAD) {
-    // One work-group to a CU goes through several tiles, and requests the next tile's first stages before it stores this one's results
-    // (267 us for 4096 x 14336 x 4096 gated with a launch's work-group for each tile, 239 so).
+    // One work-group to a CU goes through several whole tiles, and requests the next tile's first stages before it stores this one's results
+    // (267 us for 4096 x 14336 x 4096 gated with a launch's work-group for each tile, 239 so).  Parts of K, which meet through LDS, have a
+    // work-group each.
     const MxLanes<T, false> rl(a.r);
     const MxLanes<T, true> cl(a.c);
     const int items = a.items();
@@ -526,15 +527,11 @@ __global__ __launch_bounds__(T::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     for (;;) {
       loop.run(rl, cl, acc, lds);
       const int next = item + gridDim.x;
-      const bool more = next < items, ahead = more && a.split == 1;  // (parts of K meet through LDS)
+      const bool more = next < items;
       const Place q = more ? place_of(next) : p;
-      if (ahead) loop = MxPingPong<T>(a.r, a.c, rl, cl, q.tm * T::BM, q.tn * COLS, q.st0, q.nk, lds);
+      if (more) loop = MxPingPong<T>(a.r, a.c, rl, cl, q.tm * T::BM, q.tn * COLS, q.st0, q.nk, lds);
       finish_product<T>(a, acc, 0, p.tile, p.s, p.tm, p.tn, lds);
       if (!more) return;
-      if (!ahead) {
-        __syncthreads();
-        loop = MxPingPong<T>(a.r, a.c, rl, cl, q.tm * T::BM, q.tn * COLS, q.st0, q.nk, lds);
-      }
       item = next;
       p = q;
     }
