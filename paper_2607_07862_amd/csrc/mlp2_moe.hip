@@ -103,8 +103,10 @@ __device__ __forceinline__ void choose_experts(const double* logits, int E, int 
   for (int i = 0; i < PER; ++i) {
     const int e = lane + 64 * i;
     v[i] = e < E ? logits[e] : 0.0;
-    v[i] = v[i] != v[i] ? __builtin_huge_val() : v[i] == __builtin_huge_val() ? 0x1p1000 : v[i];
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (64 * i < E) v[i] = v[i] != v[i] ? __builtin_huge_val() : v[i] == __builtin_huge_val() ? 0x1p1000 : v[i];
   uint32_t gone = 0;  // of this lane's experts, those that are chosen already or do not exist
 #pragma unroll
   for (int i = 0; i < PER; ++i) gone |= lane + 64 * i >= E ? 1u << i : 0u;
