@@ -502,19 +502,22 @@ void mlp2_mx_destroy(mlp2_mx_t plan);
  * bits), so an infinite weight of W2 may give NaN where one factor would give an infinity.  All sums are fp32.  The workspace holds that
  * intermediate (4 bytes an element), up to 64 MB of partial sums or one fp32 [max_tokens * k, H] if that is more, and the router's: up
  * to 64 fp64 [max_tokens, E].
- * A plan's calls are ordered on one stream.  NULL on failure (mlp2_last_error). */
+ * A plan's calls are ordered on one stream.  NULL on failure (mlp2_last_error).
+ *
+ * Weights are streamed again for every 16 to 64 rows of an expert.  From about 32 rows an expert of a large layer on (128 tokens, two of
+ * eight experts of 4096 x 14336), some hundreds of a small one, mlp2_plan's MLP for each expert in turn is faster. */
 typedef struct mlp2_moe_s* mlp2_moe_t;
 mlp2_moe_t mlp2_moe_plan(int64_t max_tokens, int64_t H, int64_t F, int64_t E, int64_t k, int act, int w_dtype);
 
 /* Y [T, H] bf16, ids [T, k] int32 and gates [T, k] fp32 from X [T, H] bf16 and the router's weight Wr [H, E] (wr_dtype bf16 or
  * F32): ids are the k largest logits X . Wr of a token in order, ties to the lowest index, NaN ahead of +infinity; gates are
- * the softmax over those k (NaN where one of them is NaN or the largest is infinite).  The logits are summed in fp64, so the choice is
- * that of the exact ones but for differences of 1e-15.  W1_scales and W2_scales are NULL for bf16 weights.  0 <= T <= max_tokens (0 does nothing). */
+ * the softmax over those k (NaN where one of them is NaN or the largest is infinite).  The logits are summed in fp64, each off by less
+ * than H 2^-53 sum |x w|: the choice is that of the exact ones but for logits nearer to each other than that.  W1_scales and W2_scales are NULL for bf16 weights.  0 <= T <= max_tokens (0 does nothing). */
 int mlp2_moe_forward(mlp2_moe_t plan, int64_t T, const void* X, const void* Wr, int wr_dtype, const void* W1, const void* W1_scales,
                      const void* W2, const void* W2_scales, void* Y, void* ids, void* gates, void* stream);
 
 /* The same with the caller's ids and gates.  A slot whose id is outside [0, E)
- * is empty (-1 by convention; its gate is not read); a token without experts
+ * is empty (-1 by convention; its gate counts for nothing); a token without experts
  * gets zeros; an expert may stand in several slots of a token. */
 int mlp2_moe_experts(mlp2_moe_t plan, int64_t T, const void* X, const void* ids, const void* gates, const void* W1, const void* W1_scales,
                      const void* W2, const void* W2_scales, void* Y, void* stream);

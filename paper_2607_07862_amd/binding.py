@@ -680,7 +680,14 @@ class MxMatrix:
 
     @classmethod
     def of(cls, codes, scales, K: int) -> "MxMatrix":
-        """The matrices that these two tensors hold (not copied)."""
+        """The matrices that these two tensors hold (not copied).
+
+        Arrays of unpadded rows, codes ``[count, rows, K / 2]`` and one scale after the other ``[count, rows, K / 32]``, become these
+        with ``G = -(-K // 128)`` and ``pad = torch.nn.functional.pad``::
+
+            codes = pad(codes, (0, 64 * G - K // 2))
+            scales = pad(scales, (0, 4 * G - K // 32)).view(count, rows, G, 4).transpose(1, 2).contiguous()
+        """
         import torch
 
         if codes.dim() != 3:

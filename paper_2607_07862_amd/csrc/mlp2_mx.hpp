@@ -17,8 +17,11 @@
 // load (4 bytes a lane) for each wave and side.
 //
 // Few rows are bound by the weights (64 x 14336 x 4096, gated: 64 MB in 12.6 us, partly
-// out of the caches), many by the matrix cores and their power (4096 x 14336 x 4096,
-// gated: 240 us, 4.0 PFLOP/s; matrix cores busy for 44 % of the clocks, at 2 GHz).
+// out of the caches; 15.0 from memory), many by the matrix cores and their power (4096 x
+// 14336 x 4096, gated: 239 to 250 us on several machines, 3.85 to 4.0 PFLOP/s; matrix cores
+// busy for 44 % of the clocks, at 2 GHz).  Between them waits do: 777 x 2111 x 5441 takes
+// 15.6 us with LDS busy for 11 % of the clocks and the matrix cores for 9 %, its waves
+// waiting for 40 % of theirs.
 //
 // K is dealt to the lanes so that a lane's two 16-byte chunks of a stage are
 // neighbours, chunks 2 g and 2 g + 1 for lane group g = lane / 16: their scales are
