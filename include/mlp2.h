@@ -470,7 +470,7 @@ typedef struct mlp2_mx_s* mlp2_mx_t;
  * NaN or an infinity makes its block NaN (codes 0, scale 255).  `values` (or
  * NULL) receives what codes and scales stand for, bf16 [count, rows, cols] in
  * X's order; they are bf16 numbers, so nothing is rounded again.
- * 0 <= count <= 65535, 0 <= rows, cols <= 1<<20 (0: nothing to do), ldx and matrix_stride <= 1<<40, and at most 2^24 pieces of 32 x 128
+ * 0 <= count <= 65535, 0 <= rows, cols <= 1<<20 (0: nothing to do), ldx and matrix_stride <= 1<<40, and fewer than 2^24 pieces of 32 x 128
  * (down: 512 bytes of columns by 256 rows).  The current device, no workspace. */
 int mlp2_mx_quantize(int64_t count, int64_t rows, int64_t cols, int down, const void* X, int dtype, int64_t ldx, int64_t matrix_stride,
                      void* codes, void* scales, void* values, void* stream);
